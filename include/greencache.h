@@ -309,6 +309,62 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
                                         size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Rotary positions. A program whose projections hand over keys and queries without
+ * their position gives the rotation to the append: head elements x of the token at
+ * position p = P_r + i form rotary_dim / 2 pairs (a, b), and
+ *     y_a = x_a cos(p, j) - x_b sin(p, j),   y_b = x_b cos(p, j) + x_a sin(p, j)
+ * with pair j = 0 .. rotary_dim / 2 - 1. Elements from rotary_dim on keep their bits.
+ */
+typedef enum gc_rotary_pairs {
+    GC_PAIRS_HALVES = 0,     /* pair j is (j, j + rotary_dim / 2) */
+    GC_PAIRS_INTERLEAVED = 1 /* pair j is (2 j, 2 j + 1) */
+} gc_rotary_pairs;
+
+typedef struct gc_rotary {
+    const float* table_dev; /* device fp32 [num_positions][rotary_dim / 2][2]: cos, sin */
+    int32_t num_positions;  /* every position of the batch, max(P_r + n_r) of them, must have a row */
+    int32_t rotary_dim;     /* rotated elements of a head: a multiple of 16, 16 .. head_dim */
+    int32_t pairs;          /* a gc_rotary_pairs value; other values: GC_ERR_BAD_SHAPE */
+    int32_t reserved[5];    /* must be zero */
+} gc_rotary;
+
+/* The new tokens' projections: row t of each starts `stride` elements after row t - 1
+ * (a multiple of 8, at least heads * head_dim), its heads side by side. Views of one
+ * [T][Hq + 2 Hkv][D] buffer fit, and so do three packed tensors. */
+typedef struct gc_new_rows {
+    const void* q; /* bf16, Hq heads a row; NULL: no queries (q_out NULL too) */
+    const void* k; /* bf16, Hkv heads a row */
+    const void* v; /* bf16, Hkv heads a row */
+    int64_t q_stride, k_stride, v_stride;
+} gc_new_rows;
+
+/*
+ * gc_kv_append with the rotary position applied on the way: the rotated keys and the
+ * values as they are go to the slots gc_kv_append writes, and the rotated queries to
+ * q_out, in one launch. Rotation in fp32 (a product and a fused multiply-add), rounded
+ * once, to nearest even.
+ *   rows  : the projections; device memory, 16-byte aligned
+ *   q_out : device bf16 [T][Hq][D], 16-byte aligned: the q argument of the attention
+ *           calls. It may be rows->q where that is packed (q_stride == Hq * D), and
+ *           otherwise overlaps none of the inputs (else GC_ERR_BAD_SHAPE)
+ * A cached prefix is in the pool with its rotation, so restoring it (gc_kv_append)
+ * and appending to it mix freely. Errors: those of gc_kv_append, and GC_ERR_NULL_ARG
+ * for a missing table, rows->k or rows->v, or one of q and q_out without the other;
+ * GC_ERR_BAD_SHAPE for a rotary_dim, stride or alignment outside the above and for a
+ * table with fewer rows than the batch has positions.
+ */
+gc_status gc_kv_append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                              const gc_new_rows* rows, void* q_out, void* k_pool, void* v_pool,
+                              hipStream_t stream);
+
+/* The same into 8-bit pools: a key element is stored as the E4M3 code nearest to
+ * fl32(y * fl32(1 / k_scale)) of the fp32 rotated y (not rounded to bf16 in between),
+ * values and scales as gc_kv_append_fp8. */
+gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                                  const gc_new_rows* rows, void* q_out, float k_scale, float v_scale,
+                                  void* k_pool8, void* v_pool8, hipStream_t stream);
+
+/*
  * Calibration, not part of the attention path: read every byte of `buf`
  * (device memory, `bytes` a multiple of 16) once as a streaming reduction,
  * writing GC_READ_PROBE_SINK_WORDS 32-bit words to `sink` (device). Timing it

@@ -23,7 +23,8 @@ STATUS_NAMES = {0: "GC_OK", -1: "GC_ERR_NULL_ARG", -2: "GC_ERR_BAD_SHAPE", -3: "
                 -4: "GC_ERR_BLOCK_TABLE", -5: "GC_ERR_WORKSPACE", -6: "GC_ERR_HIP", -7: "GC_ERR_LENGTHS"}
 GC_ERR_LENGTHS = -7
 
-EXPORTED = ("gc_kv_append", "gc_prefix_prefill_workspace_size", "gc_prefix_prefill_plan",
+EXPORTED = ("gc_kv_append", "gc_kv_append_rotary", "gc_kv_append_rotary_fp8",
+            "gc_prefix_prefill_workspace_size", "gc_prefix_prefill_plan",
             "gc_prefix_prefill_run", "gc_prefix_prefill_attention", "gc_kv_append_fp8",
             "gc_prefix_prefill_run_fp8", "gc_prefix_prefill_attention_fp8", "gc_prefix_prefill_prepare",
             "gc_prefix_prefill_prepare_fp8", "gc_prefix_prefill_run_with_append",
@@ -67,6 +68,20 @@ class PlanOptions(ctypes.Structure):
                 ("reserved", ctypes.c_int32 * 6)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("table_dev", ctypes.c_void_p), ("num_positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 5)]
+
+
+class NewRows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+# gc_rotary_pairs values
+PAIRS_HALVES, PAIRS_INTERLEAVED = 0, 1
+
 # gc_tiling values
 TILES_AUTO, TILES_PREFILL, TILES_SMALL, TILES_WIDE = 0, 1, 2, 3
 
@@ -100,6 +115,11 @@ def load_library(path: str | None = None):
     for fn in (lib.gc_prefix_prefill_run_fp8, lib.gc_prefix_prefill_attention_fp8):
         fn.restype = i32
         fn.argtypes = [G, Bp, O, vp, vp, vp, f32, f32, f32, vp, vp, vp, ctypes.c_size_t, vp]
+    Ro, Nr = ctypes.POINTER(Rotary), ctypes.POINTER(NewRows)
+    lib.gc_kv_append_rotary.restype = i32
+    lib.gc_kv_append_rotary.argtypes = [G, Bp, Ro, Nr, vp, vp, vp, vp]
+    lib.gc_kv_append_rotary_fp8.restype = i32
+    lib.gc_kv_append_rotary_fp8.argtypes = [G, Bp, Ro, Nr, vp, f32, f32, vp, vp, vp]
     lib.gc_prefix_prefill_prepare.restype = i32
     lib.gc_prefix_prefill_prepare.argtypes = [G, Bp, O, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.gc_prefix_prefill_prepare_fp8.restype = i32
@@ -532,3 +552,130 @@ def prepare(k_new, v_new, k_pool, v_pool, batch: PagedBatch, num_q_heads, worksp
     else:
         st = lib.gc_prefix_prefill_prepare(*head, *tail)
         _check("gc_prefix_prefill_prepare", st, lib)
+
+
+# ----------------------------------------------------------------- rotary positions
+
+def rotary_table(positions, rotary_dim, base=10000.0, inv_freq=None, amplitude=1.0, device="cuda"):
+    """The (cos, sin) table of kv_append_rotary: float32 [positions][rotary_dim / 2][2], every angle
+    p * inv_freq[j] computed in 64 bits (fp32 angles of far positions are off by 1e-2 and more).
+    inv_freq: the rotary_dim / 2 frequencies, base ** (-2 j / rotary_dim) by default; pass a
+    model's own where it scales them for long contexts, and its amplitude (a factor on both)."""
+    torch = _t()
+    positions, rotary_dim = int(positions), int(rotary_dim)
+    if positions < 0 or rotary_dim <= 0 or rotary_dim % 2:
+        raise ValueError("positions must be >= 0 and rotary_dim even and positive")
+    if inv_freq is None:
+        inv_freq = float(base) ** (-np.arange(0, rotary_dim, 2, dtype=np.float64) / rotary_dim)
+    inv_freq = np.asarray(inv_freq, np.float64)
+    if inv_freq.shape != (rotary_dim // 2,):
+        raise ValueError("inv_freq must hold rotary_dim / 2 frequencies")
+    angle = np.arange(positions, dtype=np.float64)[:, None] * inv_freq
+    table = np.stack([np.cos(angle), np.sin(angle)], axis=-1) * float(amplitude)
+    return torch.from_numpy(table.astype(np.float32)).to(device)
+
+
+def _require_rows(t, name, T, heads, D, device):
+    """Token rows [T][heads][D] whose heads lie side by side; returns the elements between tokens."""
+    torch = _t()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16 (got {t.dtype})")
+    if tuple(t.shape) != (T, heads, D):
+        raise ValueError(f"{name} must be [T][heads][D] = {(T, heads, D)}, got {tuple(t.shape)}")
+    if T == 0:
+        return heads * D
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != D):
+        raise ValueError(f"{name}: the heads of a token must lie side by side")
+    if T == 1:
+        return heads * D
+    if st[0] < heads * D or st[0] % 8:
+        raise ValueError(f"{name}: the stride between tokens must be a multiple of 8 and at least heads * D")
+    return st[0]
+
+
+class _on:
+    """The batch's device as the current one (a launch goes to the current device), where it is another."""
+
+    def __init__(self, device, stream=None):
+        torch = _t()
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the batch on {device}")
+        self._guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _empty_on(stream, *size, **kw):
+    """A tensor that belongs to `stream` (the current one for None), so that its memory is not handed
+    on before that stream's work is done."""
+    torch = _t()
+    if stream is None:
+        return torch.empty(*size, **kw)
+    with torch.cuda.stream(stream):
+        return torch.empty(*size, **kw)
+
+
+def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, interleaved, stream, scales):
+    torch = _t()
+    lib = load_library()
+    pool_dtype = torch.uint8 if scales else torch.bfloat16
+    for name, t in (("k_pool", k_pool), ("v_pool", v_pool)):
+        _require(t, pool_dtype, name, batch.device)
+    _require(table, torch.float32, "table", batch.device)
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table must be [positions][rotary_dim / 2][2]")
+    T, Hkv, D = batch.total_new, k_pool.shape[1], k_pool.shape[3]
+    with _on(batch.device, stream):
+        rows = NewRows(k=k_new.data_ptr(), v=v_new.data_ptr(),
+                       k_stride=_require_rows(k_new, "k_new", T, Hkv, D, batch.device),
+                       v_stride=_require_rows(v_new, "v_new", T, Hkv, D, batch.device))
+        Hq = Hkv
+        if q is not None:
+            Hq = q.shape[1]
+            rows.q_stride = _require_rows(q, "q", T, Hq, D, batch.device)
+            rows.q = q.data_ptr()
+            if q_out is None:
+                q_out = _empty_on(stream, (T, Hq, D), dtype=torch.bfloat16, device=batch.device)
+            _require(q_out, torch.bfloat16, "q_out", batch.device)
+            if tuple(q_out.shape) != (T, Hq, D):
+                raise ValueError("q_out must have q's shape")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        geo = _geo_from_pools(k_pool, v_pool, Hq, batch)
+        rot = Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+                     PAIRS_INTERLEAVED if interleaved else PAIRS_HALVES)
+        st = getattr(lib, fn)(ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(rot), ctypes.byref(rows),
+                              q_out.data_ptr() if q_out is not None else None, *scales, k_pool.data_ptr(),
+                              v_pool.data_ptr(), _stream_handle(stream))
+    _check(fn, st, lib)
+    return q_out
+
+
+def kv_append_rotary(q, k_new, v_new, k_pool, v_pool, batch: PagedBatch, table, q_out=None, interleaved=False,
+                     stream=None):
+    """Append the new tokens' K/V ([T][Hkv][D] bf16) into the pools in place with the keys rotated to
+    their positions P_r + i, and rotate the queries ([T][Hq][D] bf16) into q_out, which is returned (made
+    where None; it may be q itself). q None: keys and values only. The tokens of q, k_new and v_new may
+    be strided: views of one projection's output [T][Hq + 2 Hkv][D]. table: rotary_table(...), float32
+    [positions][rotary_dim / 2][2], rotary_dim a multiple of 16 up to D; pairs (j, j + rotary_dim / 2),
+    or (2 j, 2 j + 1) with interleaved=True."""
+    return _append_rotary("gc_kv_append_rotary", q, k_new, v_new, k_pool, v_pool, batch, table, q_out, interleaved,
+                          stream, ())
+
+
+def kv_append_rotary_fp8(q, k_new, v_new, k_pool8, v_pool8, batch: PagedBatch, table, k_scale, v_scale, q_out=None,
+                         interleaved=False, stream=None):
+    """kv_append_rotary into 8-bit pools: the rotated keys are quantised from fp32, the queries stay bf16."""
+    return _append_rotary("gc_kv_append_rotary_fp8", q, k_new, v_new, k_pool8, v_pool8, batch, table, q_out,
+                          interleaved, stream, (float(k_scale), float(v_scale)))

@@ -570,6 +570,70 @@ gc_status append(const gc_geometry* geo, const gc_batch* batch, const void* k_ne
     return gc::launch_append(a, geo->head_dim, pk.fp8, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Bytes that T rows of `width` elements, `stride` elements apart, span from their first one.
+int64_t span_bytes(int64_t T, int64_t stride, int64_t width) { return ((T - 1) * stride + width) * 2; }
+
+bool overlap(const void* p, int64_t np, const void* q, int64_t nq) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return a < b + (uintptr_t)nq && b < a + (uintptr_t)np;
+}
+
+gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rot, const gc_new_rows* rows,
+                        void* q_out, void* k_pool, void* v_pool, const PoolKind& pk, hipStream_t stream) {
+    Shape sh;
+    gc_status st = check_common(geo, batch, &sh);
+    if (st != GC_OK) return st;
+    if (rot == nullptr || rows == nullptr) return GC_ERR_NULL_ARG;
+    if (rot->rotary_dim < 16 || rot->rotary_dim > geo->head_dim || rot->rotary_dim % 16 != 0 || rot->num_positions < 0 ||
+        (rot->pairs != GC_PAIRS_HALVES && rot->pairs != GC_PAIRS_INTERLEAVED))
+        return GC_ERR_BAD_SHAPE;
+    for (int i = 0; i < 5; ++i)
+        if (rot->reserved[i] != 0) return GC_ERR_BAD_SHAPE;
+    if (sh.total_tokens == 0) return GC_OK;
+    if (rot->table_dev == nullptr || rows->k == nullptr || rows->v == nullptr || k_pool == nullptr || v_pool == nullptr)
+        return GC_ERR_NULL_ARG;
+    if ((rows->q == nullptr) != (q_out == nullptr)) return GC_ERR_NULL_ARG;
+    const bool with_q = rows->q != nullptr;
+    const int64_t T = sh.total_tokens, D = geo->head_dim;
+    const int64_t q_row = geo->num_q_heads * D, kv_row = geo->num_kv_heads * D;
+    // (the upper bound keeps byte offsets of 2^31 rows within 64 bits)
+    auto bad_stride = [](int64_t stride, int64_t row) { return stride < row || stride % 8 != 0 || stride > (1LL << 28); };
+    if (bad_stride(rows->k_stride, kv_row) || bad_stride(rows->v_stride, kv_row) ||
+        (with_q && bad_stride(rows->q_stride, q_row)))
+        return GC_ERR_BAD_SHAPE;
+    if (!aligned16(rows->q) || !aligned16(rows->k) || !aligned16(rows->v) || !aligned16(q_out) || !aligned16(rot->table_dev))
+        return GC_ERR_BAD_SHAPE;
+    for (int r = 0; r < batch->batch; ++r)
+        if (batch->new_lens_host[r] > 0 &&
+            (int64_t)batch->prefix_lens_host[r] + batch->new_lens_host[r] > rot->num_positions)
+            return GC_ERR_BAD_SHAPE;
+    if (with_q) {
+        const int64_t out = T * q_row * 2;
+        const bool in_place = q_out == rows->q && rows->q_stride == q_row;
+        if ((!in_place && overlap(q_out, out, rows->q, span_bytes(T, rows->q_stride, q_row))) ||
+            overlap(q_out, out, rows->k, span_bytes(T, rows->k_stride, kv_row)) ||
+            overlap(q_out, out, rows->v, span_bytes(T, rows->v_stride, kv_row)))
+            return GC_ERR_BAD_SHAPE;
+    }
+    gc::RotaryArgs ra{};
+    ra.a = append_args(geo, batch, sh, rows->k, rows->v, k_pool, v_pool, pk);
+    if (gc::rotary_workgroups(ra.a.total_pages, geo->num_q_heads, geo->num_kv_heads, geo->head_dim, with_q) >= (int64_t)INT32_MAX)
+        return GC_ERR_UNSUPPORTED;
+    ra.q = static_cast<const uint16_t*>(rows->q);
+    ra.q_out = static_cast<uint16_t*>(q_out);
+    ra.table = rot->table_dev;
+    ra.q_stride = rows->q_stride;
+    ra.k_stride = rows->k_stride;
+    ra.v_stride = rows->v_stride;
+    ra.num_q_heads = geo->num_q_heads;
+    ra.num_positions = rot->num_positions;
+    ra.rotary_dim = rot->rotary_dim;
+    ra.interleaved = rot->pairs == GC_PAIRS_INTERLEAVED;
+    return gc::launch_append_rotary(ra, geo->head_dim, pk.fp8, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+}
+
 // Append and plan in one launch (the plan reads only the lengths, so the two are
 // independent).
 gc_status prepare(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
@@ -699,6 +763,22 @@ gc_status gc_kv_append_fp8(const gc_geometry* geo, const gc_batch* batch, const 
     const gc_status st = check_pool_scales(k_scale, v_scale);
     if (st != GC_OK) return st;
     return append(geo, batch, k_new, v_new, k_pool, v_pool, PoolKind{true, k_scale, v_scale}, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                              const gc_new_rows* rows, void* q_out, void* k_pool, void* v_pool,
+                              hipStream_t stream) {
+    return append_rotary(geo, batch, rotary, rows, q_out, k_pool, v_pool, PoolKind{}, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                                  const gc_new_rows* rows, void* q_out, float k_scale, float v_scale,
+                                  void* k_pool, void* v_pool, hipStream_t stream) {
+    const gc_status st = check_pool_scales(k_scale, v_scale);
+    if (st != GC_OK) return st;
+    return append_rotary(geo, batch, rotary, rows, q_out, k_pool, v_pool, PoolKind{true, k_scale, v_scale}, stream);
 }
 
 __attribute__((visibility("default")))

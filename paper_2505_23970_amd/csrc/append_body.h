@@ -105,21 +105,17 @@ constexpr int kSearchWorkgroups = 512;  // (see above)
 // KV heads one append workgroup serves (the grid's second dimension covers the rest).
 constexpr int append_heads(int head_dim) { return kAppendThreads / (kPage * head_dim / 8); }
 
-// One append workgroup: page unit u (over the batch, request-major), group hg of KV heads.
-template <int D, bool FP8>
-__device__ __forceinline__ void append_body(const AppendArgs& a, AppendLds<D>& sm, int u, int hg) {
-    constexpr int CPR = D / 8;  // 16-byte chunks per row
-    constexpr int kStride = AppendLds<D>::kStride;
-    constexpr int kPer = kPage * CPR;  // threads per head
-    static_assert(kAppendThreads % kPer == 0 && kPer == 2 * D, "one chunk of K, V and the page per thread");
-    const int tid = threadIdx.x % kPer;
-    const int sub = threadIdx.x / kPer;
-    const int h = hg * AppendLds<D>::kHeads + sub;
-    const bool head_ok = h < a.num_kv_heads;
-
-    // 1. which request and which of its pages
+// The request that page unit u of the batch belongs to, and which of its pages (k) it is.
+struct PageUnit {
     int r, P, cu, n, k;
-    if (a.batch <= 64 && a.total_pages * ceil_div(a.num_kv_heads, AppendLds<D>::kHeads) <= kSearchWorkgroups) {
+};
+
+// Finds page unit u. wgs: workgroups that search one after another in this launch (the choice of the
+// search, above). false: no such page, in lengths that the host did not check.
+template <int D>
+__device__ __forceinline__ bool locate_page(const AppendArgs& a, AppendLds<D>& sm, int u, int wgs, PageUnit& at) {
+    int r, P, cu, n, k;
+    if (a.batch <= 64 && wgs <= kSearchWorkgroups) {
         const int lane = threadIdx.x & 63;
         int c0 = 0, c1 = 0, pre = 0;
         if (lane < a.batch) {
@@ -135,11 +131,11 @@ __device__ __forceinline__ void append_body(const AppendArgs& a, AppendLds<D>& s
             if (lane >= d) x += y;
         }
         const unsigned long long past = __ballot(x > u);  // the first of them holds page u
-        if (past == 0) return;
+        if (past == 0) return false;
         r = (int)__builtin_ctzll(past);
         const int count = __builtin_amdgcn_readlane(pg, r);
         k = u - (__builtin_amdgcn_readlane(x, r) - count);
-        if (r >= a.batch || k < 0 || k >= count) return;  // lengths no valid batch has
+        if (r >= a.batch || k < 0 || k >= count) return false;  // lengths no valid batch has
         P = __builtin_amdgcn_readlane(pre, r);
         cu = __builtin_amdgcn_readlane(c0, r);
         n = __builtin_amdgcn_readlane(c1, r) - cu;
@@ -164,12 +160,67 @@ __device__ __forceinline__ void append_body(const AppendArgs& a, AppendLds<D>& s
             if (sm.found_r >= 0 || carry > u) break;
         }
         r = sm.found_r;
-        if (r < 0) return;
+        if (r < 0) return false;
         k = sm.found_k;
         P = a.prefix_lens[r];
         cu = a.cu_new_lens[r];
         n = a.cu_new_lens[r + 1] - cu;
     }
+    at = PageUnit{r, P, cu, n, k};
+    return true;
+}
+
+// The new slots [s0, s1) of a value page ([D][16 slots]) from its rows in LDS: thread (d, half) writes
+// slots 8 half .. 8 half + 7 of value row d. page: its (block, head) index; tid: thread of the page's 2 D.
+template <int D, bool FP8>
+__device__ __forceinline__ void store_values(const AppendArgs& a, const uint16_t* sv, int64_t page, int tid, int s0, int s1) {
+    constexpr int kStride = AppendLds<D>::kStride;
+    const int d = tid >> 1, half = tid & 1;
+    const int x0 = 8 * half;
+    const int64_t dst = (page * D + d) * kPage + x0;
+    uint16_t e[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) e[x] = sv[(x0 + x) * kStride + d];
+    if (x0 >= s0 && x0 + 8 <= s1) {
+        if constexpr (FP8) {
+            const uint32_t w0 = (uint32_t)e[0] | ((uint32_t)e[1] << 16), w1 = (uint32_t)e[2] | ((uint32_t)e[3] << 16);
+            const uint32_t w2 = (uint32_t)e[4] | ((uint32_t)e[5] << 16), w3 = (uint32_t)e[6] | ((uint32_t)e[7] << 16);
+            *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.v_pool) + dst) =
+                u32x2{quantise4(w0, w1, a.v_inv), quantise4(w2, w3, a.v_inv)};
+        } else {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)e[2 * i] | ((uint32_t)e[2 * i + 1] << 16);
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.v_pool) + dst) = w;
+        }
+    } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            if (x0 + x < s0 || x0 + x >= s1) continue;
+            if constexpr (FP8)
+                static_cast<uint8_t*>(a.v_pool)[dst + x] = quantise1(e[x], a.v_inv);
+            else
+                static_cast<uint16_t*>(a.v_pool)[dst + x] = e[x];
+        }
+    }
+}
+
+// One append workgroup: page unit u (over the batch, request-major), group hg of KV heads.
+template <int D, bool FP8>
+__device__ __forceinline__ void append_body(const AppendArgs& a, AppendLds<D>& sm, int u, int hg) {
+    constexpr int CPR = D / 8;  // 16-byte chunks per row
+    constexpr int kStride = AppendLds<D>::kStride;
+    constexpr int kPer = kPage * CPR;  // threads per head
+    static_assert(kAppendThreads % kPer == 0 && kPer == 2 * D, "one chunk of K, V and the page per thread");
+    const int tid = threadIdx.x % kPer;
+    const int sub = threadIdx.x / kPer;
+    const int h = hg * AppendLds<D>::kHeads + sub;
+    const bool head_ok = h < a.num_kv_heads;
+
+    // 1. which request and which of its pages
+    PageUnit at;
+    if (!locate_page<D>(a, sm, u, a.total_pages * ceil_div(a.num_kv_heads, AppendLds<D>::kHeads), at)) return;
+    const int r = at.r, P = at.P, cu = at.cu, n = at.n, k = at.k;
     const int lp = P / kPage + k;                         // logical page
     const int s0 = max(P - lp * kPage, 0);                // first new slot of the page
     const int s1 = min(P + n - lp * kPage, kPage);        // one past the last
@@ -202,37 +253,8 @@ __device__ __forceinline__ void append_body(const AppendArgs& a, AppendLds<D>& s
     *reinterpret_cast<u32x4*>(&sv[s * kStride + c * 8]) = v;
     __syncthreads();
 
-    // 3. values: thread (d, half) writes slots 8 half .. 8 half + 7 of value row d
-    if (head_ok) {
-        const int d = tid >> 1, half = tid & 1;
-        const int x0 = 8 * half;
-        const int64_t dst = (page * D + d) * kPage + x0;
-        uint16_t e[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) e[x] = sv[(x0 + x) * kStride + d];
-        if (x0 >= s0 && x0 + 8 <= s1) {
-            if constexpr (FP8) {
-                const uint32_t w0 = (uint32_t)e[0] | ((uint32_t)e[1] << 16), w1 = (uint32_t)e[2] | ((uint32_t)e[3] << 16);
-                const uint32_t w2 = (uint32_t)e[4] | ((uint32_t)e[5] << 16), w3 = (uint32_t)e[6] | ((uint32_t)e[7] << 16);
-                *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.v_pool) + dst) =
-                    u32x2{quantise4(w0, w1, a.v_inv), quantise4(w2, w3, a.v_inv)};
-            } else {
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = (uint32_t)e[2 * i] | ((uint32_t)e[2 * i + 1] << 16);
-                *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.v_pool) + dst) = w;
-            }
-        } else {
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                if (x0 + x < s0 || x0 + x >= s1) continue;
-                if constexpr (FP8)
-                    static_cast<uint8_t*>(a.v_pool)[dst + x] = quantise1(e[x], a.v_inv);
-                else
-                    static_cast<uint16_t*>(a.v_pool)[dst + x] = e[x];
-            }
-        }
-    }
+    // 3. values
+    if (head_ok) store_values<D, FP8>(a, sv, page, tid, s0, s1);
 }
 
 }  // namespace

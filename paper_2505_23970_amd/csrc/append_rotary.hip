@@ -1,0 +1,257 @@
+// KV append with the rotary position applied on the way (GreenCache §2.2, Fig. 1a step 1, for a program
+// whose projections hand over keys and queries without their position): the new tokens' keys are rotated
+// and saved with their values, the queries are rotated into q_out, in one launch.
+//
+// Mathematics. Token i of request r stands at position p = P_r + i. Its head vector's first R elements
+// form R / 2 pairs, (j, j + R/2) or (2j, 2j + 1), and pair j is turned by the angle whose cosine and sine
+// the caller's table holds:
+//     y_a = x_a cos - x_b sin,   y_b = x_b cos + x_a sin,
+// in fp32 (one product and one fused multiply-add), rounded once: to bf16, or for keys of 8-bit pools
+// straight to the E4M3 code nearest to y / scale (rounding to bf16 in between would add half as much
+// again as a bf16 ulp to a code's own error for nothing). Elements from R on pass through bit for bit.
+// The table is fp32 [position][pair][cos, sin]: angles of far positions need 64 bits, which the kernel
+// would have to spend per token and head; the table costs 4 R bytes a token, read once per workgroup.
+//
+// Work. A workgroup owns one destination page (up to 16 tokens of one request) of either
+//   - one KV head (two at D = 64): keys in 16-byte chunks, one per thread, whose partner chunk in the other
+//     half comes from the lane that holds it; values as in the plain append (append_body.h);
+//   - or kRotQHeads query heads: a thread owns a pair of 16-byte chunks (elements j .. j + 7 and their
+//     partners), holds the eight (cos, sin) of its token in registers and goes through the heads, so it may
+//     write q_out over q. Pages with few new tokens (decode) put their threads on heads instead.
+// What bounds it: memory for prompts; for decode the chain lengths -> block id, rows and table -> stores.
+#include "append_body.h"
+
+namespace gc {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kRotQHeads = 16;  // query heads of a workgroup
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __bf16 a = (__bf16)lo, b = (__bf16)hi;
+    return (uint32_t)__builtin_bit_cast(uint16_t, a) | ((uint32_t)__builtin_bit_cast(uint16_t, b) << 16);
+}
+
+__device__ __forceinline__ uint32_t quantise4f(float x0, float x1, float x2, float x3, float inv) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x0 * inv), clamp448(x1 * inv), 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(x2 * inv), clamp448(x3 * inv), r, true);
+    return (uint32_t)r;
+}
+
+// Eight bf16 values (a 16-byte chunk) in fp32.
+__device__ __forceinline__ void widen8(const u32x4 w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&y)[8]) {
+    return u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+}
+
+// (cos, sin) of N consecutive pairs.
+template <int N>
+__device__ __forceinline__ void load_angles(const float* at, float (&cs)[N], float (&sn)[N]) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const f32x4 w = *reinterpret_cast<const f32x4*>(at + 4 * i);
+        cs[2 * i] = w[0];
+        sn[2 * i] = w[1];
+        cs[2 * i + 1] = w[2];
+        sn[2 * i + 1] = w[3];
+    }
+}
+
+// Pairs side by side: elements 2j and 2j + 1 of a chunk.
+__device__ __forceinline__ void turn_adjacent(float (&x)[8], const float* cs, const float* sn) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float a = x[2 * j], b = x[2 * j + 1];
+        x[2 * j] = fmaf(a, cs[j], -(b * sn[j]));
+        x[2 * j + 1] = fmaf(b, cs[j], a * sn[j]);
+    }
+}
+
+// Keys and values of one page and KV head (group hg of heads).
+template <int D, bool FP8>
+__device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm, const PageUnit& at, int lp, int s0,
+                                          int s1, int hg) {
+    const AppendArgs& a = ra.a;
+    constexpr int CPR = D / 8;
+    constexpr int kStride = AppendLds<D>::kStride;
+    constexpr int kPer = kPage * CPR;
+    const int tid = threadIdx.x % kPer;
+    const int sub = threadIdx.x / kPer;
+    const int h = hg * AppendLds<D>::kHeads + sub;
+    const bool head_ok = h < a.num_kv_heads;
+    const int blk = a.block_tables[(int64_t)at.r * a.max_blocks + lp];
+    const int s = tid / CPR, c = tid % CPR;
+    const int64_t row = (int64_t)at.cu + (int64_t)lp * kPage - at.P + s;
+    const int pos = lp * kPage + s;
+    const bool ok = head_ok && s >= s0 && s < s1 && row >= 0 && row < a.total_tokens && pos < ra.num_positions;
+    const int half = ra.rotary_dim / 16;  // chunks of half the rotated elements
+    const bool turned = c < 2 * half;
+    u32x4 key = u32x4{0u, 0u, 0u, 0u}, v = key;
+    float cs[8] = {}, sn[8] = {};
+    if (ok) {  // (before the block id is looked at, so that the loads run beside its own)
+        key = *reinterpret_cast<const u32x4*>(a.k_new + row * ra.k_stride + h * D + c * 8);
+        v = *reinterpret_cast<const u32x4*>(a.v_new + row * ra.v_stride + h * D + c * 8);
+        if (turned) {
+            const float* table = ra.table + (int64_t)pos * ra.rotary_dim;
+            if (ra.interleaved) {
+                float c4[4], s4[4];
+                load_angles<4>(table + 8 * c, c4, s4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    cs[j] = c4[j];
+                    sn[j] = s4[j];
+                }
+            } else {
+                load_angles<8>(table + 16 * (c < half ? c : c - half), cs, sn);
+            }
+        }
+    }
+    float x[8];
+    widen8(key, x);
+    if (ra.interleaved) {
+        if (turned) turn_adjacent(x, cs, sn);
+    } else {
+        // the partner chunk, from the lane that holds it (a row's chunks lie in one wavefront)
+        const int lane = threadIdx.x & 63;
+        const int from = turned ? lane + (c < half ? half : -half) : lane;
+        u32x4 other;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = (uint32_t)__shfl((int)key[i], from);
+        if (turned) {
+            float y[8];
+            widen8(other, y);
+            // the upper half adds the product that the lower half subtracts
+            const bool low = c < half;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = fmaf(x[j], cs[j], low ? -(y[j] * sn[j]) : y[j] * sn[j]);
+        }
+    }
+    if (blk < 0 || blk >= a.num_blocks) return;
+    const int64_t page = (int64_t)blk * a.num_kv_heads + h;
+    if (ok) {
+        const int64_t dst = (page * kPage + s) * D + c * 8;
+        if constexpr (FP8) {
+            *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.k_pool) + dst) =
+                u32x2{quantise4f(x[0], x[1], x[2], x[3], a.k_inv), quantise4f(x[4], x[5], x[6], x[7], a.k_inv)};
+        } else {
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.k_pool) + dst) = turned ? pack8(x) : key;
+        }
+    }
+    uint16_t* const sv = sm.v[sub];
+    *reinterpret_cast<u32x4*>(&sv[s * kStride + c * 8]) = v;
+    __syncthreads();
+    if (head_ok) store_values<D, FP8>(a, sv, page, tid, s0, s1);
+}
+
+// kRotQHeads query heads (group qg) of the tokens of one page.
+template <int D>
+__device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int qg) {
+    constexpr int U = D / 16;  // pairs of chunks per head
+    constexpr int kBatch = 4;  // heads whose loads a thread keeps in flight
+    const int slots = s1 - s0;
+    const int span = slots <= 1 ? 1 : slots <= 2 ? 2 : slots <= 4 ? 4 : slots <= 8 ? 8 : 16;  // threads over slots
+    const int u = threadIdx.x % U;
+    const int rest = threadIdx.x / U;
+    const int s = s0 + rest % span;
+    const int step = kAppendThreads / (U * span);
+    const int64_t row = (int64_t)at.cu + (int64_t)lp * kPage - at.P + s;
+    const int pos = lp * kPage + s;
+    if (s >= s1 || row < 0 || row >= ra.a.total_tokens || pos >= ra.num_positions) return;
+    const int half = ra.rotary_dim / 16;
+    const bool turned = u < half;
+    // this thread's two chunks, 8 elements each
+    const int c0 = turned && !ra.interleaved ? u : 2 * u;
+    const int c1 = turned && !ra.interleaved ? u + half : 2 * u + 1;
+    float cs[8] = {}, sn[8] = {};
+    if (turned) load_angles<8>(ra.table + (int64_t)pos * ra.rotary_dim + 16 * u, cs, sn);
+    const int h_end = min((qg + 1) * kRotQHeads, ra.num_q_heads);
+    const uint16_t* src = ra.q + row * ra.q_stride;
+    uint16_t* dst = ra.q_out + row * ra.num_q_heads * D;
+    for (int h0 = qg * kRotQHeads + rest / span; h0 < h_end; h0 += kBatch * step) {
+        u32x4 w0[kBatch], w1[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int h = h0 + b * step;
+            if (h < h_end) {
+                w0[b] = *reinterpret_cast<const u32x4*>(src + h * D + 8 * c0);
+                w1[b] = *reinterpret_cast<const u32x4*>(src + h * D + 8 * c1);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int h = h0 + b * step;
+            if (h >= h_end) break;
+            if (turned) {
+                float x[8], y[8];
+                widen8(w0[b], x);
+                widen8(w1[b], y);
+                if (ra.interleaved) {
+                    turn_adjacent(x, cs, sn);
+                    turn_adjacent(y, cs + 4, sn + 4);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float lo = x[j], hi = y[j];
+                        x[j] = fmaf(lo, cs[j], -(hi * sn[j]));
+                        y[j] = fmaf(hi, cs[j], lo * sn[j]);
+                    }
+                }
+                w0[b] = pack8(x);
+                w1[b] = pack8(y);
+            }
+            *reinterpret_cast<u32x4*>(dst + h * D + 8 * c0) = w0[b];
+            *reinterpret_cast<u32x4*>(dst + h * D + 8 * c1) = w1[b];
+        }
+    }
+}
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(const RotaryArgs ra) {
+    __shared__ AppendLds<D> lds;
+    const AppendArgs& a = ra.a;
+    const int u = (int)(blockIdx.x % (unsigned)a.total_pages);
+    const int job = (int)(blockIdx.x / (unsigned)a.total_pages);
+    PageUnit at;
+    if (!locate_page<D>(a, lds, u, (int)gridDim.x, at)) return;
+    const int lp = at.P / kPage + at.k;
+    const int s0 = max(at.P - lp * kPage, 0);
+    const int s1 = min(at.P + at.n - lp * kPage, kPage);
+    if (lp >= a.max_blocks) return;
+    const int kv_jobs = ceil_div(a.num_kv_heads, append_heads(D));
+    if (job < kv_jobs)
+        rotary_kv<D, FP8>(ra, lds, at, lp, s0, s1, job);
+    else
+        rotary_q<D>(ra, at, lp, s0, s1, job - kv_jobs);
+}
+
+}  // namespace
+
+int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int head_dim, bool with_q) {
+    return pages * (ceil_div(num_kv_heads, append_heads(head_dim)) + (with_q ? ceil_div(num_q_heads, kRotQHeads) : 0));
+}
+
+hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, bool fp8, hipStream_t s) {
+    if (ra.a.total_pages <= 0) return hipSuccess;
+    const dim3 grid((unsigned)rotary_workgroups(ra.a.total_pages, ra.num_q_heads, ra.a.num_kv_heads, head_dim, ra.q != nullptr));
+    if (fp8) {
+        if (head_dim == 128)
+            append_rotary_kernel<128, true><<<grid, kAppendThreads, 0, s>>>(ra);
+        else
+            append_rotary_kernel<64, true><<<grid, kAppendThreads, 0, s>>>(ra);
+    } else {
+        if (head_dim == 128)
+            append_rotary_kernel<128, false><<<grid, kAppendThreads, 0, s>>>(ra);
+        else
+            append_rotary_kernel<64, false><<<grid, kAppendThreads, 0, s>>>(ra);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace gc

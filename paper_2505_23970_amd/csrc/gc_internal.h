@@ -126,6 +126,16 @@ struct AppendArgs {
     float k_inv, v_inv;  // 8-bit pools: fl32(1 / scale) of each pool
 };
 
+// Append with rotation: keys and queries of token rows `stride` elements apart.
+struct RotaryArgs {
+    AppendArgs a;
+    const uint16_t* q;      // may be null: keys and values only
+    uint16_t* q_out;        // [T][Hq][D]; may be q
+    const float* table;     // [num_positions][rotary_dim / 2][cos, sin]
+    int64_t q_stride, k_stride, v_stride;
+    int32_t num_q_heads, num_positions, rotary_dim, interleaved;
+};
+
 struct PlanArgs {
     const int32_t* prefix_lens;
     const int32_t* cu_new_lens;
@@ -181,6 +191,9 @@ struct CombineArgs {
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool fp8, hipStream_t s);
 hipError_t launch_plan(const PlanArgs& a, hipStream_t s);
+hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, bool fp8, hipStream_t s);
+// workgroups of that launch
+int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int head_dim, bool with_q);
 // append (AppendArgs) and plan (PlanArgs) in one launch
 hipError_t launch_prepare(const AppendArgs& aa, const PlanArgs& pa, int head_dim, bool fp8, hipStream_t s);
 // resident > 0 (wide tiles only): that many resident workgroups take
