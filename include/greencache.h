@@ -309,6 +309,76 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
                                         size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Shared prefixes. Requests that reuse the same context (a system prompt, a document
+ * that many ask about) hold the same pool pages at the head of their block-table rows.
+ * The calls below read those pages once for all of a group's queries instead of once
+ * per request; their results are those of the plain attention calls up to the order
+ * of the sums.
+ *   Groups are consecutive requests; every request is in one (alone, with shared
+ *   length 0, where it shares nothing). The first shared_lens[g] tokens of every request of
+ *   group g, a multiple of page_size and at most the least P_r of the group, are the
+ *   same tokens in the same blocks: entries 0 .. shared_lens[g] / page_size - 1 of the
+ *   group's block-table rows agree. Those of the group's first request are read
+ *   (that request may have no new tokens; its row must hold the entries).
+ */
+typedef enum gc_share_policy {
+    GC_SHARE_AUTO = 0,  /* take a group's shared keys once where that saves work (at least two
+                           requests with new tokens, 64 shared keys and a tenth of the query
+                           tiles); a batch without such a group runs as the plain attention */
+    GC_SHARE_ALWAYS = 1 /* take them once whatever it costs (tests, measurements) */
+} gc_share_policy;
+
+typedef struct gc_shared {
+    int32_t groups;                  /* G: 1 .. batch (0 for an empty batch) */
+    const int32_t* group_first_host; /* [G+1] group g is requests group_first[g] .. group_first[g+1] - 1:
+                                        0, increasing, batch */
+    const int32_t* shared_lens_host; /* [G] */
+    const int32_t* group_first_dev;  /* [G+1] device copies */
+    const int32_t* shared_lens_dev;  /* [G] */
+    int32_t policy;                  /* a gc_share_policy value; other values: GC_ERR_BAD_SHAPE */
+    int32_t reserved[6];             /* must be zero */
+} gc_shared;
+
+/*
+ * As gc_prefix_prefill_workspace_size / _plan / _run / _attention (= plan + run) and their
+ * 8-bit forms, over groups. Plans and workspaces are of their own kind (a plan made by
+ * gc_shared_prefix_plan is run by gc_shared_prefix_run with the same batch, groups and
+ * options), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1); gc_prefix_prefill_plan_status
+ * serves them too, and covers the groups' device arrays. Options: tiling GC_TILES_AUTO only
+ * (else GC_ERR_UNSUPPORTED); kv_split_tiles counts 64-key tiles, 32-key tiles for requests whose new
+ * tokens fit one small tile. Everything else, layouts, results in `out` and `lse`, sharing of a
+ * workspace by runs, errors, is as for those calls; further errors: GC_ERR_NULL_ARG for a
+ * missing array, GC_ERR_BAD_SHAPE for groups or shared lengths outside the above and for q, pools or
+ * out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_BLOCK_TABLE for a shared length
+ * past the block-table row.
+ */
+gc_status gc_shared_prefix_workspace_size(const gc_geometry* geo, const gc_batch* batch,
+                                          const gc_shared* shared, const gc_plan_options* opts,
+                                          int32_t fp8, size_t* bytes);
+gc_status gc_shared_prefix_plan(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                const gc_plan_options* opts, int32_t fp8, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+gc_status gc_shared_prefix_run(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                               const gc_plan_options* opts, const void* q, const void* k_pool,
+                               const void* v_pool, float scale, void* out, float* lse, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+gc_status gc_shared_prefix_attention(const gc_geometry* geo, const gc_batch* batch,
+                                     const gc_shared* shared, const gc_plan_options* opts, const void* q,
+                                     const void* k_pool, const void* v_pool, float scale, void* out,
+                                     float* lse, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+gc_status gc_shared_prefix_run_fp8(const gc_geometry* geo, const gc_batch* batch,
+                                   const gc_shared* shared, const gc_plan_options* opts, const void* q,
+                                   const void* k_pool8, const void* v_pool8, float k_scale,
+                                   float v_scale, float scale, void* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+gc_status gc_shared_prefix_attention_fp8(const gc_geometry* geo, const gc_batch* batch,
+                                         const gc_shared* shared, const gc_plan_options* opts,
+                                         const void* q, const void* k_pool8, const void* v_pool8,
+                                         float k_scale, float v_scale, float scale, void* out, float* lse,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Rotary positions. A program whose projections hand over keys and queries without
  * their position gives the rotation to the append: head elements x of the token at
  * position p = P_r + i form rotary_dim / 2 pairs (a, b), and

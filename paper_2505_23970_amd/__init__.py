@@ -28,6 +28,8 @@ EXPORTED = ("gc_kv_append", "gc_kv_append_rotary", "gc_kv_append_rotary_fp8",
             "gc_prefix_prefill_run", "gc_prefix_prefill_attention", "gc_kv_append_fp8",
             "gc_prefix_prefill_run_fp8", "gc_prefix_prefill_attention_fp8", "gc_prefix_prefill_prepare",
             "gc_prefix_prefill_prepare_fp8", "gc_prefix_prefill_run_with_append",
+            "gc_shared_prefix_workspace_size", "gc_shared_prefix_plan", "gc_shared_prefix_run",
+            "gc_shared_prefix_attention", "gc_shared_prefix_run_fp8", "gc_shared_prefix_attention_fp8",
             "gc_prefix_prefill_plan_status", "gc_prefix_prefill_attention_noalloc", "gc_read_bandwidth_probe",
             "gc_mfma_peak_probe", "gc_status_string")
 READ_PROBE_SINK_WORDS = 2048 * 256
@@ -66,6 +68,18 @@ class BatchDesc(ctypes.Structure):
 class PlanOptions(ctypes.Structure):
     _fields_ = [("kv_split_tiles", ctypes.c_int32), ("tiling", ctypes.c_int32),
                 ("reserved", ctypes.c_int32 * 6)]
+
+
+class Shared(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32),
+                ("group_first_host", ctypes.POINTER(ctypes.c_int32)),
+                ("shared_lens_host", ctypes.POINTER(ctypes.c_int32)),
+                ("group_first_dev", ctypes.c_void_p), ("shared_lens_dev", ctypes.c_void_p),
+                ("policy", ctypes.c_int32), ("reserved", ctypes.c_int32 * 6)]
+
+
+# gc_share_policy values
+SHARE_AUTO, SHARE_ALWAYS = 0, 1
 
 
 class Rotary(ctypes.Structure):
@@ -115,6 +129,17 @@ def load_library(path: str | None = None):
     for fn in (lib.gc_prefix_prefill_run_fp8, lib.gc_prefix_prefill_attention_fp8):
         fn.restype = i32
         fn.argtypes = [G, Bp, O, vp, vp, vp, f32, f32, f32, vp, vp, vp, ctypes.c_size_t, vp]
+    Sp = ctypes.POINTER(Shared)
+    lib.gc_shared_prefix_workspace_size.restype = i32
+    lib.gc_shared_prefix_workspace_size.argtypes = [G, Bp, Sp, O, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.gc_shared_prefix_plan.restype = i32
+    lib.gc_shared_prefix_plan.argtypes = [G, Bp, Sp, O, i32, vp, ctypes.c_size_t, vp]
+    for fn in (lib.gc_shared_prefix_run, lib.gc_shared_prefix_attention):
+        fn.restype = i32
+        fn.argtypes = [G, Bp, Sp, O, vp, vp, vp, f32, vp, vp, vp, ctypes.c_size_t, vp]
+    for fn in (lib.gc_shared_prefix_run_fp8, lib.gc_shared_prefix_attention_fp8):
+        fn.restype = i32
+        fn.argtypes = [G, Bp, Sp, O, vp, vp, vp, f32, f32, f32, vp, vp, vp, ctypes.c_size_t, vp]
     Ro, Nr = ctypes.POINTER(Rotary), ctypes.POINTER(NewRows)
     lib.gc_kv_append_rotary.restype = i32
     lib.gc_kv_append_rotary.argtypes = [G, Bp, Ro, Nr, vp, vp, vp, vp]
@@ -679,3 +704,120 @@ def kv_append_rotary_fp8(q, k_new, v_new, k_pool8, v_pool8, batch: PagedBatch, t
     """kv_append_rotary into 8-bit pools: the rotated keys are quantised from fp32, the queries stay bf16."""
     return _append_rotary("gc_kv_append_rotary_fp8", q, k_new, v_new, k_pool8, v_pool8, batch, table, q_out,
                           interleaved, stream, (float(k_scale), float(v_scale)))
+
+
+# ----------------------------------------------------------------- shared prefixes
+
+class SharedPrefixes:
+    """Groups of requests that share the head of their cached prefix, over a PagedBatch.
+
+    group_sizes[g]: requests of group g, consecutive in the batch (their sum is the batch);
+    shared_lens[g]: tokens that all of them share, in the same pool blocks: a multiple of the page
+    size, at most every member's prefix length (0: nothing). policy: SHARE_AUTO or SHARE_ALWAYS."""
+
+    def __init__(self, batch: PagedBatch, group_sizes, shared_lens, policy=SHARE_AUTO):
+        import torch
+        sizes = np.ascontiguousarray(group_sizes, dtype=np.int32)
+        self.shared_lens = np.ascontiguousarray(shared_lens, dtype=np.int32)
+        if sizes.ndim != 1 or self.shared_lens.shape != sizes.shape:
+            raise ValueError("group_sizes and shared_lens must be one list each, of one length")
+        if int(sizes.sum()) != batch.batch or (sizes <= 0).any():
+            raise ValueError("group_sizes must be positive and add up to the batch")
+        self.batch = batch
+        first = np.zeros(sizes.shape[0] + 1, np.int32)
+        np.cumsum(sizes, out=first[1:])
+        self.group_first = first
+        for g, S in enumerate(self.shared_lens):   # the pages must be the same ones
+            rows = batch.block_tables_host[first[g]:first[g + 1], :max(0, int(S)) // 16]
+            if (rows != rows[:1]).any():
+                raise ValueError(f"group {g}: its block-table rows differ within the {int(S)} shared tokens")
+        self.group_first_dev = torch.from_numpy(first.copy()).to(batch.device)
+        self.shared_lens_dev = torch.from_numpy(self.shared_lens.copy()).to(batch.device)
+        as_int = ctypes.POINTER(ctypes.c_int32)
+        self._desc = Shared(int(sizes.shape[0]), first.ctypes.data_as(as_int), self.shared_lens.ctypes.data_as(as_int),
+                            self.group_first_dev.data_ptr(), self.shared_lens_dev.data_ptr(), int(policy))
+
+    def desc(self) -> Shared:
+        return self._desc
+
+
+def shared_workspace_size(num_q_heads, k_pool, v_pool, shared: SharedPrefixes, kv_split_tiles=None) -> int:
+    lib = load_library()
+    batch = shared.batch
+    geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
+    out = ctypes.c_size_t(0)
+    with _on(batch.device):   # (the plan goes by the device's compute units)
+        st = lib.gc_shared_prefix_workspace_size(ctypes.byref(geo), ctypes.byref(batch.desc()),
+                                                 ctypes.byref(shared.desc()), _opts(kv_split_tiles),
+                                                 k_pool.dtype == _t().uint8, ctypes.byref(out))
+    _check("gc_shared_prefix_workspace_size", st, lib)
+    return int(out.value)
+
+
+def alloc_shared_workspace(num_q_heads, k_pool, v_pool, shared: SharedPrefixes, kv_split_tiles=None, stream=None):
+    n = shared_workspace_size(num_q_heads, k_pool, v_pool, shared, kv_split_tiles)
+    return _empty_on(stream, max(n, 256), dtype=_t().uint8, device=shared.batch.device)
+
+
+def plan_shared(num_q_heads, k_pool, v_pool, shared: SharedPrefixes, workspace, kv_split_tiles=None, stream=None):
+    """Build the work list of run_shared (or run_shared_fp8, by the pools' type) in `workspace`: once per
+    batch, for every layer."""
+    torch = _t()
+    lib = load_library()
+    batch = shared.batch
+    _require(workspace, torch.uint8, "workspace", batch.device)
+    geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
+    with _on(batch.device, stream):
+        st = lib.gc_shared_prefix_plan(ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(shared.desc()),
+                                       _opts(kv_split_tiles), k_pool.dtype == torch.uint8, workspace.data_ptr(),
+                                       workspace.numel(), _stream_handle(stream))
+    _check("gc_shared_prefix_plan", st, lib)
+
+
+def _shared_call(fn, q, k_pool, v_pool, shared, scale, scales, workspace, out, lse, kv_split_tiles, stream):
+    torch = _t()
+    lib = load_library()
+    batch = shared.batch
+    pool_dtype = torch.uint8 if scales else torch.bfloat16
+    with _on(batch.device, stream):
+        if workspace is None:
+            _require(k_pool, pool_dtype, "k_pool", batch.device)
+            workspace = alloc_shared_workspace(q.shape[1], k_pool, v_pool, shared, kv_split_tiles, stream)
+        if out is None:
+            out = _empty_on(stream, q.shape, dtype=torch.bfloat16, device=batch.device)
+        geo, out = _attn_args(q, k_pool, v_pool, batch, out, lse, workspace, pool_dtype)
+        st = getattr(lib, fn)(ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(shared.desc()),
+                              _opts(kv_split_tiles), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *scales,
+                              float(scale), out.data_ptr(), lse.data_ptr() if lse is not None else None,
+                              workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+    _check(fn, st, lib)
+    return out
+
+
+def run_shared(q, k_pool, v_pool, shared: SharedPrefixes, scale, workspace, out=None, lse=None, kv_split_tiles=None,
+               stream=None):
+    """Attention of the new tokens (q: [T][Hq][D] bf16) from a plan made by plan_shared, each group's shared
+    keys read once. Returns out ([T][Hq][D] bf16); fills lse ([T][Hq] fp32) when given."""
+    return _shared_call("gc_shared_prefix_run", q, k_pool, v_pool, shared, scale, (), workspace, out, lse,
+                        kv_split_tiles, stream)
+
+
+def run_shared_fp8(q, k_pool8, v_pool8, shared: SharedPrefixes, scale, k_scale, v_scale, workspace, out=None, lse=None,
+                   kv_split_tiles=None, stream=None):
+    """run_shared over 8-bit pools."""
+    return _shared_call("gc_shared_prefix_run_fp8", q, k_pool8, v_pool8, shared, scale,
+                        (float(k_scale), float(v_scale)), workspace, out, lse, kv_split_tiles, stream)
+
+
+def shared_prefix_attention(q, k_pool, v_pool, shared: SharedPrefixes, scale, workspace=None, out=None, lse=None,
+                            kv_split_tiles=None, stream=None):
+    """plan_shared and run_shared in one call. The pools must already hold the new tokens' K/V."""
+    return _shared_call("gc_shared_prefix_attention", q, k_pool, v_pool, shared, scale, (), workspace, out, lse,
+                        kv_split_tiles, stream)
+
+
+def shared_prefix_attention_fp8(q, k_pool8, v_pool8, shared: SharedPrefixes, scale, k_scale, v_scale, workspace=None,
+                                out=None, lse=None, kv_split_tiles=None, stream=None):
+    """shared_prefix_attention over 8-bit pools."""
+    return _shared_call("gc_shared_prefix_attention_fp8", q, k_pool8, v_pool8, shared, scale,
+                        (float(k_scale), float(v_scale)), workspace, out, lse, kv_split_tiles, stream)

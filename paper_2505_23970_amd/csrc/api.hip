@@ -746,6 +746,248 @@ gc_status run_with_append(const gc_geometry* geo, const gc_batch* batch, const g
     return enqueue_run(geo, batch, sh, pl, q, k_pool, v_pool, scale, out, lse, workspace, stream);
 }
 
+// ---------------------------------------------------------------- shared prefixes
+struct SharedPlan {
+    bool any = false;  // some group's shared keys are taken once (else the plain attention runs)
+    gc::SharedSizes z{};
+    int64_t big = 0, small = 0, big_slots = 0, small_slots = 0;  // items and partial slots
+    gc::SharedLayout layout{};
+};
+
+gc_status check_shared(const gc_geometry* geo, const gc_batch* b, const gc_shared* s) {
+    if (s == nullptr) return GC_ERR_NULL_ARG;
+    if (s->groups < 0 || s->groups > b->batch || (s->groups == 0) != (b->batch == 0)) return GC_ERR_BAD_SHAPE;
+    if (s->policy != GC_SHARE_AUTO && s->policy != GC_SHARE_ALWAYS) return GC_ERR_BAD_SHAPE;
+    for (int i = 0; i < 6; ++i)
+        if (s->reserved[i] != 0) return GC_ERR_BAD_SHAPE;
+    if (b->batch == 0) return GC_OK;
+    if (s->group_first_host == nullptr || s->shared_lens_host == nullptr) return GC_ERR_NULL_ARG;
+    if (s->group_first_host[0] != 0 || s->group_first_host[s->groups] != b->batch) return GC_ERR_BAD_SHAPE;
+    for (int g = 0; g < s->groups; ++g) {
+        const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1], S = s->shared_lens_host[g];
+        if (ra < 0 || rb <= ra || rb > b->batch || S < 0 || S % gc::kPage != 0) return GC_ERR_BAD_SHAPE;
+        if (S / gc::kPage > geo->max_blocks_per_seq) return GC_ERR_BLOCK_TABLE;
+        for (int r = ra; r < rb; ++r)
+            if (b->prefix_lens_host[r] < S) return GC_ERR_BAD_SHAPE;
+    }
+    return GC_OK;
+}
+
+// f(PartWork, shared) for every shared and own part of the batch.
+template <typename F>
+void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes& z, F&& f) {
+    for (int g = 0; g < s->groups; ++g) {
+        const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1];
+        int active = 0, tokens = 0, tiles = 0;
+        for (int r = ra; r < rb; ++r) {
+            const int n = b->new_lens_host[r];
+            active += n > 0;
+            tokens += n;
+            tiles += gc::ceil_div(n, z.tq);
+        }
+        const int S = gc::shared_taken(s->shared_lens_host[g], active, tokens, tiles, z);
+        f(gc::shared_part(S, tokens, z), S > 0);
+        for (int r = ra; r < rb; ++r) f(gc::own_part(b->prefix_lens_host[r] - S, b->new_lens_host[r], z), S > 0);
+    }
+}
+
+// Chunks of the key axis. The launch has two 128-row workgroups a compute unit, or as many workgroups
+// of small items, so the parts are cut until they fill those slots: the smallest chunk length (in cost;
+// a small item's tiles are shorter) whose items fit, at least kMinChunk key tiles, below which an item's
+// fixed cost and its partial rows outweigh the shorter chunk.
+constexpr int kMinChunk = 8, kMinChunkSmall = 12;
+
+void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
+    const int64_t slots = 2LL * device_cus();
+    const int per = gc::shared_small_per_workgroup(pk.fp8);
+    z->chunk = z->chunk_small = 0;
+    int longest = 1;  // in units of cost: a 64-key tile 4, a small tile 3
+    for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) {
+        if (w.tiles == 0) return;
+        const int cost = w.small ? 3 * gc::ceil_div(w.keys, gc::kDecN) : 4 * gc::ceil_div(w.keys, gc::kBlockN);
+        if (cost > longest) longest = cost;
+    });
+    auto set = [&](int cost) {
+        z->chunk = cost / 4 > kMinChunk ? cost / 4 : kMinChunk;
+        z->chunk_small = cost / 3 > kMinChunkSmall ? cost / 3 : kMinChunkSmall;
+    };
+    auto fits = [&](int cost) {
+        set(cost);
+        int64_t big = 0, small = 0;
+        for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) { (w.small ? small : big) += (int64_t)w.tiles * w.ns; });
+        return big * geo->num_kv_heads + (small * geo->num_kv_heads + per - 1) / per <= slots;
+    };
+    int lo = 1, hi = longest;
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (fits(mid)) hi = mid;
+        else lo = mid + 1;
+    }
+    set(lo);
+}
+
+gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,
+                           const Shape& sh, const PoolKind& pk, SharedPlan* pl) {
+    gc::SharedSizes& z = pl->z;
+    z.tq = gc::tokens_per_tile(sh.group, gc::kBlockM);
+    z.tq_small = sh.group <= gc::kDecM ? gc::tokens_per_tile(sh.group, gc::kDecM) : 0;
+    z.always = s->policy == GC_SHARE_ALWAYS;
+    pl->any = false;
+    for_each_part(b, s, z, [&](const gc::PartWork&, bool shared) { pl->any |= shared; });
+    if (!pl->any) return GC_OK;
+    if (o != nullptr && o->kv_split_tiles != 0) {
+        z.chunk = z.chunk_small = o->kv_split_tiles > 0 ? o->kv_split_tiles : 0;
+    } else {
+        choose_shared_chunks(geo, b, s, pk, &z);
+    }
+    for_each_part(b, s, z, [&](const gc::PartWork& w, bool shared) {
+        const int64_t items = (int64_t)w.tiles * w.ns;
+        (w.small ? pl->small : pl->big) += items;
+        if (shared || w.ns > 1) (w.small ? pl->small_slots : pl->big_slots) += items;
+    });
+    const int64_t most = (int64_t)INT32_MAX / geo->num_kv_heads - 64;
+    if (pl->big > most || pl->small > most || sh.total_tokens * geo->num_q_heads / 8 >= INT32_MAX) return GC_ERR_BAD_SHAPE;
+    gc::SharedLayout& l = pl->layout;
+    size_t off = 256;  // (the status word leads, as in the plain workspace)
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = gc::align_up(off + bytes, 256);
+        return at;
+    };
+    const size_t heads = (size_t)geo->num_kv_heads, D = (size_t)geo->head_dim;
+    l.reqs_off = take(sizeof(gc::SharedReq) * (size_t)b->batch);
+    l.big_off = take(sizeof(gc::SharedItem) * (size_t)pl->big);
+    l.small_off = take(sizeof(gc::SharedItem) * (size_t)pl->small);
+    l.scratch_off = take(sizeof(int32_t) * gc::shared_scratch_ints(b->batch));
+    l.big_lse_off = take(sizeof(float) * (size_t)pl->big_slots * heads * gc::kBlockM);
+    l.small_lse_off = take(sizeof(float) * (size_t)pl->small_slots * heads * gc::kDecM);
+    l.big_o_off = take(sizeof(float) * (size_t)pl->big_slots * heads * gc::kBlockM * D);
+    l.small_o_off = take(sizeof(float) * (size_t)pl->small_slots * heads * gc::kDecM * D);
+    l.total = off;
+    return GC_OK;
+}
+
+// Every check that needs no tensors, and the plan. Where no group shares, the plain attention's shape and plan.
+gc_status shared_checked(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,
+                         const PoolKind& pk, Shape* sh, SharedPlan* spl, Plan* pl) {
+    gc_status st = check_common(geo, b, sh);
+    if (st != GC_OK) return st;
+    st = check_options(o);
+    if (st != GC_OK) return st;
+    if (o != nullptr && o->tiling != GC_TILES_AUTO) return GC_ERR_UNSUPPORTED;
+    st = check_shared(geo, b, s);
+    if (st != GC_OK || sh->total_tokens == 0) return st;
+    if (s->group_first_dev == nullptr || s->shared_lens_dev == nullptr) return GC_ERR_NULL_ARG;
+    st = make_shared_plan(geo, b, s, o, *sh, pk, spl);
+    if (st != GC_OK || spl->any) return st;
+    return plan_checked(geo, b, o, sh, pl);
+}
+
+gc_status check_shared_workspace(const SharedPlan& spl, const Plan& pl, const void* ws, size_t bytes) {
+    if (!aligned16(ws)) return GC_ERR_WORKSPACE;
+    if (!spl.any) return check_workspace(pl, ws, bytes);
+    return ws == nullptr || bytes < spl.layout.total ? GC_ERR_WORKSPACE : GC_OK;
+}
+
+gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh,
+                              const SharedPlan& spl, void* ws, hipStream_t stream) {
+    gc::SharedPlanArgs a{};
+    a.prefix_lens = b->prefix_lens_dev;
+    a.cu_new_lens = b->cu_new_lens_dev;
+    a.group_first = s->group_first_dev;
+    a.shared_lens = s->shared_lens_dev;
+    a.status = at<int32_t>(ws, gc::kStatusOffset);
+    a.scratch = at<int32_t>(ws, spl.layout.scratch_off);
+    a.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
+    a.big_items = at<gc::SharedItem>(ws, spl.layout.big_off);
+    a.small_items = at<gc::SharedItem>(ws, spl.layout.small_off);
+    a.batch = b->batch;
+    a.groups = s->groups;
+    a.total_tokens = (int32_t)sh.total_tokens;
+    a.max_blocks = geo->max_blocks_per_seq;
+    a.expect_big = (int32_t)spl.big;
+    a.expect_small = (int32_t)spl.small;
+    a.expect_big_slots = (int32_t)spl.big_slots;
+    a.expect_small_slots = (int32_t)spl.small_slots;
+    a.z = spl.z;
+    return gc::launch_shared_plan(a, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+}
+
+gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh, const SharedPlan& spl,
+                             const void* q, const void* k_pool, const void* v_pool, float scale, void* out, float* lse,
+                             void* ws, hipStream_t stream, const PoolKind& pk) {
+    gc::SharedAttnArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k_pool = static_cast<const uint16_t*>(k_pool);
+    a.v_pool = static_cast<const uint16_t*>(v_pool);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse = lse;
+    a.part_o = at<float>(ws, spl.layout.big_o_off);
+    a.part_lse = at<float>(ws, spl.layout.big_lse_off);
+    a.block_tables = b->block_tables_dev;
+    a.items = reinterpret_cast<const gc::WorkItem*>(at<gc::SharedItem>(ws, spl.layout.big_off));
+    a.num_q_heads = geo->num_q_heads;
+    a.num_kv_heads = geo->num_kv_heads;
+    a.group = sh.group;
+    a.tq = spl.z.tq;
+    a.num_blocks = geo->num_blocks;
+    a.max_blocks = geo->max_blocks_per_seq;
+    a.scale_log2 = (float)((double)scale * (double)pk.k_scale * 1.4426950408889634074);
+    a.v_scale = pk.v_scale;
+    a.prefer_span = (uint32_t)device_cus();
+    a.prefer_odd = 0;
+    a.small_items = at<gc::SharedItem>(ws, spl.layout.small_off);
+    a.small_o = at<float>(ws, spl.layout.small_o_off);
+    a.small_lse = at<float>(ws, spl.layout.small_lse_off);
+    a.big = (int32_t)(spl.big * geo->num_kv_heads);
+    a.small = (int32_t)(spl.small * geo->num_kv_heads);
+    if (gc::launch_attention_shared(a, geo->head_dim, pk.fp8, stream) != hipSuccess) return GC_ERR_HIP;
+    gc::SharedMergeArgs m{};
+    m.out = a.out;
+    m.lse = lse;
+    m.big_o = a.part_o;
+    m.big_lse = a.part_lse;
+    m.small_o = a.small_o;
+    m.small_lse = a.small_lse;
+    m.cu_new_lens = b->cu_new_lens_dev;
+    m.status = at<int32_t>(ws, gc::kStatusOffset);
+    m.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
+    m.rows = sh.total_tokens * geo->num_q_heads;
+    m.batch = b->batch;
+    m.num_q_heads = geo->num_q_heads;
+    m.num_kv_heads = geo->num_kv_heads;
+    m.group = sh.group;
+    m.tq = spl.z.tq;
+    m.tq_small = spl.z.tq_small;
+    return gc::launch_shared_merge(m, geo->head_dim, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+}
+
+gc_status run_shared(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared, const gc_plan_options* opts,
+                     const void* q, const void* k_pool, const void* v_pool, float scale, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, hipStream_t stream, bool with_plan, const PoolKind& pk) {
+    Shape sh;
+    SharedPlan spl;
+    Plan pl;
+    gc_status st = shared_checked(geo, batch, shared, opts, pk, &sh, &spl, &pl);
+    if (st != GC_OK || sh.total_tokens == 0) return st;
+    st = check_run_args(q, k_pool, v_pool, scale, out);
+    if (st != GC_OK) return st;
+    if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(out)) return GC_ERR_BAD_SHAPE;
+    if (pk.fp8) {
+        st = check_pool_scales(pk.k_scale, pk.v_scale);
+        if (st != GC_OK) return st;
+    }
+    st = check_shared_workspace(spl, pl, workspace, workspace_bytes);
+    if (st != GC_OK) return st;
+    if (with_plan) {
+        st = spl.any ? enqueue_shared_plan(geo, batch, shared, sh, spl, workspace, stream)
+                     : enqueue_plan(geo, batch, sh, pl, workspace, stream);
+        if (st != GC_OK) return st;
+    }
+    return spl.any ? enqueue_shared_run(geo, batch, sh, spl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk)
+                   : enqueue_run(geo, batch, sh, pl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk);
+}
+
 }  // namespace
 
 extern "C" {
@@ -891,6 +1133,70 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
                                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
     return prepare(geo, batch, opts, k_new, v_new, k_pool8, v_pool8, workspace, workspace_bytes, stream,
                    PoolKind{true, k_scale, v_scale});
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_workspace_size(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                          const gc_plan_options* opts, int32_t fp8, size_t* bytes) {
+    if (bytes == nullptr) return GC_ERR_NULL_ARG;
+    Shape sh;
+    SharedPlan spl;
+    Plan pl;
+    const gc_status st = shared_checked(geo, batch, shared, opts, PoolKind{fp8 != 0}, &sh, &spl, &pl);
+    if (st != GC_OK) return st;
+    *bytes = sh.total_tokens == 0 ? 0 : spl.any ? spl.layout.total : pl.layout.total;
+    return GC_OK;
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_plan(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                const gc_plan_options* opts, int32_t fp8, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream) {
+    Shape sh;
+    SharedPlan spl;
+    Plan pl;
+    gc_status st = shared_checked(geo, batch, shared, opts, PoolKind{fp8 != 0}, &sh, &spl, &pl);
+    if (st != GC_OK || sh.total_tokens == 0) return st;
+    st = check_shared_workspace(spl, pl, workspace, workspace_bytes);
+    if (st != GC_OK) return st;
+    return spl.any ? enqueue_shared_plan(geo, batch, shared, sh, spl, workspace, stream)
+                   : enqueue_plan(geo, batch, sh, pl, workspace, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_run(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                               const gc_plan_options* opts, const void* q, const void* k_pool, const void* v_pool,
+                               float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream) {
+    return run_shared(geo, batch, shared, opts, q, k_pool, v_pool, scale, out, lse, workspace, workspace_bytes, stream,
+                      false, PoolKind{});
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_attention(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                     const gc_plan_options* opts, const void* q, const void* k_pool, const void* v_pool,
+                                     float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream) {
+    return run_shared(geo, batch, shared, opts, q, k_pool, v_pool, scale, out, lse, workspace, workspace_bytes, stream,
+                      true, PoolKind{});
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_run_fp8(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                   const gc_plan_options* opts, const void* q, const void* k_pool, const void* v_pool,
+                                   float k_scale, float v_scale, float scale, void* out, float* lse, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+    return run_shared(geo, batch, shared, opts, q, k_pool, v_pool, scale, out, lse, workspace, workspace_bytes, stream,
+                      false, PoolKind{true, k_scale, v_scale});
+}
+
+__attribute__((visibility("default")))
+gc_status gc_shared_prefix_attention_fp8(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared,
+                                         const gc_plan_options* opts, const void* q, const void* k_pool,
+                                         const void* v_pool, float k_scale, float v_scale, float scale, void* out,
+                                         float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return run_shared(geo, batch, shared, opts, q, k_pool, v_pool, scale, out, lse, workspace, workspace_bytes, stream,
+                      true, PoolKind{true, k_scale, v_scale});
 }
 
 __attribute__((visibility("default")))

@@ -37,6 +37,9 @@
 // the key scale is folded into the softmax scale, the value scale into the
 // final normalisation.
 #pragma once
+#include <type_traits>
+
+#include "attention_small_body.h"
 #include "gc_internal.h"
 
 namespace gc {
@@ -47,8 +50,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-constexpr float kLn2 = 0.69314718055994530942f;
 
 // Position of 16-byte chunk `chunk` inside key row `row` of a tile in LDS. A fragment
 // read takes, per 16 lanes, the rows 16 p + 8 h + 4 b + v (p, h = 0, 1, v = 0 .. 3) of one
@@ -120,9 +121,12 @@ __device__ __forceinline__ void widen_e4m3x16(const u32x4 c, u32x4& lo, u32x4& h
 }
 
 // One work item (a workgroup of WAVES wavefronts): the item of launch index bid (blockIdx.x
-// in the regular launch), i.e. work item bid / Hkv for KV head bid % Hkv.
-template <int D, int WAVES, bool FP8, int WGS = 8 / WAVES>
-__device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned bid) {
+// in the regular launch), i.e. work item bid / Hkv for KV head bid % Hkv. SHARED: an item of a
+// shared-prefix launch (SharedItem): its keys start at page page0 of the table row, and all of
+// them are visible to every row where `full` is set; the launch's small items run here too, in
+// the same LDS.
+template <int D, int WAVES, bool FP8, int WGS = 8 / WAVES, bool SHARED = false, typename Args = AttnArgs>
+__device__ __forceinline__ void attention_body(const Args& a, unsigned bid) {
     constexpr int kBlockRows = WAVES * kRowsPerWave;  // query rows of a work item
     constexpr int KS = D / 32;                      // k-steps of QK^T
     constexpr int DB = D / 16;                      // 16-row blocks of O^T
@@ -143,6 +147,29 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     __shared__ __align__(16) unsigned char k_lds1[kTileBytes];
     __shared__ __align__(16) unsigned char v_lds1[kTileBytes];
 
+    if constexpr (SHARED) {
+        // (i * mix >> 32 of the first i groups of eight are of the first kind)
+        const unsigned grp = bid / kQueues, in = bid % kQueues;
+        const unsigned before = (unsigned)(grp * a.mix >> 32);
+        if ((unsigned)((grp + 1) * a.mix >> 32) == before) {
+            constexpr int kPer = FP8 ? 4 : 2;  // rings that fit the tile buffers
+            constexpr int kTile = kSmallTileBytes<D, FP8>;
+            static_assert(WAVES == 4 && (FP8 ? 2 * kTile : kTile) == kTileBytes, "rings");
+            const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+            const unsigned at = ((grp - before) * kQueues + in) * kPer + w;
+            if (w >= kPer || at >= (unsigned)a.small) return;
+            AttnArgs s = a;
+            s.part_o = a.small_o;
+            s.part_lse = a.small_lse;
+            unsigned char* const r0 = FP8 ? (w == 0 ? k_lds0 : w == 1 ? v_lds0 : w == 2 ? k_lds1 : v_lds1) : (w == 0 ? k_lds0 : k_lds1);
+            unsigned char* const r1 = FP8 ? r0 + kTile : (w == 0 ? v_lds0 : v_lds1);
+            small_body<D, FP8, true>(s, a.small_items[at / (unsigned)a.num_kv_heads], (int)(at % (unsigned)a.num_kv_heads), r0, r1);
+            return;
+        }
+        bid = before * kQueues + in;
+        if (bid >= (unsigned)a.big) return;
+    }
+
     // (opaque to the compiler, so that the lane constants derived from it are computed per
     // work item: hoisted out of the resident launch's item loop they would be held, or
     // spilled, across the tile loop)
@@ -159,12 +186,13 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     // 2052 us, 70B chat 434 -> 422, 8B chat 125.7 -> 121.5, over 8-bit pools 173.6 -> 154.8; at
     // d = 64, where three 128-row workgroups share a compute unit, 2 % slower, so not there.
     // (Before the item's loads: between them and their uses the branch cost 1-3 % of short launches.)
-    if (WAVES == kWideWaves ? wave < WAVES / 2 : D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd)
+    if (WAVES == kWideWaves ? wave < WAVES / 2 : D == 128 && ((SHARED ? blockIdx.x : bid) / a.prefer_span & 1) == a.prefer_odd)
         __builtin_amdgcn_s_setprio(2);
     const int g4 = lane >> 4;
     const int j16 = lane & 15;
     const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
-    const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
+    using Item = std::conditional_t<SHARED, SharedItem, WorkItem>;
+    const Item it = reinterpret_cast<const Item*>(a.items)[bid / (unsigned)a.num_kv_heads];
     // all eight fields in one load (else the fields the test below needs are loaded
     // first and the rest after it, a second dependent round trip)
     asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P),
@@ -175,7 +203,9 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     const int P = it.P;
     const int cu = it.cu;
     const int n = it.n;
-    const int L = P + n;
+    const int L = item_keys(it);
+    const int page0 = item_page0(it);  // of the table row
+    const bool full = item_full(it);
     const int ntok = min(a.tq, n - it.q0);
 
     // this lane's query rows, 16 rb + j16 of the wavefront's 32: token t of the tile, query
@@ -189,6 +219,7 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
         const int t = (int)((unsigned)m / (unsigned)a.group);
         row_ok[rb] = t < ntok;
         lim[rb] = P + it.q0 + (row_ok[rb] ? t : 0);
+        if (SHARED && full) lim[rb] = L - 1;
         qrow[rb] = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group);
     }
 
@@ -196,7 +227,7 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     // order, so the first tile's copies then wait for these entries only and go out
     // while Q is still in flight (entry p in lanes with lane % 4 == p; clamped into
     // the row, checked at use)
-    int ids = a.block_tables[(int64_t)r * a.max_blocks + min(it.kt_begin * 4 + (lane & 3), a.max_blocks - 1)];
+    int ids = a.block_tables[(int64_t)r * a.max_blocks + page0 + min(it.kt_begin * 4 + (lane & 3), a.max_blocks - page0 - 1)];
 
     // Q^T operands: lane holds q[row 16 rb + j16][32 ks + 8 g4 .. +7]
     bf16x8 qf[RB][KS];
@@ -228,14 +259,14 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     const int v_d = sub * 32 + (lane >> 1);                            // value row (d) in the page
     const int v_half = (lane & 1) ^ ((v_d >> 3) & 1);                  // logical half held by the lane
     const uint32_t v_src = v_d * 32 + v_half * 16;
-    const int32_t* table = a.block_tables + (int64_t)r * a.max_blocks;
+    const int32_t* table = a.block_tables + (int64_t)r * a.max_blocks + page0;
     const int64_t head_off = (int64_t)kvh * kPageBytes;
     const int64_t block_stride = (int64_t)a.num_kv_heads * kPageBytes;
     // raw table entries of tile kt (indices clamped into the row; checked at use)
     // (a vector load: lane p of every 4 holds entry p; it completes with the tile loads,
     // and no scalar load is left in flight to force full LDS waits in the compute phase)
     auto fetch_ids = [&](int kt, int& ids) {
-        ids = table[(uint32_t)min(kt * 4 + (lane & 3), a.max_blocks - 1)];
+        ids = table[(uint32_t)min(kt * 4 + (lane & 3), a.max_blocks - page0 - 1)];
     };
     // Copies of piece e of tile kt (one page of K and of V for this wave). A page past the
     // table, past the sequence or with a block id outside the pool is copied from block 0
@@ -249,7 +280,7 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
     auto issue_page = [&](int buf, int kt, const int blk, int e) {
         const int pg = page_of(e);
         const int lp = kt * 4 + pg;
-        const bool ok = lp < a.max_blocks && lp * kPage < L && blk >= 0 && blk < a.num_blocks;
+        const bool ok = lp < a.max_blocks - page0 && lp * kPage < L && blk >= 0 && blk < a.num_blocks;
         const int64_t off = (int64_t)(ok ? blk : 0) * block_stride + head_off;
         const uint32_t at = pg * kPageBytes + lds_piece;
         dma16(kpool + off, k_src[e & 1], lds_address(buf ? k_lds1 : k_lds0) + at);
@@ -361,7 +392,7 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
 
         // s[rb][hb][b][v] is the score of row 16 rb + j16 and tile key 32 hb + key_lane + 4 b + v
         const int key0 = kt * kBlockN;
-        if (key0 + kBlockN - 1 > P + it.q0) {
+        if (key0 + kBlockN - 1 > (SHARED && full ? L - 1 : P + it.q0)) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int rel = lim[rb] - key0 - key_lane;
@@ -470,9 +501,9 @@ __device__ __forceinline__ void attention_body(const AttnArgs& a, const unsigned
                 int kb = __builtin_amdgcn_readlane(ids, kpg), vb = __builtin_amdgcn_readlane(ids, vpg);
                 // pages past the table, past the sequence or with a bad id read block 0
                 // (their keys are masked and their values zeroed below)
-                const bool kok = kt * 4 + kpg < a.max_blocks && (kt * 4 + kpg) * kPage < L &&
+                const bool kok = kt * 4 + kpg < a.max_blocks - page0 && (kt * 4 + kpg) * kPage < L &&
                                  kb >= 0 && kb < a.num_blocks;
-                const bool vok = kt * 4 + vpg < a.max_blocks && (kt * 4 + vpg) * kPage < L &&
+                const bool vok = kt * 4 + vpg < a.max_blocks - page0 && (kt * 4 + vpg) * kPage < L &&
                                  vb >= 0 && vb < a.num_blocks;
                 kb = kok ? kb : 0;
                 vb = vok ? vb : 0;

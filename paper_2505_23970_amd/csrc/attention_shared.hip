@@ -1,0 +1,158 @@
+// Attention of a batch whose requests share long prefixes (GreenCache §2.2: many requests reuse one
+// context, a system prompt or a document): the shared keys and values are read once for all of a
+// group's queries.
+//
+// Mathematics. A row's softmax over its keys is joined from two sets, the S keys that its group shares
+// and its own (the rest of its cached prefix and its new tokens): with the partial outputs o_c and
+// log-sum-exps l_c of any split of the keys into chunks c,
+//     m = max_c l_c,   o = sum_c exp(l_c - m) o_c / sum_c exp(l_c - m),   lse = m + ln sum_c exp(l_c - m),
+// so the shared set may be computed for all rows of the group at once: rows of other requests are
+// further rows of the same matrix products, with no mask.
+//
+// Work. Three launches: plan (once a batch), items, merge. One launch runs both kinds of items, so that
+// they overlap: 128-row items (64-key tiles through LDS; the shared parts, and own parts of many new
+// tokens), bound by the matrix cores and the softmax, and small items (one wavefront, 16 rows; own parts
+// of single tokens), bound by reading K and V. Workgroups of the two kinds are mixed evenly.
+#include "attention_kernels.h"
+
+namespace gc {
+namespace {
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(kAttnThreads, 2) void attention_shared_kernel(const SharedAttnArgs a) {
+    attention_body<D, kWaves, FP8, 2, true>(a, blockIdx.x);
+}
+
+// Merge: a thread owns four consecutive output elements of one row; its chunks' log-sum-exps and
+// values are read kBatch at a time in one pass with a running maximum, the shared chunks first, in a
+// fixed order (deterministic). What bounds it is the chain of dependent loads: the request (a search
+// of the new-token offsets, 64 at a step), its record, the chunks.
+template <int D>
+__global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const SharedMergeArgs a) {
+    constexpr int CPR = D / 4;
+    constexpr int kRows = kCombineThreads / CPR;
+    if (a.status[0] != 0) return;  // the plan holds no work
+    const int lane = threadIdx.x & 63;
+    const int c4 = (int)threadIdx.x % CPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / CPR;
+    const bool in_range = row < a.rows;
+    const int t = (int)((in_range ? row : a.rows - 1) / a.num_q_heads);
+    // the request of the wavefront's first row: the last r with cu[r] <= t0
+    const int t0 = __builtin_amdgcn_readfirstlane(t);
+    int lo = 0, hi = a.batch;  // cu[lo] <= t0 < cu[hi]
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64;
+        const int at = lo + step * (lane + 1);
+        const bool past = at >= hi || a.cu_new_lens[at < hi ? at : hi] > t0;
+        const unsigned long long not_past = __ballot(!past);
+        lo += step * __builtin_popcountll(not_past);
+        hi = min(lo + step, hi);
+    }
+    int r = lo;
+    while (r + 1 < a.batch && a.cu_new_lens[r + 1] <= t) ++r;
+    if (!in_range) return;
+    const SharedReq q = a.reqs[r];
+    const int i = t - q.cu;
+    if (!q.merge || i < 0 || i >= q.n) return;
+    const int h = (int)(row - (int64_t)t * a.num_q_heads);
+    const int kvh = (int)((unsigned)h / (unsigned)a.group), hl = h - kvh * a.group;
+
+    // rows of this row's partials: first chunk, and the distance from one chunk to the next
+    auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
+        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
+        const int tile = (int)((unsigned)i / (unsigned)tq);
+        stride = (int64_t)a.num_kv_heads * bm;
+        first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
+        return tile;
+    };
+    int64_t g_row = 0, g_stride = 0, o_row, o_stride;
+    if (q.g_ns > 0) locate(t - q.g_cu, q.g_small, q.g_slot, q.g_ns, g_row, g_stride);
+    const int tile = locate(i, q.own_small, q.own_slot, q.own_ns, o_row, o_stride);
+    int own = q.own_ns;
+    if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq, min(a.tq, q.n - tile * a.tq), kBlockN));
+    const int total = q.g_ns + own;
+    const float* const g_o = q.g_small ? a.small_o : a.big_o;
+    const float* const g_l = q.g_small ? a.small_lse : a.big_lse;
+    const float* const o_o = q.own_small ? a.small_o : a.big_o;
+    const float* const o_l = q.own_small ? a.small_lse : a.big_lse;
+
+    constexpr int kBatch = 8;
+    float mx = -INFINITY, tot = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < total; s0 += kBatch) {
+        float l[kBatch];
+        f32x4 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int c = s0 + u;
+            l[u] = -INFINITY;
+            v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (c < total) {
+                const bool shared = c < q.g_ns;
+                const int64_t pr = shared ? g_row + c * g_stride : o_row + (c - q.g_ns) * o_stride;
+                l[u] = (shared ? g_l : o_l)[pr];
+                v[u] = *reinterpret_cast<const f32x4*>((shared ? g_o : o_o) + pr * D + 4 * c4);
+            }
+        }
+        float mn = mx;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, l[u]);
+        const float off = mn == -INFINITY ? 0.f : mn;
+        const float alpha = expf(mx - off);
+        tot *= alpha;
+        acc *= alpha;
+        mx = mn;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const float w = expf(l[u] - off);  // 0 for the padding entries
+            tot += w;
+            acc += w * v[u];
+        }
+    }
+    // as in an unsplit item: weights that are all 0 give 0, a NaN sum gives NaN, both with lse -inf
+    const float lse_tot = tot > 0.f ? mx + logf(tot) : -INFINITY;
+    acc *= tot > 0.f ? 1.f / tot : 0.f;
+    u32x2 w2;
+    w2[0] = pack_bf16x2(acc[0], acc[1]);
+    w2[1] = pack_bf16x2(acc[2], acc[3]);
+    *reinterpret_cast<u32x2*>(a.out + row * D + 4 * c4) = w2;
+    if (a.lse != nullptr && c4 == 0) a.lse[row] = lse_tot;
+}
+
+}  // namespace
+
+int shared_small_per_workgroup(bool fp8) { return fp8 ? 4 : 2; }
+
+hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, bool fp8, hipStream_t s) {
+    SharedAttnArgs a = args;
+    const int64_t big = ceil_div64(a.big, kQueues);
+    const int64_t small = ceil_div64(ceil_div64(a.small, shared_small_per_workgroup(fp8)), kQueues);
+    if (big + small == 0) return hipSuccess;
+    // rounded up: then exactly `big` of all groups are of the first kind
+    a.mix = (((uint64_t)big << 32) + (uint64_t)(big + small) - 1) / (uint64_t)(big + small);
+    const dim3 grid((unsigned)((big + small) * kQueues));
+    if (fp8) {
+        if (head_dim == 128)
+            attention_shared_kernel<128, true><<<grid, kAttnThreads, 0, s>>>(a);
+        else
+            attention_shared_kernel<64, true><<<grid, kAttnThreads, 0, s>>>(a);
+    } else {
+        if (head_dim == 128)
+            attention_shared_kernel<128, false><<<grid, kAttnThreads, 0, s>>>(a);
+        else
+            attention_shared_kernel<64, false><<<grid, kAttnThreads, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s) {
+    const int64_t rows = kCombineThreads / (head_dim / 4);
+    const dim3 grid((unsigned)ceil_div64(a.rows, rows));
+    if (head_dim == 128)
+        shared_merge_kernel<128><<<grid, kCombineThreads, 0, s>>>(a);
+    else
+        shared_merge_kernel<64><<<grid, kCombineThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace gc

@@ -18,6 +18,7 @@ constexpr int kBlockN = 64;
 constexpr int kDecM = 16;
 constexpr int kDecN = 32;
 constexpr int kPage = 16;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kAttnThreads = kWaves * 64;
 // Wide prefill tiles: 8 wavefronts, 256 query rows per work item (one workgroup
 // per CU; every K/V tile copied into LDS feeds twice the rows).
@@ -44,6 +45,22 @@ struct WorkItem {
     int32_t r, q0, kt_begin, kt_end, part, P, cu, n;
 };
 
+// The same in a shared-prefix launch. Keys (and key tiles) count from page page0 of table row r:
+// `keys` of them, of which row t of the tile sees the first P + q0 + t + 1, or all where full is set.
+// part < 0: written to the output, else a partial slot of the tile's height.
+struct SharedItem {
+    int32_t r, q0, kt_begin, kt_end, part, P, cu, n;
+    int32_t page0, keys, full, pad;
+};
+
+// Keys of an item, its first page in the table row, and whether every row sees all of its keys.
+__host__ __device__ inline int item_keys(const WorkItem& it) { return it.P + it.n; }
+__host__ __device__ inline int item_keys(const SharedItem& it) { return it.keys; }
+__host__ __device__ inline constexpr int item_page0(const WorkItem&) { return 0; }
+__host__ __device__ inline int item_page0(const SharedItem& it) { return it.page0; }
+__host__ __device__ inline constexpr bool item_full(const WorkItem&) { return false; }
+__host__ __device__ inline bool item_full(const SharedItem& it) { return it.full != 0; }
+
 // One query tile whose keys were split: partial slots [part_base, part_base + ns).
 struct CombineItem {
     int32_t r, q0, part_base, ns;
@@ -67,6 +84,75 @@ __host__ __device__ inline int key_tiles(int prefix, int q0, int ntok, int block
 __host__ __device__ inline int num_splits(int kt, int chunk) {
     return (chunk <= 0 || kt <= chunk) ? 1 : ceil_div(kt, chunk);
 }
+
+// ---------------------------------------------------------------- shared prefixes
+// Work of a shared-prefix launch, derived by the same functions on the host (grid sizes, workspace)
+// and in the planner kernel (the list). Every group of requests whose prefix is taken once has one
+// shared part: its requests' new tokens, adjacent in the packed order, against the S shared keys, all
+// visible. Every request has an own part: its new tokens against its keys from S on, causal.
+struct SharedSizes {
+    int tq, tq_small;             // new tokens per 128-row and per 16-row query tile (0: no small tiles)
+    int chunk, chunk_small;       // key tiles per chunk: of 64 keys, of 32 for small tiles; 0: never split
+    int always;                   // share whatever it costs (gc_shared.policy)
+};
+
+// What one group or request adds to the launch: `tiles` query tiles of `ns` key chunks each.
+struct PartWork {
+    int keys, small, tiles, ns;
+    __host__ __device__ int items() const { return tiles * ns; }
+};
+
+// Shared keys that are taken once for a group of `active` requests with `tokens` new tokens in all,
+// whose own query tiles of 128 rows number `own_tiles`: all S of them, or none where that saves nothing.
+__host__ __device__ inline int shared_taken(int S, int active, int tokens, int own_tiles, const SharedSizes& z) {
+    if (S <= 0 || active <= 0) return 0;
+    if (z.always) return S;
+    if (active < 2 || S < kBlockN) return 0;
+    return ceil_div(tokens, z.tq) * 10 <= own_tiles * 9 ? S : 0;
+}
+
+__host__ __device__ inline PartWork shared_part(int S, int tokens, const SharedSizes& z) {
+    PartWork w{S, 0, 0, 0};
+    if (S <= 0 || tokens <= 0) return w;
+    w.small = tokens <= z.tq_small;
+    w.tiles = w.small ? 1 : ceil_div(tokens, z.tq);
+    w.ns = num_splits(ceil_div(S, w.small ? kDecN : kBlockN), w.small ? z.chunk_small : z.chunk);
+    return w;
+}
+
+// (P: cached tokens of the request past the shared ones. The chunks are those of its last query
+// tile; a tile of fewer key tiles than chunks leaves the last of its items empty.)
+__host__ __device__ inline PartWork own_part(int P, int n, const SharedSizes& z) {
+    PartWork w{P + n, 0, 0, 0};
+    if (n <= 0) return w;
+    w.small = n <= z.tq_small;
+    w.tiles = w.small ? 1 : ceil_div(n, z.tq);
+    w.ns = num_splits(ceil_div(P + n, w.small ? kDecN : kBlockN), w.small ? z.chunk_small : z.chunk);
+    return w;
+}
+
+// Key tiles [begin, end) of chunk c of ns: the first kt % ns chunks take one more.
+__host__ __device__ inline int chunk_begin(int kt, int ns, int c) {
+    const int lo = kt / ns, more = kt - lo * ns;
+    return c * lo + (c < more ? c : more);
+}
+
+// What the merge has to know of a request (written by the planner).
+struct SharedReq {
+    int32_t cu, n, P, merge;              // first row, new tokens, own cached tokens; rows are merged
+    int32_t own_small, own_ns, own_slot;  // chunks and first partial slot of its own part
+    int32_t g_cu, g_small, g_ns, g_slot;  // the group's: first row, chunks (0: nothing shared), first slot
+    int32_t pad[5];
+};
+static_assert(sizeof(SharedReq) == 64, "four 16-byte loads");
+
+// The planner's scratch: four prefix sums, a record of 8 int32 per group (at most as many as requests),
+// a position per request.
+inline size_t shared_scratch_ints(int batch) { return 4 * ((size_t)batch + 1) + 8 * (size_t)batch + (size_t)batch; }
+
+struct SharedLayout {
+    size_t reqs_off, big_off, small_off, scratch_off, big_lse_off, big_o_off, small_lse_off, small_o_off, total;
+};
 
 // Pool pages that receive new tokens over the batch (the append grid), from the
 // host lengths: pages P_r / 16 .. (P_r + n_r - 1) / 16 of every request with n_r > 0.
@@ -178,6 +264,44 @@ struct AttnArgs {
     float v_scale;       // value scale of 8-bit pools, 1 for bf16 pools
 };
 
+// One launch of both kinds of items: `big` workgroups of 128-row items, and workgroups whose
+// wavefronts take one small item each. Workgroups come in groups of eight (one per XCD); the kinds
+// are mixed evenly over the launch: of the first i groups, i * mix >> 32 are of the first kind.
+struct SharedAttnArgs : AttnArgs {  // items: the 128-row items
+    const SharedItem* small_items;
+    float* small_o;      // [slots][Hkv][16][D]
+    float* small_lse;    // [slots][Hkv][16]
+    int32_t big, small;  // workgroups of the first kind; small items times KV heads
+    uint64_t mix;
+};
+
+struct SharedPlanArgs {
+    const int32_t* prefix_lens;
+    const int32_t* cu_new_lens;
+    const int32_t* group_first;   // [groups + 1]
+    const int32_t* shared_lens;   // [groups]
+    int32_t* status;
+    int32_t* scratch;             // shared_scratch_ints(batch)
+    SharedReq* reqs;
+    SharedItem* big_items;
+    SharedItem* small_items;
+    int32_t batch, groups, total_tokens, max_blocks;
+    int32_t expect_big, expect_small, expect_big_slots, expect_small_slots;
+    SharedSizes z;
+};
+
+struct SharedMergeArgs {
+    uint16_t* out;
+    float* lse;
+    const float *big_o, *big_lse, *small_o, *small_lse;
+    const int32_t* cu_new_lens;
+    const int32_t* status;
+    const SharedReq* reqs;
+    int64_t rows;  // T * Hq
+    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small;
+    int32_t big_slots, small_slots;
+};
+
 struct CombineArgs {
     uint16_t* out;
     float* lse;
@@ -208,6 +332,11 @@ hipError_t launch_attention_small(const AttnArgs& a, int head_dim, int64_t num_i
                                   hipStream_t s);
 hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* sink, hipStream_t s);
 hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
+hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
+hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool fp8, hipStream_t s);
+// small items that one workgroup of that launch takes
+int shared_small_per_workgroup(bool fp8);
+hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s);
 // max_splits: the most key chunks of any split query tile
 hipError_t launch_combine(const CombineArgs& a, int head_dim, int64_t num_combines, int max_splits, hipStream_t s);
 

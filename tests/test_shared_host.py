@@ -1,0 +1,126 @@
+"""Shared-prefix attention on the CPU: refusals before any HIP call, workspace sizes, what the policy takes."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2505_23970_amd as gc
+from test_abi_host import HostBatch, geo
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return gc.load_library()
+
+
+class HostShared:
+    def __init__(self, first, lens, policy=1, dev=0x1000, groups=None):
+        self.first = np.ascontiguousarray(first, np.int32)
+        self.lens = np.ascontiguousarray(lens, np.int32)
+        p = ctypes.POINTER(ctypes.c_int32)
+        self.desc = gc.Shared(len(self.lens) if groups is None else groups, self.first.ctypes.data_as(p),
+                              self.lens.ctypes.data_as(p), dev, dev, policy)
+
+
+def size(lib, g, b, s, opts=None, fp8=0):
+    out = ctypes.c_size_t(0)
+    st = lib.gc_shared_prefix_workspace_size(ctypes.byref(g), ctypes.byref(b.desc), ctypes.byref(s.desc),
+                                             ctypes.byref(opts) if opts is not None else None, fp8, ctypes.byref(out))
+    return st, out.value
+
+
+def run(lib, g, b, s, opts=None, scale=0.1, ptrs=(0x2000, 0x2000, 0x2000, 0x2000), ws=0x3000, ws_bytes=1 << 40, scales=None):
+    q, kp, vp, out = ptrs
+    head = (ctypes.byref(g), ctypes.byref(b.desc), ctypes.byref(s.desc) if s is not None else None,
+            ctypes.byref(opts) if opts is not None else None, q, kp, vp)
+    if scales is None:
+        got = {getattr(lib, f"gc_shared_prefix_{n}")(*head, scale, out, None, ws, ws_bytes, None) for n in ("run", "attention")}
+    else:
+        got = {getattr(lib, f"gc_shared_prefix_{n}_fp8")(*head, *scales, scale, out, None, ws, ws_bytes, None)
+               for n in ("run", "attention")}
+    assert len(got) == 1
+    return got.pop()
+
+
+B = lambda: HostBatch([40, 35, 33, 8], [1, 2, 1, 1])  # noqa: E731
+GOOD = lambda **k: HostShared([0, 3, 4], [32, 0], **k)  # noqa: E731
+
+
+def test_groups_and_shared_lengths(lib):
+    assert size(lib, geo(), B(), GOOD())[0] == 0
+    for first, lens in (([0, 3, 5], [32, 0]), ([0, 3, 3], [32, 0]), ([1, 3, 4], [32, 0]), ([0, 5, 4], [32, 0]),
+                        ([0, 3, 4], [30, 0]), ([0, 3, 4], [-16, 0]), ([0, 3, 4], [48, 0]), ([0, 3, 4], [32, 16]),
+                        ([0, 1, 2, 3, 4, 4], [0, 0, 0, 0, 0])):
+        s = HostShared(first, lens)
+        assert size(lib, geo(), B(), s)[0] == -2, (first, lens)
+        assert run(lib, geo(), B(), s) == -2
+    assert size(lib, geo(), B(), HostShared([0, 4], [8], groups=0))[0] == -2
+    assert size(lib, geo(), B(), GOOD(policy=2))[0] == -2
+    s = GOOD()
+    s.desc.reserved[5] = 1
+    assert size(lib, geo(), B(), s)[0] == -2
+    # the shared pages must lie in the table row, also of a group without new tokens
+    assert size(lib, geo(maxb=3), HostBatch([80, 8], [0, 1]), HostShared([0, 1, 2], [80, 0]))[0] == -4
+
+
+def test_null_arguments_and_pointers(lib):
+    assert run(lib, geo(), B(), None) == -1
+    assert run(lib, geo(), B(), GOOD(dev=None)) == -1
+    for k in range(4):
+        ptrs = [0x2000] * 4
+        ptrs[k] = None
+        assert run(lib, geo(), B(), GOOD(), ptrs=ptrs) == -1
+        ptrs[k] = 0x2008
+        assert run(lib, geo(), B(), GOOD(), ptrs=ptrs) == -2
+    assert run(lib, geo(), B(), GOOD(), ws=None) == -5
+    assert run(lib, geo(), B(), GOOD(), ws=0x3008) == -5
+    need = size(lib, geo(), B(), GOOD())[1]
+    assert run(lib, geo(), B(), GOOD(), ws_bytes=need - 1) == -5
+    s = GOOD()
+    assert lib.gc_shared_prefix_workspace_size(ctypes.byref(geo()), ctypes.byref(B().desc), ctypes.byref(s.desc), None, 0, None) == -1
+    s.desc.group_first_host = None
+    assert size(lib, geo(), B(), s)[0] == -1
+    assert lib.gc_shared_prefix_plan(ctypes.byref(geo()), ctypes.byref(B().desc), ctypes.byref(GOOD().desc), None, 0, 0x3000, 100, None) == -5
+
+
+def test_options_and_scales(lib):
+    for tiling in (gc.TILES_PREFILL, gc.TILES_SMALL, gc.TILES_WIDE):
+        assert run(lib, geo(), B(), GOOD(), opts=gc.PlanOptions(0, tiling)) == -3
+    assert run(lib, geo(), B(), GOOD(), opts=gc.PlanOptions(0, 9)) == -2
+    for scale in (0.0, float("inf"), float("nan")):
+        assert run(lib, geo(), B(), GOOD(), scale=scale) == -2
+    assert run(lib, geo(), B(), GOOD(), scales=(0.0, 1.0)) == -2
+    assert run(lib, geo(D=96), B(), GOOD()) == -3
+
+
+def test_nothing_to_do(lib):
+    empty = HostShared([0], [])
+    assert run(lib, geo(), HostBatch([], []), empty) == 0
+    assert size(lib, geo(), HostBatch([], []), empty) == (0, 0)
+    assert run(lib, geo(), HostBatch([40, 40], [0, 0]), HostShared([0, 2], [32])) == 0
+
+
+def plain_size(lib, g, b):
+    out = ctypes.c_size_t(0)
+    assert lib.gc_prefix_prefill_workspace_size(ctypes.byref(g), ctypes.byref(b.desc), None, ctypes.byref(out)) == 0
+    return out.value
+
+
+@pytest.mark.parametrize("P,n,first,lens,taken", [
+    ([6000] * 16, [1] * 16, [0, 16], [5600], True),                # answers on one document
+    ([6000] * 16, [1] * 16, [0, 16], [48], False),                 # less than a key tile
+    ([6000, 6000], [1, 0], [0, 2], [5600], False),                 # one request alone
+    ([6000] * 4, [160] * 4, [0, 4], [5600], False),                # whole query tiles each: nothing to save
+    ([6000] * 4, [20] * 4, [0, 4], [5600], True),                  # tiles a third full
+    ([6000] * 4 + [50], [160] * 4 + [1], [0, 4, 5], [5600, 0], False),
+])
+def test_what_the_policy_takes(lib, P, n, first, lens, taken):
+    """A batch that is left to the plain attention has its workspace."""
+    g, b = geo(Hq=64, Hkv=8, NB=100000, maxb=400), HostBatch(P, n)
+    st, auto = size(lib, g, b, HostShared(first, lens, policy=gc.SHARE_AUTO))
+    assert st == 0
+    assert (auto != plain_size(lib, g, b)) == taken
+    st, always = size(lib, g, b, HostShared(first, lens, policy=gc.SHARE_ALWAYS))
+    assert st == 0 and always != plain_size(lib, g, b)
+    if taken:
+        assert auto == always
