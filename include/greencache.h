@@ -345,8 +345,9 @@ typedef struct gc_shared {
  * gc_shared_prefix_plan is run by gc_shared_prefix_run with the same batch, groups and
  * options), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1); gc_prefix_prefill_plan_status
  * serves them too, and covers the groups' device arrays. Options: tiling GC_TILES_AUTO only
- * (else GC_ERR_UNSUPPORTED); kv_split_tiles counts 64-key tiles, 32-key tiles for requests whose new
- * tokens fit one small tile. Everything else, layouts, results in `out` and `lse`, sharing of a
+ * (else GC_ERR_UNSUPPORTED); kv_split_tiles > 0 cuts 128-row tiles into chunks of that many 64-key
+ * tiles, and the small tiles of successive requests into runs of that many 32-key tiles, < 0 leaves
+ * 128-row tiles whole and makes a run as long as the longest small tile. Everything else, layouts, results in `out` and `lse`, sharing of a
  * workspace by runs, errors, is as for those calls; further errors: GC_ERR_NULL_ARG for a
  * missing array, GC_ERR_BAD_SHAPE for groups or shared lengths outside the above and for q, pools or
  * out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_BLOCK_TABLE for a shared length

@@ -750,7 +750,9 @@ gc_status run_with_append(const gc_geometry* geo, const gc_batch* batch, const g
 struct SharedPlan {
     bool any = false;  // some group's shared keys are taken once (else the plain attention runs)
     gc::SharedSizes z{};
-    int64_t big = 0, small = 0, big_slots = 0, small_slots = 0;  // items and partial slots
+    int64_t big = 0, big_slots = 0;         // 128-row items and their partial slots
+    int64_t parts = 0, places = 0;          // small parts and their places in the sequence
+    int64_t pieces = 0, runs = 0;           // of the small tiles' sequence
     gc::SharedLayout layout{};
 };
 
@@ -773,57 +775,74 @@ gc_status check_shared(const gc_geometry* geo, const gc_batch* b, const gc_share
     return GC_OK;
 }
 
-// f(PartWork, shared) for every shared and own part of the batch.
+// f(PartWork, shared) for every shared part, and then for every own part of the batch (shared: of a group
+// whose shared keys are taken once).
 template <typename F>
 void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes& z, F&& f) {
-    for (int g = 0; g < s->groups; ++g) {
-        const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1];
-        int active = 0, tokens = 0, tiles = 0;
-        for (int r = ra; r < rb; ++r) {
-            const int n = b->new_lens_host[r];
-            active += n > 0;
-            tokens += n;
-            tiles += gc::ceil_div(n, z.tq);
+    int64_t at = 0;
+    auto part = [&](int keys, int n, bool shared) {
+        const gc::PartWork w = gc::part_work(keys, n, at, z);
+        if (w.small) at += gc::kPieceCost + w.kt;
+        f(w, shared);
+    };
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int g = 0; g < s->groups; ++g) {
+            const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1];
+            int active = 0, tokens = 0, tiles = 0;
+            for (int r = ra; r < rb; ++r) {
+                const int n = b->new_lens_host[r];
+                active += n > 0;
+                tokens += n;
+                tiles += gc::ceil_div(n, z.tq);
+            }
+            const int S = gc::shared_taken(s->shared_lens_host[g], active, tokens, tiles, z);
+            if (pass == 0) {
+                part(S, tokens, S > 0);
+                continue;
+            }
+            for (int r = ra; r < rb; ++r)
+                part(b->prefix_lens_host[r] - S + b->new_lens_host[r], b->new_lens_host[r], S > 0);
         }
-        const int S = gc::shared_taken(s->shared_lens_host[g], active, tokens, tiles, z);
-        f(gc::shared_part(S, tokens, z), S > 0);
-        for (int r = ra; r < rb; ++r) f(gc::own_part(b->prefix_lens_host[r] - S, b->new_lens_host[r], z), S > 0);
     }
 }
 
-// Chunks of the key axis. The launch has two 128-row workgroups a compute unit, or as many workgroups
-// of small items, so the parts are cut until they fill those slots: the smallest chunk length (in cost;
-// a small item's tiles are shorter) whose items fit, at least kMinChunk key tiles, below which an item's
-// fixed cost and its partial rows outweigh the shorter chunk.
-constexpr int kMinChunk = 8, kMinChunkSmall = 12;
+// Chunks of the key axis. TODO(rule text)
+constexpr int kMinChunk = 4, kMinRun = 8;
 
 void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
-    const int64_t slots = 2LL * device_cus();
-    const int per = gc::shared_small_per_workgroup(pk.fp8);
-    z->chunk = z->chunk_small = 0;
-    int longest = 1;  // in units of cost: a 64-key tile 4, a small tile 3
+    const int64_t cus = device_cus(), heads = geo->num_kv_heads;
+    z->chunk = 0;
+    z->run = 1;
+    int64_t units = 0, places = 0;
+    int longest = 1;
     for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) {
-        if (w.tiles == 0) return;
-        const int cost = w.small ? 3 * gc::ceil_div(w.keys, gc::kDecN) : 4 * gc::ceil_div(w.keys, gc::kBlockN);
-        if (cost > longest) longest = cost;
+        if (w.small) {
+            places += gc::kPieceCost + w.kt;
+        } else if (w.tiles > 0) {
+            units += w.tiles;
+            if (w.kt > longest) longest = w.kt;
+        }
     });
-    auto set = [&](int cost) {
-        z->chunk = cost / 4 > kMinChunk ? cost / 4 : kMinChunk;
-        z->chunk_small = cost / 3 > kMinChunkSmall ? cost / 3 : kMinChunkSmall;
+    int64_t slots = geo->head_dim == 128 ? cus : 2 * cus, big = 0;
+    if (units * heads > slots) slots = 2 * cus;
+    auto fits = [&](int c) {
+        z->chunk = c;
+        big = 0;
+        for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) { big += w.small ? 0 : (int64_t)w.tiles * w.ns; });
+        return big * heads <= slots;
     };
-    auto fits = [&](int cost) {
-        set(cost);
-        int64_t big = 0, small = 0;
-        for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) { (w.small ? small : big) += (int64_t)w.tiles * w.ns; });
-        return big * geo->num_kv_heads + (small * geo->num_kv_heads + per - 1) / per <= slots;
-    };
-    int lo = 1, hi = longest;
+    int lo = kMinChunk < longest ? kMinChunk : longest, hi = longest;
     while (lo < hi) {
         const int mid = lo + (hi - lo) / 2;
         if (fits(mid)) hi = mid;
         else lo = mid + 1;
     }
-    set(lo);
+    fits(lo);
+    int64_t wgs = 2 * cus - big * heads;
+    if (wgs < cus) wgs = cus;
+    const int64_t waves = gc::shared_small_per_workgroup(pk.fp8) * wgs;
+    const int64_t run = waves >= heads ? gc::ceil_div64(places, waves / heads) : gc::ceil_div64(places * heads, waves);
+    z->run = run > kMinRun ? (int)run : kMinRun;
 }
 
 gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,
@@ -832,21 +851,36 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
     z.tq = gc::tokens_per_tile(sh.group, gc::kBlockM);
     z.tq_small = sh.group <= gc::kDecM ? gc::tokens_per_tile(sh.group, gc::kDecM) : 0;
     z.always = s->policy == GC_SHARE_ALWAYS;
+    z.run = 1;
     pl->any = false;
     for_each_part(b, s, z, [&](const gc::PartWork&, bool shared) { pl->any |= shared; });
     if (!pl->any) return GC_OK;
     if (o != nullptr && o->kv_split_tiles != 0) {
-        z.chunk = z.chunk_small = o->kv_split_tiles > 0 ? o->kv_split_tiles : 0;
+        z.chunk = z.run = o->kv_split_tiles > 0 ? o->kv_split_tiles : 0;
+        if (z.run == 0) {
+            z.run = 1;
+            int longest = 1;
+            for_each_part(b, s, z, [&](const gc::PartWork& w, bool) { longest = w.small && w.kt + gc::kPieceCost > longest ? w.kt + gc::kPieceCost : longest; });
+            z.run = longest;
+        }
     } else {
         choose_shared_chunks(geo, b, s, pk, &z);
     }
     for_each_part(b, s, z, [&](const gc::PartWork& w, bool shared) {
-        const int64_t items = (int64_t)w.tiles * w.ns;
-        (w.small ? pl->small : pl->big) += items;
-        if (shared || w.ns > 1) (w.small ? pl->small_slots : pl->big_slots) += items;
+        const int64_t items = w.small ? 0 : (int64_t)w.tiles * w.ns;
+        pl->big += items;
+        if (shared || w.ns > 1) pl->big_slots += items;
+        pl->parts += w.small;
+        pl->places += w.small ? gc::kPieceCost + w.kt : 0;
     });
+    if (pl->places > 0) {
+        pl->pieces = pl->parts + (pl->places - 1) / z.run;
+        pl->runs = gc::ceil_div64(pl->places, z.run);
+    }
     const int64_t most = (int64_t)INT32_MAX / geo->num_kv_heads - 64;
-    if (pl->big > most || pl->small > most || sh.total_tokens * geo->num_q_heads / 8 >= INT32_MAX) return GC_ERR_BAD_SHAPE;
+    if (pl->big > most || pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run ||
+        sh.total_tokens * geo->num_q_heads / 8 >= INT32_MAX)
+        return GC_ERR_BAD_SHAPE;
     gc::SharedLayout& l = pl->layout;
     size_t off = 256;  // (the status word leads, as in the plain workspace)
     auto take = [&](size_t bytes) {
@@ -857,12 +891,13 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
     const size_t heads = (size_t)geo->num_kv_heads, D = (size_t)geo->head_dim;
     l.reqs_off = take(sizeof(gc::SharedReq) * (size_t)b->batch);
     l.big_off = take(sizeof(gc::SharedItem) * (size_t)pl->big);
-    l.small_off = take(sizeof(gc::SharedItem) * (size_t)pl->small);
+    l.small_off = take(sizeof(gc::SharedItem) * (size_t)pl->pieces);
+    l.runs_off = take(sizeof(int32_t) * (size_t)pl->runs);
     l.scratch_off = take(sizeof(int32_t) * gc::shared_scratch_ints(b->batch));
     l.big_lse_off = take(sizeof(float) * (size_t)pl->big_slots * heads * gc::kBlockM);
-    l.small_lse_off = take(sizeof(float) * (size_t)pl->small_slots * heads * gc::kDecM);
+    l.small_lse_off = take(sizeof(float) * (size_t)pl->pieces * heads * gc::kDecM);
     l.big_o_off = take(sizeof(float) * (size_t)pl->big_slots * heads * gc::kBlockM * D);
-    l.small_o_off = take(sizeof(float) * (size_t)pl->small_slots * heads * gc::kDecM * D);
+    l.small_o_off = take(sizeof(float) * (size_t)pl->pieces * heads * gc::kDecM * D);
     l.total = off;
     return GC_OK;
 }
@@ -905,10 +940,13 @@ gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const g
     a.groups = s->groups;
     a.total_tokens = (int32_t)sh.total_tokens;
     a.max_blocks = geo->max_blocks_per_seq;
+    a.run_first = at<int32_t>(ws, spl.layout.runs_off);
     a.expect_big = (int32_t)spl.big;
-    a.expect_small = (int32_t)spl.small;
     a.expect_big_slots = (int32_t)spl.big_slots;
-    a.expect_small_slots = (int32_t)spl.small_slots;
+    a.expect_parts = (int32_t)spl.parts;
+    a.expect_places = (int32_t)spl.places;
+    a.pieces = (int32_t)spl.pieces;
+    a.num_runs = (int32_t)spl.runs;
     a.z = spl.z;
     return gc::launch_shared_plan(a, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
@@ -940,7 +978,9 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     a.small_o = at<float>(ws, spl.layout.small_o_off);
     a.small_lse = at<float>(ws, spl.layout.small_lse_off);
     a.big = (int32_t)(spl.big * geo->num_kv_heads);
-    a.small = (int32_t)(spl.small * geo->num_kv_heads);
+    a.runs = at<int32_t>(ws, spl.layout.runs_off);
+    a.small = (int32_t)(spl.runs * geo->num_kv_heads);
+    a.pieces = (int32_t)spl.pieces;
     if (gc::launch_attention_shared(a, geo->head_dim, pk.fp8, stream) != hipSuccess) return GC_ERR_HIP;
     gc::SharedMergeArgs m{};
     m.out = a.out;
@@ -959,6 +999,7 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     m.group = sh.group;
     m.tq = spl.z.tq;
     m.tq_small = spl.z.tq_small;
+    m.block_m = gc::kBlockM;
     return gc::launch_shared_merge(m, geo->head_dim, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 

@@ -126,7 +126,7 @@ __device__ __forceinline__ void widen_e4m3x16(const u32x4 c, u32x4& lo, u32x4& h
 // them are visible to every row where `full` is set; the launch's small items run here too, in
 // the same LDS.
 template <int D, int WAVES, bool FP8, int WGS = 8 / WAVES, bool SHARED = false, typename Args = AttnArgs>
-__device__ __forceinline__ void attention_body(const Args& a, unsigned bid) {
+__device__ __forceinline__ void attention_body(const Args& a, const unsigned bid) {
     constexpr int kBlockRows = WAVES * kRowsPerWave;  // query rows of a work item
     constexpr int KS = D / 32;                      // k-steps of QK^T
     constexpr int DB = D / 16;                      // 16-row blocks of O^T
@@ -148,25 +148,27 @@ __device__ __forceinline__ void attention_body(const Args& a, unsigned bid) {
     __shared__ __align__(16) unsigned char v_lds1[kTileBytes];
 
     if constexpr (SHARED) {
-        // (i * mix >> 32 of the first i groups of eight are of the first kind)
-        const unsigned grp = bid / kQueues, in = bid % kQueues;
-        const unsigned before = (unsigned)(grp * a.mix >> 32);
-        if ((unsigned)((grp + 1) * a.mix >> 32) == before) {
+        if (bid >= (unsigned)a.big_wgs) {
             constexpr int kPer = FP8 ? 4 : 2;  // rings that fit the tile buffers
             constexpr int kTile = kSmallTileBytes<D, FP8>;
             static_assert(WAVES == 4 && (FP8 ? 2 * kTile : kTile) == kTileBytes, "rings");
             const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-            const unsigned at = ((grp - before) * kQueues + in) * kPer + w;
+            const unsigned at = (bid - (unsigned)a.big_wgs) * kPer + w;
             if (w >= kPer || at >= (unsigned)a.small) return;
             AttnArgs s = a;
             s.part_o = a.small_o;
             s.part_lse = a.small_lse;
             unsigned char* const r0 = FP8 ? (w == 0 ? k_lds0 : w == 1 ? v_lds0 : w == 2 ? k_lds1 : v_lds1) : (w == 0 ? k_lds0 : k_lds1);
             unsigned char* const r1 = FP8 ? r0 + kTile : (w == 0 ? v_lds0 : v_lds1);
-            small_body<D, FP8, true>(s, a.small_items[at / (unsigned)a.num_kv_heads], (int)(at % (unsigned)a.num_kv_heads), r0, r1);
+            const int kvh = (int)(at % (unsigned)a.num_kv_heads);
+            // (the bound holds whatever the plan wrote)
+            for (int id = a.runs[at / (unsigned)a.num_kv_heads]; id >= 0 && id < a.pieces; ++id) {
+                const SharedItem it = a.small_items[id];
+                small_body<D, FP8, true>(s, it, kvh, r0, r1);
+                if (it.last) break;
+            }
             return;
         }
-        bid = before * kQueues + in;
         if (bid >= (unsigned)a.big) return;
     }
 
@@ -186,7 +188,7 @@ __device__ __forceinline__ void attention_body(const Args& a, unsigned bid) {
     // 2052 us, 70B chat 434 -> 422, 8B chat 125.7 -> 121.5, over 8-bit pools 173.6 -> 154.8; at
     // d = 64, where three 128-row workgroups share a compute unit, 2 % slower, so not there.
     // (Before the item's loads: between them and their uses the branch cost 1-3 % of short launches.)
-    if (WAVES == kWideWaves ? wave < WAVES / 2 : D == 128 && ((SHARED ? blockIdx.x : bid) / a.prefer_span & 1) == a.prefer_odd)
+    if (WAVES == kWideWaves ? wave < WAVES / 2 : !SHARED && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd)
         __builtin_amdgcn_s_setprio(2);
     const int g4 = lane >> 4;
     const int j16 = lane & 15;

@@ -31,7 +31,7 @@ template <int D>
 __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const SharedMergeArgs a) {
     constexpr int CPR = D / 4;
     constexpr int kRows = kCombineThreads / CPR;
-    if (a.status[0] != 0) return;  // the plan holds no work
+    const int status = a.status[0];  // (looked at below, so that the search does not wait for it)
     const int lane = threadIdx.x & 63;
     const int c4 = (int)threadIdx.x % CPR;
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / CPR;
@@ -44,22 +44,20 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
         const int step = (hi - lo + 63) / 64;
         const int at = lo + step * (lane + 1);
         const bool past = at >= hi || a.cu_new_lens[at < hi ? at : hi] > t0;
-        const unsigned long long not_past = __ballot(!past);
-        lo += step * __builtin_popcountll(not_past);
+        lo += step * __builtin_popcountll(__ballot(!past));
         hi = min(lo + step, hi);
     }
     int r = lo;
-    while (r + 1 < a.batch && a.cu_new_lens[r + 1] <= t) ++r;
-    if (!in_range) return;
-    const SharedReq q = a.reqs[r];
+    SharedReq q = a.reqs[r];
+    while (t >= q.cu + q.n && r + 1 < a.batch) q = a.reqs[++r];  // (later rows of the wavefront)
     const int i = t - q.cu;
-    if (!q.merge || i < 0 || i >= q.n) return;
+    if (status != 0 || !in_range || !q.merge || i < 0 || i >= q.n) return;
     const int h = (int)(row - (int64_t)t * a.num_q_heads);
     const int kvh = (int)((unsigned)h / (unsigned)a.group), hl = h - kvh * a.group;
 
-    // rows of this row's partials: first chunk, and the distance from one chunk to the next
+    // row of this row's first partial, and the distance to the next chunk's
     auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
-        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
+        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : a.block_m;
         const int tile = (int)((unsigned)i / (unsigned)tq);
         stride = (int64_t)a.num_kv_heads * bm;
         first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
@@ -68,7 +66,7 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     int64_t g_row = 0, g_stride = 0, o_row, o_stride;
     if (q.g_ns > 0) locate(t - q.g_cu, q.g_small, q.g_slot, q.g_ns, g_row, g_stride);
     const int tile = locate(i, q.own_small, q.own_slot, q.own_ns, o_row, o_stride);
-    int own = q.own_ns;
+    int own = q.own_ns;  // (a tile of fewer key tiles has fewer chunks)
     if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq, min(a.tq, q.n - tile * a.tq), kBlockN));
     const int total = q.g_ns + own;
     const float* const g_o = q.g_small ? a.small_o : a.big_o;
@@ -76,7 +74,7 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     const float* const o_o = q.own_small ? a.small_o : a.big_o;
     const float* const o_l = q.own_small ? a.small_lse : a.big_lse;
 
-    constexpr int kBatch = 8;
+    constexpr int kBatch = 16;
     float mx = -INFINITY, tot = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < total; s0 += kBatch) {
@@ -125,12 +123,10 @@ int shared_small_per_workgroup(bool fp8) { return fp8 ? 4 : 2; }
 
 hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, bool fp8, hipStream_t s) {
     SharedAttnArgs a = args;
-    const int64_t big = ceil_div64(a.big, kQueues);
-    const int64_t small = ceil_div64(ceil_div64(a.small, shared_small_per_workgroup(fp8)), kQueues);
-    if (big + small == 0) return hipSuccess;
-    // rounded up: then exactly `big` of all groups are of the first kind
-    a.mix = (((uint64_t)big << 32) + (uint64_t)(big + small) - 1) / (uint64_t)(big + small);
-    const dim3 grid((unsigned)((big + small) * kQueues));
+    a.big_wgs = (int)(ceil_div64(a.big, kQueues) * kQueues);
+    const int64_t small = ceil_div64(a.small, shared_small_per_workgroup(fp8));
+    if (a.big_wgs + small == 0) return hipSuccess;
+    const dim3 grid((unsigned)(a.big_wgs + small));
     if (fp8) {
         if (head_dim == 128)
             attention_shared_kernel<128, true><<<grid, kAttnThreads, 0, s>>>(a);

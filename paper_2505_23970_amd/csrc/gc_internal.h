@@ -47,10 +47,11 @@ struct WorkItem {
 
 // The same in a shared-prefix launch. Keys (and key tiles) count from page page0 of table row r:
 // `keys` of them, of which row t of the tile sees the first P + q0 + t + 1, or all where full is set.
-// part < 0: written to the output, else a partial slot of the tile's height.
+// part < 0: written to the output, else a partial slot of the tile's height. last: the last of a
+// wavefront's small items.
 struct SharedItem {
     int32_t r, q0, kt_begin, kt_end, part, P, cu, n;
-    int32_t page0, keys, full, pad;
+    int32_t page0, keys, full, last;
 };
 
 // Keys of an item, its first page in the table row, and whether every row sees all of its keys.
@@ -91,16 +92,23 @@ __host__ __device__ inline int num_splits(int kt, int chunk) {
 // shared part: its requests' new tokens, adjacent in the packed order, against the S shared keys, all
 // visible. Every request has an own part: its new tokens against its keys from S on, causal.
 struct SharedSizes {
-    int tq, tq_small;             // new tokens per 128-row and per 16-row query tile (0: no small tiles)
-    int chunk, chunk_small;       // key tiles per chunk: of 64 keys, of 32 for small tiles; 0: never split
-    int always;                   // share whatever it costs (gc_shared.policy)
+    int tq, tq_small;  // new tokens per 128-row and per 16-row query tile (0: no small tiles)
+    int chunk;         // 64-key tiles per chunk of a 128-row tile; 0: never split
+    int run;           // places of one wavefront's run over the small tiles (PartWork)
+    int always;        // share whatever it costs (gc_shared.policy)
 };
 
-// What one group or request adds to the launch: `tiles` query tiles of `ns` key chunks each.
+// What one group or request adds to the launch. 128-row tiles: `tiles` query tiles of `ns` key chunks
+// each. Small: one query tile of kt key tiles. The small tiles of the batch form one sequence (per KV
+// head), groups first, each part kPieceCost places for its start (its loads before the first tile, its
+// results) and then its key tiles; wavefront j takes the key tiles at places [j run, (j + 1) run). So a
+// part is cut into ns pieces where runs end, and its pieces have numbers of their own: the part's index
+// among the small parts plus the run's (numbers in between may be nobody's).
 struct PartWork {
-    int keys, small, tiles, ns;
-    __host__ __device__ int items() const { return tiles * ns; }
+    int keys, small, tiles, ns, kt;
 };
+constexpr int kPieceCost = 4;
+__host__ __device__ inline int run_of(int64_t place, int run) { return (int)((uint32_t)place / (uint32_t)run); }
 
 // Shared keys that are taken once for a group of `active` requests with `tokens` new tokens in all,
 // whose own query tiles of 128 rows number `own_tiles`: all S of them, or none where that saves nothing.
@@ -111,24 +119,19 @@ __host__ __device__ inline int shared_taken(int S, int active, int tokens, int o
     return ceil_div(tokens, z.tq) * 10 <= own_tiles * 9 ? S : 0;
 }
 
-__host__ __device__ inline PartWork shared_part(int S, int tokens, const SharedSizes& z) {
-    PartWork w{S, 0, 0, 0};
-    if (S <= 0 || tokens <= 0) return w;
-    w.small = tokens <= z.tq_small;
-    w.tiles = w.small ? 1 : ceil_div(tokens, z.tq);
-    w.ns = num_splits(ceil_div(S, w.small ? kDecN : kBlockN), w.small ? z.chunk_small : z.chunk);
-    return w;
-}
-
-// (P: cached tokens of the request past the shared ones. The chunks are those of its last query
-// tile; a tile of fewer key tiles than chunks leaves the last of its items empty.)
-__host__ __device__ inline PartWork own_part(int P, int n, const SharedSizes& z) {
-    PartWork w{P + n, 0, 0, 0};
-    if (n <= 0) return w;
+// A part of n new tokens against `keys` keys; at: its first place in the sequence.
+__host__ __device__ inline PartWork part_work(int keys, int n, int64_t at, const SharedSizes& z) {
+    PartWork w{keys, 0, 0, 0, 0};
+    if (keys <= 0 || n <= 0) return w;
     w.small = n <= z.tq_small;
     w.tiles = w.small ? 1 : ceil_div(n, z.tq);
-    w.ns = num_splits(ceil_div(P + n, w.small ? kDecN : kBlockN), w.small ? z.chunk_small : z.chunk);
+    w.kt = ceil_div(keys, w.small ? kDecN : kBlockN);
+    w.ns = w.small ? run_of(at + kPieceCost + w.kt - 1, z.run) - run_of(at + kPieceCost, z.run) + 1 : num_splits(w.kt, z.chunk);
     return w;
+}
+// Number of a small part's first piece; parts: small parts before it.
+__host__ __device__ inline int first_piece(int parts, int64_t at, const SharedSizes& z) {
+    return parts + run_of(at + kPieceCost, z.run);
 }
 
 // Key tiles [begin, end) of chunk c of ns: the first kt % ns chunks take one more.
@@ -146,12 +149,10 @@ struct SharedReq {
 };
 static_assert(sizeof(SharedReq) == 64, "four 16-byte loads");
 
-// The planner's scratch: four prefix sums, a record of 8 int32 per group (at most as many as requests),
-// a position per request.
-inline size_t shared_scratch_ints(int batch) { return 4 * ((size_t)batch + 1) + 8 * (size_t)batch + (size_t)batch; }
+size_t shared_scratch_ints(int batch);  // the planner's scratch, for batches that do not fit its LDS
 
 struct SharedLayout {
-    size_t reqs_off, big_off, small_off, scratch_off, big_lse_off, big_o_off, small_lse_off, small_o_off, total;
+    size_t reqs_off, big_off, small_off, runs_off, scratch_off, big_lse_off, big_o_off, small_lse_off, small_o_off, total;
 };
 
 // Pool pages that receive new tokens over the batch (the append grid), from the
@@ -264,15 +265,15 @@ struct AttnArgs {
     float v_scale;       // value scale of 8-bit pools, 1 for bf16 pools
 };
 
-// One launch of both kinds of items: `big` workgroups of 128-row items, and workgroups whose
-// wavefronts take one small item each. Workgroups come in groups of eight (one per XCD); the kinds
-// are mixed evenly over the launch: of the first i groups, i * mix >> 32 are of the first kind.
+// One launch of both kinds of items: workgroups of 128-row items first (rounded up to whole rounds of
+// the XCDs), then workgroups whose wavefronts take one run of small items each.
 struct SharedAttnArgs : AttnArgs {  // items: the 128-row items
-    const SharedItem* small_items;
-    float* small_o;      // [slots][Hkv][16][D]
-    float* small_lse;    // [slots][Hkv][16]
-    int32_t big, small;  // workgroups of the first kind; small items times KV heads
-    uint64_t mix;
+    const SharedItem* small_items;  // by piece number
+    const int32_t* runs;            // [runs] first piece of every run
+    float* small_o;                 // [pieces][Hkv][16][D]
+    float* small_lse;               // [pieces][Hkv][16]
+    int32_t big, big_wgs;           // 128-row items times KV heads, their workgroups
+    int32_t small, pieces;          // runs times KV heads; pieces
 };
 
 struct SharedPlanArgs {
@@ -285,8 +286,10 @@ struct SharedPlanArgs {
     SharedReq* reqs;
     SharedItem* big_items;
     SharedItem* small_items;
+    int32_t* run_first;
     int32_t batch, groups, total_tokens, max_blocks;
-    int32_t expect_big, expect_small, expect_big_slots, expect_small_slots;
+    int32_t expect_big, expect_big_slots, expect_parts, expect_places;  // small parts and their places
+    int32_t pieces, num_runs;
     SharedSizes z;
 };
 
@@ -298,8 +301,7 @@ struct SharedMergeArgs {
     const int32_t* status;
     const SharedReq* reqs;
     int64_t rows;  // T * Hq
-    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small;
-    int32_t big_slots, small_slots;
+    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small, block_m;
 };
 
 struct CombineArgs {
@@ -334,7 +336,7 @@ hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* sink, hipS
 hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
 hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool fp8, hipStream_t s);
-// small items that one workgroup of that launch takes
+// runs of small items that one workgroup of that launch takes
 int shared_small_per_workgroup(bool fp8);
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s);
 // max_splits: the most key chunks of any split query tile

@@ -1,12 +1,15 @@
 // Work lists of the shared-prefix attention, built on the device from the device copies of the lengths
 // (no host-to-device copy, so a plan can be enqueued freely and captured in a graph). One workgroup:
 //   1. the device lengths are checked before anything is derived from them;
-//   2. per-request prefix sums (requests with new tokens, own 128-row query tiles) give every group its
+//   2. prefix sums over requests (requests with new tokens, own 128-row query tiles) give every group its
 //      rows and whether its shared keys are taken once; scans over groups and then requests give each
-//      its items and partial slots;
-//   3. every request's record for the merge; every item, found from its index by a search of the scans.
-// Items of a shared part are ordered chunk by chunk, so that the query tiles that read one chunk of keys
-// run side by side and share it in L2; a request's own query tiles longest first.
+//      its items and partial slots, and every request's record for the merge;
+//   3. every item, found from its index by a search of the scans.
+// What bounds it is the chain of these steps, each a barrier and some reads of what the one before wrote:
+// up to kPlanLdsBatch requests all of it stays in LDS.
+// 128-row items of a shared part are ordered chunk by chunk, so that the query tiles that read one chunk
+// of keys run side by side and share it in L2; a request's own query tiles longest first. Small items
+// are pieces of one sequence, cut into equal runs (PartWork).
 // Where the device lengths disagree with the host's, every item is emitted empty and status[0] set.
 #include "gc_internal.h"
 
@@ -16,10 +19,11 @@ namespace {
 struct Quad {
     int x[4];
 };
-enum { kBigItems, kSmallItems, kBigSlots, kSmallSlots };
+enum { kBigItems, kBigSlots, kParts, kPlaces };  // kParts, kPlaces: small parts and their places
 
-// Exclusive scan of four values per thread over the workgroup, from `base`; base receives the totals on top.
-__device__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThreads / 64], Quad& base) {
+// Exclusive scan of four values per thread over the workgroup, from `base`; base receives the totals on
+// top. (Each call has its own tmp, so that one barrier does.)
+__device__ __forceinline__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThreads / 64], Quad& base) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Quad s = v;
 #pragma unroll
@@ -36,20 +40,21 @@ __device__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThreads / 64], Quad& 
     for (int w = 0; w < kPlanThreads / 64; ++w)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (w < wave) at.x[k] += tmp[w].x[k];
-            base.x[k] += tmp[w].x[k];
+            const int t = tmp[w].x[k];
+            if (w < wave) at.x[k] += t;
+            base.x[k] += t;
         }
-    __syncthreads();  // tmp is reused
 #pragma unroll
     for (int k = 0; k < 4; ++k) at.x[k] += s.x[k] - v.x[k];
     return at;
 }
 
-__device__ __forceinline__ Quad quad_of(const PartWork& w, bool slots) {
-    Quad q{{0, 0, 0, 0}};
-    q.x[w.small ? kSmallItems : kBigItems] = w.items();
-    if (slots) q.x[w.small ? kSmallSlots : kBigSlots] = w.items();
-    return q;
+__device__ __forceinline__ void add_part(Quad& q, const PartWork& w, bool slots) {
+    const int n = w.small ? 0 : w.tiles * w.ns;
+    q.x[kBigItems] += n;
+    q.x[kBigSlots] += slots ? n : 0;
+    q.x[kParts] += w.small;
+    q.x[kPlaces] += w.small ? kPieceCost + w.kt : 0;
 }
 
 // largest i with a[i] <= v, in [0, n)
@@ -63,29 +68,32 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int v) {
     return lo;
 }
 
-struct SharedPlanLds {
-    Quad tmp[kPlanThreads / 64];
-    int bad;
-    int cu[kPlanLdsBatch + 1], pre[kPlanLdsBatch], first[kPlanLdsBatch + 1], share[kPlanLdsBatch];
-    int active[kPlanLdsBatch + 1], tiles[kPlanLdsBatch + 1], r_items[kPlanLdsBatch + 1], g_items[kPlanLdsBatch + 1];
-};
+constexpr int kPlanArrays = 11;  // int32 per request of what the planner derives
 
-// A group's record while the plan is made (kept in the workspace behind the requests' scratch).
-struct GroupRec {
-    int taken, r, cu, tokens, slot, big, small_, ns;  // big, small_: position of its first item of that kind
+struct SharedPlanLds {
+    Quad tmp[3][kPlanThreads / 64];
+    int bad;
+    int cu[kPlanLdsBatch + 1], pre[kPlanLdsBatch + 1], first[kPlanLdsBatch + 1], share[kPlanLdsBatch + 1];
+    int derived[kPlanArrays][kPlanLdsBatch + 1];
 };
 
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedPlanArgs a) {
     __shared__ SharedPlanLds sm;
     const int tid = threadIdx.x, B = a.batch, G = a.groups;
+    const SharedSizes z = a.z;
     const bool lds = B <= kPlanLdsBatch;  // (G <= B)
-    int* const s = a.scratch;
-    int* const active = lds ? sm.active : s;
-    int* const tiles = lds ? sm.tiles : s + (B + 1);
-    int* const r_items = lds ? sm.r_items : s + 2 * (B + 1);
-    int* const g_items = lds ? sm.g_items : s + 3 * (B + 1);
-    GroupRec* const groups = reinterpret_cast<GroupRec*>(s + 4 * (B + 1));
-    int* const r_at = s + 4 * (B + 1) + 8 * B;  // position of a request's first own item of its kind
+    auto derived = [&](int k) -> int* { return lds ? sm.derived[k] : a.scratch + (size_t)k * (B + 1); };
+    int* const group_of = derived(0);  // [B]
+    int* const active = derived(1);    // [B + 1] requests with new tokens before this one
+    int* const tiles = derived(2);     // [B + 1] 128-row tiles before it
+    int* const r_big = derived(3);     // [B] own 128-row items before it (after all shared ones)
+    int* const r_slot = derived(4);    // [B] its first partial slot, of 128 rows
+    int* const r_piece = derived(5);   // [B] number of its first piece, if it were small
+    int* const r_at = derived(6);      // [B] its first place, if it were small
+    int* const g_big = derived(7);     // [G] the same of the groups' shared parts
+    int* const g_piece = derived(8);
+    int* const g_at = derived(9);
+    int* const g_taken = derived(10);  // [G] shared keys that are taken once
     if (tid == 0) sm.bad = 0;
     if (lds) {
         for (int r = tid; r <= B; r += kPlanThreads) {
@@ -102,9 +110,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     const int* const share = lds ? sm.share : a.shared_lens;
 
     auto empty_all = [&] {
-        const SharedItem none{-1, 0, 0, 0, -1, 0, 0, 0, 0, 0, 0, 0};
+        const SharedItem none{-1, 0, 0, 0, -1, 0, 0, 0, 0, 0, 0, 1};
         for (int i = tid; i < a.expect_big; i += kPlanThreads) a.big_items[i] = none;
-        for (int i = tid; i < a.expect_small; i += kPlanThreads) a.small_items[i] = none;
+        for (int i = tid; i < a.pieces; i += kPlanThreads) a.small_items[i] = none;
+        for (int i = tid; i < a.num_runs; i += kPlanThreads) a.run_first[i] = 0;
         if (tid == 0) a.status[0] = 1;
     };
 
@@ -123,30 +132,28 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     }
     __syncthreads();
     if (sm.bad) return empty_all();
-    {
-        bool bad = false;  // (in a pass of its own: group bounds are known to be good)
-        for (int r = tid; r < B; r += kPlanThreads) bad |= pre[r] < share[last_at_most(first, G, r)];
-        if (bad) sm.bad = 1;
-    }
-    __syncthreads();
-    if (sm.bad) return empty_all();
 
-    // 2. prefix sums over requests: those with new tokens, and own 128-row tiles
+    // 2. prefix sums over requests. (A thread owns consecutive requests, and groups below.)
     const int per = ceil_div(B, kPlanThreads), r0 = min(B, tid * per), r1 = min(B, r0 + per);
+    const int per_g = ceil_div(G, kPlanThreads), g0 = min(G, tid * per_g), g1 = min(G, g0 + per_g);
     {
         Quad v{{0, 0, 0, 0}}, total{{0, 0, 0, 0}};
+        bool bad = false;
         for (int r = r0; r < r1; ++r) {
-            const int n = cu[r + 1] - cu[r];
+            const int g = last_at_most(first, G, r), n = cu[r + 1] - cu[r];
+            group_of[r] = g;
+            bad |= pre[r] < share[g];
             v.x[0] += n > 0;
-            v.x[1] += ceil_div(n, a.z.tq);
+            v.x[1] += ceil_div(n, z.tq);
         }
-        Quad at = block_scan4(v, sm.tmp, total);
+        if (bad) sm.bad = 1;
+        Quad at = block_scan4(v, sm.tmp[0], total);
         for (int r = r0; r < r1; ++r) {
             const int n = cu[r + 1] - cu[r];
             active[r] = at.x[0];
             tiles[r] = at.x[1];
             at.x[0] += n > 0;
-            at.x[1] += ceil_div(n, a.z.tq);
+            at.x[1] += ceil_div(n, z.tq);
         }
         if (tid == 0) {
             active[B] = total.x[0];
@@ -155,120 +162,136 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     }
     __threadfence_block();
     __syncthreads();
+    if (sm.bad) return empty_all();
 
-    //    groups: what each shares, its items and slots
+    auto tokens_of = [&](int g) { return cu[first[g + 1]] - cu[first[g]]; };
+
+    //    groups: what each shares, its items, slots and pieces
     Quad total{{0, 0, 0, 0}};
-    auto taken_of = [&](int g, int& tokens) {
-        const int ra = first[g], rb = first[g + 1];
-        tokens = cu[rb] - cu[ra];
-        return shared_taken(share[g], active[rb] - active[ra], tokens, tiles[rb] - tiles[ra], a.z);
-    };
-    const int per_g = ceil_div(G, kPlanThreads), g0 = min(G, tid * per_g), g1 = min(G, g0 + per_g);
     {
         Quad v{{0, 0, 0, 0}};
         for (int g = g0; g < g1; ++g) {
-            int tokens;
-            const int S = taken_of(g, tokens);
-            const Quad q = quad_of(shared_part(S, tokens, a.z), true);
-            for (int k = 0; k < 4; ++k) v.x[k] += q.x[k];
+            const int ra = first[g], rb = first[g + 1], tokens = cu[rb] - cu[ra];
+            const int S = shared_taken(share[g], active[rb] - active[ra], tokens, tiles[rb] - tiles[ra], z);
+            g_taken[g] = S;
+            add_part(v, part_work(S, tokens, 0, z), true);
         }
-        Quad at = block_scan4(v, sm.tmp, total);
+        Quad at = block_scan4(v, sm.tmp[1], total);
         for (int g = g0; g < g1; ++g) {
-            int tokens;
-            const int S = taken_of(g, tokens);
-            const PartWork w = shared_part(S, tokens, a.z);
-            groups[g] = GroupRec{S, first[g], cu[first[g]], tokens, at.x[w.small ? kSmallSlots : kBigSlots], at.x[kBigItems], at.x[kSmallItems], w.ns};
-            g_items[g] = at.x[kBigItems] + at.x[kSmallItems];
-            const Quad q = quad_of(w, true);
-            for (int k = 0; k < 4; ++k) at.x[k] += q.x[k];
+            g_big[g] = at.x[kBigItems];  // (and its first slot: every shared item has one)
+            g_piece[g] = first_piece(at.x[kParts], at.x[kPlaces], z);
+            g_at[g] = at.x[kPlaces];
+            add_part(at, part_work(g_taken[g], tokens_of(g), 0, z), true);
         }
     }
-    const int shared_items = total.x[kBigItems] + total.x[kSmallItems];
+    const Quad shared_total = total;
     __threadfence_block();
     __syncthreads();
 
-    //    requests: own items and slots, and the record for the merge
+    //    requests: own items, slots and pieces, and the record for the merge
     {
+        // (a small part alone is merged where runs cut it, which its place in the sequence decides; only
+        // 128-row parts have slots counted here)
         Quad v{{0, 0, 0, 0}};
         for (int r = r0; r < r1; ++r) {
-            const int S = groups[last_at_most(first, G, r)].taken;
-            const PartWork w = own_part(pre[r] - S, cu[r + 1] - cu[r], a.z);
-            const Quad q = quad_of(w, S > 0 || w.ns > 1);
-            for (int k = 0; k < 4; ++k) v.x[k] += q.x[k];
+            const int S = g_taken[group_of[r]];
+            const PartWork w = part_work(pre[r] - S + cu[r + 1] - cu[r], cu[r + 1] - cu[r], 0, z);
+            add_part(v, w, S > 0 || w.ns > 1);
         }
-        Quad at = block_scan4(v, sm.tmp, total);
+        Quad at = block_scan4(v, sm.tmp[2], total);
         for (int r = r0; r < r1; ++r) {
-            const GroupRec g = groups[last_at_most(first, G, r)];
-            const PartWork sw = shared_part(g.taken, g.tokens, a.z);
-            const int n = cu[r + 1] - cu[r];
-            const PartWork w = own_part(pre[r] - g.taken, n, a.z);
-            const bool merge = g.taken > 0 || w.ns > 1;
+            const int g = group_of[r], S = g_taken[g], n = cu[r + 1] - cu[r];
+            const PartWork sw = part_work(S, tokens_of(g), g_at[g], z);
+            const PartWork w = part_work(pre[r] - S + n, n, at.x[kPlaces], z);
+            const int piece = first_piece(at.x[kParts], at.x[kPlaces], z);
             SharedReq q{};
             q.cu = cu[r];
             q.n = n;
-            q.P = pre[r] - g.taken;
-            q.merge = merge;
+            q.P = pre[r] - S;
+            q.merge = S > 0 || w.ns > 1;
             q.own_small = w.small;
             q.own_ns = w.ns;
-            q.own_slot = at.x[w.small ? kSmallSlots : kBigSlots];
-            q.g_cu = g.cu;
+            q.own_slot = w.small ? piece : at.x[kBigSlots];
+            q.g_cu = cu[first[g]];
             q.g_small = sw.small;
-            q.g_ns = g.taken > 0 ? sw.ns : 0;
-            q.g_slot = g.slot;
+            q.g_ns = sw.ns;
+            q.g_slot = sw.small ? g_piece[g] : g_big[g];
             a.reqs[r] = q;
-            r_at[r] = at.x[w.small ? kSmallItems : kBigItems];
-            r_items[r] = at.x[kBigItems] + at.x[kSmallItems] - shared_items;
-            const Quad add = quad_of(w, merge);
-            for (int k = 0; k < 4; ++k) at.x[k] += add.x[k];
+            r_big[r] = at.x[kBigItems] - shared_total.x[kBigItems];
+            r_slot[r] = at.x[kBigSlots];
+            r_piece[r] = piece;
+            r_at[r] = at.x[kPlaces];
+            add_part(at, w, q.merge);
         }
     }
-    const int own_items = total.x[kBigItems] + total.x[kSmallItems] - shared_items;
+    if (total.x[kBigItems] != a.expect_big || total.x[kBigSlots] != a.expect_big_slots || total.x[kParts] != a.expect_parts ||
+        total.x[kPlaces] != a.expect_places)
+        return empty_all();
     __threadfence_block();
     __syncthreads();
-    if (total.x[kBigItems] != a.expect_big || total.x[kSmallItems] != a.expect_small ||
-        total.x[kBigSlots] != a.expect_big_slots || total.x[kSmallSlots] != a.expect_small_slots)
-        return empty_all();
 
-    // 3. items (positions and slots are in range when the totals agree; never write outside all the same)
-    auto put = [&](bool small, int pos, SharedItem it) {
-        const int most = small ? a.expect_small : a.expect_big, slots = small ? a.expect_small_slots : a.expect_big_slots;
-        if (pos < 0 || pos >= most) return;
-        if (it.part >= slots) it.r = -1;
-        (small ? a.small_items : a.big_items)[pos] = it;
-    };
-    for (int i = tid; i < shared_items; i += kPlanThreads) {
-        const int g = last_at_most(g_items, G, i);
-        const GroupRec q = groups[g];
-        const PartWork w = shared_part(q.taken, q.tokens, a.z);
-        if (w.tiles <= 0) continue;
-        const int local = i - g_items[g], c = local / w.tiles, tile = local - c * w.tiles;
-        const int kt = ceil_div(q.taken, w.small ? kDecN : kBlockN);
-        put(w.small, (w.small ? q.small_ : q.big) + local,
-            SharedItem{q.r, tile * a.z.tq, chunk_begin(kt, w.ns, c), chunk_begin(kt, w.ns, c + 1), q.slot + tile * w.ns + c, 0,
-                       q.cu, q.tokens, 0, q.taken, 1, 0});
-    }
-    for (int i = tid; i < own_items; i += kPlanThreads) {
-        const int r = last_at_most(r_items, B, i);
-        const SharedReq q = a.reqs[r];
-        const PartWork w = own_part(q.P, q.n, a.z);
-        if (w.tiles <= 0) continue;
-        const int local = i - r_items[r], c = local % w.ns, tile = w.tiles - 1 - local / w.ns;
-        const int q0 = tile * a.z.tq;
-        const int kt = w.small ? ceil_div(w.keys, kDecN) : key_tiles(q.P, q0, min(a.z.tq, q.n - q0), kBlockN);
-        const int ns = min(w.ns, kt);
-        SharedItem it{r, q0, 0, 0, q.merge ? q.own_slot + tile * w.ns + c : -1, q.P, q.cu, q.n, (pre[r] - q.P) / kPage, w.keys, 0, 0};
-        if (c < ns) {
-            it.kt_begin = chunk_begin(kt, ns, c);
-            it.kt_end = chunk_begin(kt, ns, c + 1);
+    // 3. items (positions are in range when the totals agree; never write outside all the same)
+    for (int i = tid; i < a.expect_big; i += kPlanThreads) {
+        SharedItem it;
+        if (i < shared_total.x[kBigItems]) {
+            const int g = last_at_most(g_big, G, i), S = g_taken[g], tokens = tokens_of(g);
+            const PartWork w = part_work(S, tokens, 0, z);
+            if (w.tiles <= 0) continue;  // (not reached: the group has items)
+            const int local = i - g_big[g], c = local / w.tiles, tile = local - c * w.tiles;
+            it = SharedItem{first[g], tile * z.tq, chunk_begin(w.kt, w.ns, c), chunk_begin(w.kt, w.ns, c + 1), g_big[g] + tile * w.ns + c,
+                            0, cu[first[g]], tokens, 0, S, 1, 0};
         } else {
-            it.r = -1;
+            const int own = i - shared_total.x[kBigItems], r = last_at_most(r_big, B, own), S = g_taken[group_of[r]];
+            const int P = pre[r] - S, n = cu[r + 1] - cu[r];
+            const PartWork w = part_work(P + n, n, 0, z);
+            if (w.ns <= 0) continue;  // (not reached)
+            const int local = own - r_big[r], t = local / w.ns, c = local - t * w.ns;
+            const int tile = w.tiles - 1 - t, q0 = tile * z.tq;
+            const int kt = key_tiles(P, q0, min(z.tq, n - q0), kBlockN), ns = min(w.ns, kt);
+            it = SharedItem{r, q0, 0, 0, S > 0 || w.ns > 1 ? r_slot[r] + tile * w.ns + c : -1, P, cu[r], n, S / kPage, w.keys, 0, 0};
+            if (c < ns) {
+                it.kt_begin = chunk_begin(kt, ns, c);
+                it.kt_end = chunk_begin(kt, ns, c + 1);
+            } else {
+                it.r = -1;
+            }
         }
-        put(w.small, r_at[r] + local, it);
+        if (it.part >= a.expect_big_slots) it.r = -1;
+        a.big_items[i] = it;
+    }
+    for (int i = tid; i < a.num_runs; i += kPlanThreads) a.run_first[i] = -1;  // (a run may hold no key tile)
+    __syncthreads();
+    const int shared_pieces = shared_total.x[kParts] > 0 ? first_piece(shared_total.x[kParts], shared_total.x[kPlaces], z) : 0;
+    for (int i = tid; i < a.pieces; i += kPlanThreads) {
+        // the last part whose first piece is at most i (a number may be nobody's)
+        const bool shared = i < shared_pieces;
+        const int o = shared ? last_at_most(g_piece, G, i) : last_at_most(r_piece, B, i);
+        const int g = shared ? o : group_of[o], S = g_taken[g];
+        const int n = shared ? tokens_of(g) : cu[o + 1] - cu[o], P = shared ? 0 : pre[o] - S;
+        const int at = shared ? g_at[o] : r_at[o];
+        const PartWork w = part_work(shared ? S : P + n, n, at, z);
+        const int c = i - (shared ? g_piece[o] : r_piece[o]);
+        if (!w.small || c < 0 || c >= w.ns) continue;
+        const int run = run_of(at + kPieceCost, z.run) + c;
+        // key tiles of the run, from the part's first one
+        const int64_t begin = (int64_t)run * z.run - at - kPieceCost, end = begin + z.run;
+        // the run ends with this piece: the part goes on in the next, or the next part's first tile lies there
+        const int64_t next = (int64_t)at + kPieceCost + w.kt;
+        const bool last = c + 1 < w.ns || next >= a.expect_places || run_of(next + kPieceCost, z.run) != run;
+        SharedItem it{shared ? first[g] : o, 0, (int)max(begin, (int64_t)0), (int)min(end, (int64_t)w.kt), i, P, shared ? cu[first[g]] : cu[o], n,
+                      shared ? 0 : S / kPage, w.keys, shared, last};
+        if (!shared && S == 0 && w.ns == 1) it.part = -1;
+        a.small_items[i] = it;
+        // the run's first piece: the part began in an earlier run, or the part before ended in one
+        const bool begins = c > 0 || at == 0 || run_of(at - 1, z.run) != run;
+        if (begins && run < a.num_runs) a.run_first[run] = i;
     }
     if (tid == 0) a.status[0] = 0;
 }
 
 }  // namespace
+
+size_t shared_scratch_ints(int batch) { return batch <= kPlanLdsBatch ? 1 : (size_t)kPlanArrays * ((size_t)batch + 1); }
 
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s) {
     shared_plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
