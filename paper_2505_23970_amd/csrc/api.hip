@@ -751,6 +751,7 @@ struct SharedPlan {
     bool any = false;  // some group's shared keys are taken once (else the plain attention runs)
     gc::SharedSizes z{};
     int64_t big = 0, big_slots = 0;         // 128-row items and their partial slots
+    int64_t big_shared = 0;                 // those items of shared parts
     int64_t parts = 0, places = 0;          // small parts and their places in the sequence
     int64_t pieces = 0, runs = 0;           // of the small tiles' sequence
     gc::SharedLayout layout{};
@@ -775,15 +776,15 @@ gc_status check_shared(const gc_geometry* geo, const gc_batch* b, const gc_share
     return GC_OK;
 }
 
-// f(PartWork, shared) for every shared part, and then for every own part of the batch (shared: of a group
-// whose shared keys are taken once).
+// f(PartWork, shared, own) for every shared part, and then for every own part of the batch (shared: of a
+// group whose shared keys are taken once).
 template <typename F>
 void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes& z, F&& f) {
     int64_t at = 0;
-    auto part = [&](int keys, int n, bool shared) {
-        const gc::PartWork w = gc::part_work(keys, n, at, z);
+    auto part = [&](int keys, int n, bool shared, bool own) {
+        const gc::PartWork w = gc::part_work(keys, n, (int)(at & INT32_MAX), z);  // (a longer sequence is refused)
         if (w.small) at += gc::kPieceCost + w.kt;
-        f(w, shared);
+        f(w, shared, own);
     };
     for (int pass = 0; pass < 2; ++pass) {
         for (int g = 0; g < s->groups; ++g) {
@@ -793,45 +794,73 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
                 const int n = b->new_lens_host[r];
                 active += n > 0;
                 tokens += n;
-                tiles += gc::ceil_div(n, z.tq);
+                tiles += z.tq.ceil_of(n);
             }
             const int S = gc::shared_taken(s->shared_lens_host[g], active, tokens, tiles, z);
             if (pass == 0) {
-                part(S, tokens, S > 0);
+                part(S, tokens, S > 0, false);
                 continue;
             }
             for (int r = ra; r < rb; ++r)
-                part(b->prefix_lens_host[r] - S + b->new_lens_host[r], b->new_lens_host[r], S > 0);
+                part(b->prefix_lens_host[r] - S + b->new_lens_host[r], b->new_lens_host[r], S > 0, true);
         }
     }
 }
 
-// Chunks of the key axis. TODO(rule text)
-constexpr int kMinChunk = 4, kMinRun = 8;
+// Tiles and chunks of the key axis. TODO(rule text)
+constexpr int kMinChunk = 4, kMinRun = 8, kItemSteps = 4;
+
+// The batch's work: 128-row parts (the first kKept of them kept) and the places of the small ones.
+struct SharedLoad {
+    static constexpr int kKept = 512;
+    struct {
+        int tiles, kt;
+    } part[kKept];
+    int parts = 0, longest = 1;
+    int64_t units = 0, steps = 0, places = 0;  // 128-row tiles, their key tiles
+};
+
+void shared_load(const gc_batch* b, const gc_shared* s, const gc::SharedSizes& z, SharedLoad* l) {
+    for_each_part(b, s, z, [&](const gc::PartWork& w, bool, bool) {
+        if (w.small) {
+            l->places += gc::kPieceCost + w.kt;
+        } else if (w.tiles > 0) {
+            l->units += w.tiles;
+            l->steps += (int64_t)w.tiles * w.kt;
+            if (w.kt > l->longest) l->longest = w.kt;
+            if (l->parts < SharedLoad::kKept) {
+                l->part[l->parts].tiles = w.tiles;
+                l->part[l->parts].kt = w.kt;
+            }
+            l->parts += 1;
+        }
+    });
+}
 
 void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
     const int64_t cus = device_cus(), heads = geo->num_kv_heads;
-    z->chunk = 0;
-    z->run = 1;
-    int64_t units = 0, places = 0;
-    int longest = 1;
-    for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) {
-        if (w.small) {
-            places += gc::kPieceCost + w.kt;
-        } else if (w.tiles > 0) {
-            units += w.tiles;
-            if (w.kt > longest) longest = w.kt;
-        }
-    });
+    SharedLoad l;
+    shared_load(b, s, *z, &l);
     int64_t slots = geo->head_dim == 128 ? cus : 2 * cus, big = 0;
-    if (units * heads > slots) slots = 2 * cus;
+    if (l.units * heads > slots) slots = 2 * cus;
     auto fits = [&](int c) {
-        z->chunk = c;
+        z->chunk = gc::divisor(c);
         big = 0;
-        for_each_part(b, s, *z, [&](const gc::PartWork& w, bool) { big += w.small ? 0 : (int64_t)w.tiles * w.ns; });
-        return big * heads <= slots;
+        int64_t most = 0;  // items of about the longest chunk
+        auto count = [&](int64_t tiles, int kt) {
+            const int ns = z->chunk.ceil_of(kt);
+            big += tiles * ns;
+            if ((int64_t)kt * 3 >= (int64_t)c * 2 * ns) most += tiles * ns;
+        };
+        if (l.parts <= SharedLoad::kKept)
+            for (int i = 0; i < l.parts; ++i) count(l.part[i].tiles, l.part[i].kt);
+        else
+            for_each_part(b, s, *z, [&](const gc::PartWork& w, bool, bool) {
+                if (!w.small && w.tiles > 0) count(w.tiles, w.kt);
+            });
+        return (l.steps + big * kItemSteps) * heads <= slots * (c + kItemSteps) && most * heads <= slots;
     };
-    int lo = kMinChunk < longest ? kMinChunk : longest, hi = longest;
+    int lo = kMinChunk < l.longest ? kMinChunk : l.longest, hi = l.longest;
     while (lo < hi) {
         const int mid = lo + (hi - lo) / 2;
         if (fits(mid)) hi = mid;
@@ -840,45 +869,46 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     fits(lo);
     int64_t wgs = 2 * cus - big * heads;
     if (wgs < cus) wgs = cus;
-    const int64_t waves = gc::shared_small_per_workgroup(pk.fp8) * wgs;
-    const int64_t run = waves >= heads ? gc::ceil_div64(places, waves / heads) : gc::ceil_div64(places * heads, waves);
-    z->run = run > kMinRun ? (int)run : kMinRun;
+    const int64_t waves = gc::shared_rings(pk.fp8) * wgs;
+    const int64_t run = waves >= heads ? gc::ceil_div64(l.places, waves / heads) : gc::ceil_div64(l.places * heads, waves);
+    z->run = gc::divisor(run > kMinRun ? (int)run : kMinRun);
 }
 
 gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,
                            const Shape& sh, const PoolKind& pk, SharedPlan* pl) {
     gc::SharedSizes& z = pl->z;
-    z.tq = gc::tokens_per_tile(sh.group, gc::kBlockM);
+    z.tq = gc::divisor(gc::tokens_per_tile(sh.group, gc::kBlockM));
+    z.chunk = gc::divisor(INT32_MAX / gc::kBlockN);  // whole
     z.tq_small = sh.group <= gc::kDecM ? gc::tokens_per_tile(sh.group, gc::kDecM) : 0;
     z.always = s->policy == GC_SHARE_ALWAYS;
-    z.run = 1;
     pl->any = false;
-    for_each_part(b, s, z, [&](const gc::PartWork&, bool shared) { pl->any |= shared; });
+    for_each_part(b, s, z, [&](const gc::PartWork&, bool shared, bool) { pl->any |= shared; });
     if (!pl->any) return GC_OK;
-    if (o != nullptr && o->kv_split_tiles != 0) {
-        z.chunk = z.run = o->kv_split_tiles > 0 ? o->kv_split_tiles : 0;
-        if (z.run == 0) {
-            z.run = 1;
-            int longest = 1;
-            for_each_part(b, s, z, [&](const gc::PartWork& w, bool) { longest = w.small && w.kt + gc::kPieceCost > longest ? w.kt + gc::kPieceCost : longest; });
-            z.run = longest;
-        }
+    if (o != nullptr && o->kv_split_tiles > 0) {
+        z.chunk = z.run = gc::divisor(o->kv_split_tiles < (1 << 25) ? o->kv_split_tiles : 1 << 25);
+    } else if (o != nullptr && o->kv_split_tiles < 0) {
+        int longest = 1;
+        for_each_part(b, s, z, [&](const gc::PartWork& w, bool, bool) {
+            if (w.small && w.kt + gc::kPieceCost > longest) longest = w.kt + gc::kPieceCost;
+        });
+        z.run = gc::divisor(longest);
     } else {
         choose_shared_chunks(geo, b, s, pk, &z);
     }
-    for_each_part(b, s, z, [&](const gc::PartWork& w, bool shared) {
+    for_each_part(b, s, z, [&](const gc::PartWork& w, bool shared, bool own) {
         const int64_t items = w.small ? 0 : (int64_t)w.tiles * w.ns;
         pl->big += items;
+        if (!own) pl->big_shared += items;
         if (shared || w.ns > 1) pl->big_slots += items;
         pl->parts += w.small;
         pl->places += w.small ? gc::kPieceCost + w.kt : 0;
     });
     if (pl->places > 0) {
-        pl->pieces = pl->parts + (pl->places - 1) / z.run;
-        pl->runs = gc::ceil_div64(pl->places, z.run);
+        pl->pieces = pl->parts + (pl->places - 1) / z.run.d;
+        pl->runs = gc::ceil_div64(pl->places, z.run.d);
     }
     const int64_t most = (int64_t)INT32_MAX / geo->num_kv_heads - 64;
-    if (pl->big > most || pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run ||
+    if (pl->big > most || pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run.d ||
         sh.total_tokens * geo->num_q_heads / 8 >= INT32_MAX)
         return GC_ERR_BAD_SHAPE;
     gc::SharedLayout& l = pl->layout;
@@ -967,7 +997,7 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     a.num_q_heads = geo->num_q_heads;
     a.num_kv_heads = geo->num_kv_heads;
     a.group = sh.group;
-    a.tq = spl.z.tq;
+    a.tq = spl.z.tq.d;
     a.num_blocks = geo->num_blocks;
     a.max_blocks = geo->max_blocks_per_seq;
     a.scale_log2 = (float)((double)scale * (double)pk.k_scale * 1.4426950408889634074);
@@ -977,7 +1007,8 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     a.small_items = at<gc::SharedItem>(ws, spl.layout.small_off);
     a.small_o = at<float>(ws, spl.layout.small_o_off);
     a.small_lse = at<float>(ws, spl.layout.small_lse_off);
-    a.big = (int32_t)(spl.big * geo->num_kv_heads);
+    a.shared_items = (int32_t)spl.big_shared;
+    a.own_items = (int32_t)(spl.big - spl.big_shared);
     a.runs = at<int32_t>(ws, spl.layout.runs_off);
     a.small = (int32_t)(spl.runs * geo->num_kv_heads);
     a.pieces = (int32_t)spl.pieces;
@@ -997,9 +1028,8 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     m.num_q_heads = geo->num_q_heads;
     m.num_kv_heads = geo->num_kv_heads;
     m.group = sh.group;
-    m.tq = spl.z.tq;
+    m.tq = spl.z.tq.d;
     m.tq_small = spl.z.tq_small;
-    m.block_m = gc::kBlockM;
     return gc::launch_shared_merge(m, geo->head_dim, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 

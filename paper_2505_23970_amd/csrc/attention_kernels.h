@@ -147,11 +147,14 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
     __shared__ __align__(16) unsigned char k_lds1[kTileBytes];
     __shared__ __align__(16) unsigned char v_lds1[kTileBytes];
 
+    int kvh = 0;
+    unsigned item = 0;
     if constexpr (SHARED) {
         if (bid >= (unsigned)a.big_wgs) {
-            constexpr int kPer = FP8 ? 4 : 2;  // rings that fit the tile buffers
+            // rings of two small tiles in the tile buffers
             constexpr int kTile = kSmallTileBytes<D, FP8>;
-            static_assert(WAVES == 4 && (FP8 ? 2 * kTile : kTile) == kTileBytes, "rings");
+            constexpr int kPer = shared_rings(FP8);
+            static_assert((FP8 ? 2 * kTile : kTile) == kTileBytes && kPer <= WAVES, "rings");
             const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
             const unsigned at = (bid - (unsigned)a.big_wgs) * kPer + w;
             if (w >= kPer || at >= (unsigned)a.small) return;
@@ -160,7 +163,7 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
             s.part_lse = a.small_lse;
             unsigned char* const r0 = FP8 ? (w == 0 ? k_lds0 : w == 1 ? v_lds0 : w == 2 ? k_lds1 : v_lds1) : (w == 0 ? k_lds0 : k_lds1);
             unsigned char* const r1 = FP8 ? r0 + kTile : (w == 0 ? v_lds0 : v_lds1);
-            const int kvh = (int)(at % (unsigned)a.num_kv_heads);
+            kvh = (int)(at % (unsigned)a.num_kv_heads);
             // (the bound holds whatever the plan wrote)
             for (int id = a.runs[at / (unsigned)a.num_kv_heads]; id >= 0 && id < a.pieces; ++id) {
                 const SharedItem it = a.small_items[id];
@@ -169,7 +172,21 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
             }
             return;
         }
-        if (bid >= (unsigned)a.big) return;
+        // Workgroup b runs on XCD b % 8. The shared parts' items (KV head by KV head, chunk by chunk, the
+        // query tiles of a chunk side by side) go to the XCDs in eight runs, so that a chunk of keys is
+        // read into one L2; the own parts' follow in turn.
+        const unsigned shared = (unsigned)a.shared_per_xcd * kQueues;
+        if (bid < shared) {
+            const unsigned at = bid % kQueues * (unsigned)a.shared_per_xcd + bid / kQueues;
+            if (at >= (unsigned)a.shared_items * (unsigned)a.num_kv_heads) return;
+            kvh = (int)(at / (unsigned)a.shared_items);
+            item = at - (unsigned)kvh * (unsigned)a.shared_items;
+        } else {
+            const unsigned at = bid - shared;
+            if (at >= (unsigned)a.own_items * (unsigned)a.num_kv_heads) return;
+            kvh = (int)(at % (unsigned)a.num_kv_heads);
+            item = (unsigned)a.shared_items + at / (unsigned)a.num_kv_heads;
+        }
     }
 
     // (opaque to the compiler, so that the lane constants derived from it are computed per
@@ -192,9 +209,12 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         __builtin_amdgcn_s_setprio(2);
     const int g4 = lane >> 4;
     const int j16 = lane & 15;
-    const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
+    if constexpr (!SHARED) {
+        kvh = (int)(bid % (unsigned)a.num_kv_heads);
+        item = bid / (unsigned)a.num_kv_heads;
+    }
     using Item = std::conditional_t<SHARED, SharedItem, WorkItem>;
-    const Item it = reinterpret_cast<const Item*>(a.items)[bid / (unsigned)a.num_kv_heads];
+    const Item it = reinterpret_cast<const Item*>(a.items)[item];
     // all eight fields in one load (else the fields the test below needs are loaded
     // first and the rest after it, a second dependent round trip)
     asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P),

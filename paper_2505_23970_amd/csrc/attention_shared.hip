@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
 
     // row of this row's first partial, and the distance to the next chunk's
     auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
-        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : a.block_m;
+        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
         const int tile = (int)((unsigned)i / (unsigned)tq);
         stride = (int64_t)a.num_kv_heads * bm;
         first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
@@ -119,12 +119,12 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
 
 }  // namespace
 
-int shared_small_per_workgroup(bool fp8) { return fp8 ? 4 : 2; }
-
 hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, bool fp8, hipStream_t s) {
     SharedAttnArgs a = args;
-    a.big_wgs = (int)(ceil_div64(a.big, kQueues) * kQueues);
-    const int64_t small = ceil_div64(a.small, shared_small_per_workgroup(fp8));
+    const int64_t heads = a.num_kv_heads;
+    a.shared_per_xcd = (int)ceil_div64(a.shared_items * heads, kQueues);
+    a.big_wgs = (int)((a.shared_per_xcd + ceil_div64(a.own_items * heads, kQueues)) * kQueues);
+    const int64_t small = ceil_div64(a.small, shared_rings(fp8));
     if (a.big_wgs + small == 0) return hipSuccess;
     const dim3 grid((unsigned)(a.big_wgs + small));
     if (fp8) {

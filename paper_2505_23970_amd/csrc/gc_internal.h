@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace gc {
@@ -91,11 +92,49 @@ __host__ __device__ inline int num_splits(int kt, int chunk) {
 // and in the planner kernel (the list). Every group of requests whose prefix is taken once has one
 // shared part: its requests' new tokens, adjacent in the packed order, against the S shared keys, all
 // visible. Every request has an own part: its new tokens against its keys from S on, causal.
+// (The planner is one workgroup and a chain of such arithmetic: an integer division by a variable, some
+// 35 dependent instructions, is three here.)
+struct Divisor {
+    int d = 1;
+    double inv = 1.0;  // fl64(1 / d)
+    // a / d, exact for a < 2^32: (a + 1/2) / d is at least 1 / (2 d) from every integer, and its
+    // computed value within 2^-20 / d of it.
+    __host__ __device__ int of(uint32_t a) const {
+#ifdef __HIP_DEVICE_COMPILE__
+        return (int)fma((double)a, inv, 0.5 * inv);
+#else
+        return (int)(a / (uint32_t)d);
+#endif
+    }
+    __host__ __device__ int ceil_of(int a) const { return of((uint32_t)a + (uint32_t)d - 1u); }
+};
+inline Divisor divisor(int d) { return Divisor{d, 1.0 / d}; }
+
+// a / d for 0 <= a < 2^31, 0 < d < 2^31.
+__host__ __device__ inline int quick_div(int a, int d) {
+#ifdef __HIP_DEVICE_COMPILE__
+    int q = (int)((float)a * __builtin_amdgcn_rcpf((float)d));
+    int r = a - q * d;
+    while (r < 0) {  // (a step or two where the quotient has more than 22 bits)
+        --q;
+        r += d;
+    }
+    while (r >= d) {
+        ++q;
+        r -= d;
+    }
+    return q;
+#else
+    return a / d;
+#endif
+}
+
 struct SharedSizes {
-    int tq, tq_small;  // new tokens per 128-row and per 16-row query tile (0: no small tiles)
-    int chunk;         // 64-key tiles per chunk of a 128-row tile; 0: never split
-    int run;           // places of one wavefront's run over the small tiles (PartWork)
-    int always;        // share whatever it costs (gc_shared.policy)
+    Divisor tq;    // new tokens per 128-row query tile
+    Divisor chunk; // 64-key tiles per chunk of a 128-row tile
+    Divisor run;   // places of one wavefront's run over the small tiles (PartWork)
+    int tq_small;  // new tokens per 16-row query tile (0: no small tiles)
+    int always;    // share whatever it costs (gc_shared.policy)
 };
 
 // What one group or request adds to the launch. 128-row tiles: `tiles` query tiles of `ns` key chunks
@@ -108,7 +147,6 @@ struct PartWork {
     int keys, small, tiles, ns, kt;
 };
 constexpr int kPieceCost = 4;
-__host__ __device__ inline int run_of(int64_t place, int run) { return (int)((uint32_t)place / (uint32_t)run); }
 
 // Shared keys that are taken once for a group of `active` requests with `tokens` new tokens in all,
 // whose own query tiles of 128 rows number `own_tiles`: all S of them, or none where that saves nothing.
@@ -116,27 +154,30 @@ __host__ __device__ inline int shared_taken(int S, int active, int tokens, int o
     if (S <= 0 || active <= 0) return 0;
     if (z.always) return S;
     if (active < 2 || S < kBlockN) return 0;
-    return ceil_div(tokens, z.tq) * 10 <= own_tiles * 9 ? S : 0;
+    return (int64_t)z.tq.ceil_of(tokens) * 10 <= (int64_t)own_tiles * 9 ? S : 0;
 }
 
 // A part of n new tokens against `keys` keys; at: its first place in the sequence.
-__host__ __device__ inline PartWork part_work(int keys, int n, int64_t at, const SharedSizes& z) {
+__host__ __device__ inline PartWork part_work(int keys, int n, int at, const SharedSizes& z) {
     PartWork w{keys, 0, 0, 0, 0};
     if (keys <= 0 || n <= 0) return w;
     w.small = n <= z.tq_small;
-    w.tiles = w.small ? 1 : ceil_div(n, z.tq);
+    w.tiles = w.small ? 1 : z.tq.ceil_of(n);
     w.kt = ceil_div(keys, w.small ? kDecN : kBlockN);
-    w.ns = w.small ? run_of(at + kPieceCost + w.kt - 1, z.run) - run_of(at + kPieceCost, z.run) + 1 : num_splits(w.kt, z.chunk);
+    w.ns = w.small ? z.run.of((uint32_t)at + kPieceCost + w.kt - 1) - z.run.of((uint32_t)at + kPieceCost) + 1 : z.chunk.ceil_of(w.kt);
     return w;
 }
 // Number of a small part's first piece; parts: small parts before it.
-__host__ __device__ inline int first_piece(int parts, int64_t at, const SharedSizes& z) {
-    return parts + run_of(at + kPieceCost, z.run);
+__host__ __device__ inline int first_piece(int parts, int at, const SharedSizes& z) {
+    return parts + z.run.of(at + kPieceCost);
 }
+
+// Runs of small items that one workgroup takes: its tile buffers hold that many rings of two small tiles.
+__host__ __device__ constexpr int shared_rings(bool fp8) { return fp8 ? 4 : 2; }
 
 // Key tiles [begin, end) of chunk c of ns: the first kt % ns chunks take one more.
 __host__ __device__ inline int chunk_begin(int kt, int ns, int c) {
-    const int lo = kt / ns, more = kt - lo * ns;
+    const int lo = quick_div(kt, ns), more = kt - lo * ns;
     return c * lo + (c < more ? c : more);
 }
 
@@ -272,7 +313,8 @@ struct SharedAttnArgs : AttnArgs {  // items: the 128-row items
     const int32_t* runs;            // [runs] first piece of every run
     float* small_o;                 // [pieces][Hkv][16][D]
     float* small_lse;               // [pieces][Hkv][16]
-    int32_t big, big_wgs;           // 128-row items times KV heads, their workgroups
+    int32_t shared_items, own_items;      // 128-row items of either kind, the shared ones first
+    int32_t shared_per_xcd, big_wgs;      // workgroups of the shared ones on an XCD; of both kinds
     int32_t small, pieces;          // runs times KV heads; pieces
 };
 
@@ -301,7 +343,7 @@ struct SharedMergeArgs {
     const int32_t* status;
     const SharedReq* reqs;
     int64_t rows;  // T * Hq
-    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small, block_m;
+    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small;
 };
 
 struct CombineArgs {
@@ -336,8 +378,6 @@ hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* sink, hipS
 hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
 hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool fp8, hipStream_t s);
-// runs of small items that one workgroup of that launch takes
-int shared_small_per_workgroup(bool fp8);
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s);
 // max_splits: the most key chunks of any split query tile
 hipError_t launch_combine(const CombineArgs& a, int head_dim, int64_t num_combines, int max_splits, hipStream_t s);

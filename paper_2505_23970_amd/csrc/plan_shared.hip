@@ -21,22 +21,29 @@ struct Quad {
 };
 enum { kBigItems, kBigSlots, kParts, kPlaces };  // kParts, kPlaces: small parts and their places
 
+// Inclusive scan over a wavefront: within rows of 16 lanes, then the rows' totals passed on (as lane
+// exchanges in the additions themselves: a sixth of the time of exchanges through the LDS unit).
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);  // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);  // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);  // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
 // Exclusive scan of four values per thread over the workgroup, from `base`; base receives the totals on
 // top. (Each call has its own tmp, so that one barrier does.)
 __device__ __forceinline__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThreads / 64], Quad& base) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Quad s = v;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int y = __shfl_up(s.x[k], d);
-            if (lane >= d) s.x[k] += y;
-        }
+    for (int k = 0; k < 4; ++k) s.x[k] = wave_scan(s.x[k]);
     if (lane == 63) tmp[wave] = s;
     __syncthreads();
     Quad at = base;
-#pragma unroll
+#pragma nounroll
     for (int w = 0; w < kPlanThreads / 64; ++w)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -70,19 +77,29 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int v) {
 
 constexpr int kPlanArrays = 11;  // int32 per request of what the planner derives
 
+template <int BATCH>
 struct SharedPlanLds {
     Quad tmp[3][kPlanThreads / 64];
     int bad;
-    int cu[kPlanLdsBatch + 1], pre[kPlanLdsBatch + 1], first[kPlanLdsBatch + 1], share[kPlanLdsBatch + 1];
-    int derived[kPlanArrays][kPlanLdsBatch + 1];
+    int cu[BATCH + 1], pre[BATCH + 1], first[BATCH + 1], share[BATCH + 1];
+    int derived[kPlanArrays][BATCH + 1];
 };
 
+// LDS: batches of up to kPlanLdsBatch requests. (Pointers that may be either make every access a flat one:
+// with one kernel for both the plan of 64 requests took 9.4 us instead of 8.7, before the scans changed.)
+template <bool LDS>
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedPlanArgs a) {
-    __shared__ SharedPlanLds sm;
+    __shared__ SharedPlanLds<LDS ? kPlanLdsBatch : 1> sm;
     const int tid = threadIdx.x, B = a.batch, G = a.groups;
     const SharedSizes z = a.z;
-    const bool lds = B <= kPlanLdsBatch;  // (G <= B)
-    auto derived = [&](int k) -> int* { return lds ? sm.derived[k] : a.scratch + (size_t)k * (B + 1); };
+    auto derived = [&](int k) -> int* {
+        if constexpr (LDS) return sm.derived[k];
+        else return a.scratch + (size_t)k * (B + 1);
+    };
+    auto either = [](int* in_lds, const int* global) -> const int* {
+        if constexpr (LDS) return in_lds;
+        else return global;
+    };
     int* const group_of = derived(0);  // [B]
     int* const active = derived(1);    // [B + 1] requests with new tokens before this one
     int* const tiles = derived(2);     // [B + 1] 128-row tiles before it
@@ -95,7 +112,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     int* const g_at = derived(9);
     int* const g_taken = derived(10);  // [G] shared keys that are taken once
     if (tid == 0) sm.bad = 0;
-    if (lds) {
+    if constexpr (LDS) {  // (G <= B)
+#pragma nounroll
         for (int r = tid; r <= B; r += kPlanThreads) {
             sm.cu[r] = a.cu_new_lens[r];
             if (r < B) sm.pre[r] = a.prefix_lens[r];
@@ -104,10 +122,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         }
     }
     __syncthreads();
-    const int* const cu = lds ? sm.cu : a.cu_new_lens;
-    const int* const pre = lds ? sm.pre : a.prefix_lens;
-    const int* const first = lds ? sm.first : a.group_first;
-    const int* const share = lds ? sm.share : a.shared_lens;
+    const int* const cu = either(sm.cu, a.cu_new_lens);
+    const int* const pre = either(sm.pre, a.prefix_lens);
+    const int* const first = either(sm.first, a.group_first);
+    const int* const share = either(sm.share, a.shared_lens);
 
     auto empty_all = [&] {
         const SharedItem none{-1, 0, 0, 0, -1, 0, 0, 0, 0, 0, 0, 1};
@@ -120,10 +138,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     // 1. the lengths must describe the batch the host checked
     {
         bool bad = tid == 0 && (cu[0] != 0 || cu[B] != a.total_tokens || first[0] != 0 || first[G] != B);
+#pragma nounroll
         for (int r = tid; r < B; r += kPlanThreads) {
-            const int64_t P = pre[r], n = (int64_t)cu[r + 1] - cu[r];
-            bad |= P < 0 || n < 0 || P + n > (int64_t)INT32_MAX - kBlockN || (n > 0 && ceil_div64(P + n, kPage) > a.max_blocks);
+            const int P = pre[r], n = (int)((uint32_t)cu[r + 1] - (uint32_t)cu[r]);
+            const uint32_t keys = (uint32_t)P + (uint32_t)n;
+            bad |= P < 0 || cu[r] < 0 || cu[r + 1] < cu[r] || keys > (uint32_t)(INT32_MAX - kBlockN) ||
+                   (n > 0 && (keys + kPage - 1) / kPage > (uint32_t)a.max_blocks);
         }
+#pragma nounroll
         for (int g = tid; g < G; g += kPlanThreads) {
             const int S = share[g];
             bad |= S < 0 || S % kPage != 0 || S / kPage > a.max_blocks || first[g] < 0 || first[g + 1] <= first[g] || first[g + 1] > B;
@@ -139,21 +161,23 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     {
         Quad v{{0, 0, 0, 0}}, total{{0, 0, 0, 0}};
         bool bad = false;
+#pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int g = last_at_most(first, G, r), n = cu[r + 1] - cu[r];
             group_of[r] = g;
             bad |= pre[r] < share[g];
             v.x[0] += n > 0;
-            v.x[1] += ceil_div(n, z.tq);
+            v.x[1] += z.tq.ceil_of(n);
         }
         if (bad) sm.bad = 1;
         Quad at = block_scan4(v, sm.tmp[0], total);
+#pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int n = cu[r + 1] - cu[r];
             active[r] = at.x[0];
             tiles[r] = at.x[1];
             at.x[0] += n > 0;
-            at.x[1] += ceil_div(n, z.tq);
+            at.x[1] += z.tq.ceil_of(n);
         }
         if (tid == 0) {
             active[B] = total.x[0];
@@ -170,6 +194,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     Quad total{{0, 0, 0, 0}};
     {
         Quad v{{0, 0, 0, 0}};
+#pragma nounroll
         for (int g = g0; g < g1; ++g) {
             const int ra = first[g], rb = first[g + 1], tokens = cu[rb] - cu[ra];
             const int S = shared_taken(share[g], active[rb] - active[ra], tokens, tiles[rb] - tiles[ra], z);
@@ -177,6 +202,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             add_part(v, part_work(S, tokens, 0, z), true);
         }
         Quad at = block_scan4(v, sm.tmp[1], total);
+#pragma nounroll
         for (int g = g0; g < g1; ++g) {
             g_big[g] = at.x[kBigItems];  // (and its first slot: every shared item has one)
             g_piece[g] = first_piece(at.x[kParts], at.x[kPlaces], z);
@@ -193,12 +219,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         // (a small part alone is merged where runs cut it, which its place in the sequence decides; only
         // 128-row parts have slots counted here)
         Quad v{{0, 0, 0, 0}};
+#pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int S = g_taken[group_of[r]];
             const PartWork w = part_work(pre[r] - S + cu[r + 1] - cu[r], cu[r + 1] - cu[r], 0, z);
             add_part(v, w, S > 0 || w.ns > 1);
         }
         Quad at = block_scan4(v, sm.tmp[2], total);
+#pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int g = group_of[r], S = g_taken[g], n = cu[r + 1] - cu[r];
             const PartWork sw = part_work(S, tokens_of(g), g_at[g], z);
@@ -231,23 +259,24 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     __syncthreads();
 
     // 3. items (positions are in range when the totals agree; never write outside all the same)
+#pragma nounroll
     for (int i = tid; i < a.expect_big; i += kPlanThreads) {
         SharedItem it;
         if (i < shared_total.x[kBigItems]) {
             const int g = last_at_most(g_big, G, i), S = g_taken[g], tokens = tokens_of(g);
             const PartWork w = part_work(S, tokens, 0, z);
             if (w.tiles <= 0) continue;  // (not reached: the group has items)
-            const int local = i - g_big[g], c = local / w.tiles, tile = local - c * w.tiles;
-            it = SharedItem{first[g], tile * z.tq, chunk_begin(w.kt, w.ns, c), chunk_begin(w.kt, w.ns, c + 1), g_big[g] + tile * w.ns + c,
+            const int local = i - g_big[g], c = quick_div(local, w.tiles), tile = local - c * w.tiles;
+            it = SharedItem{first[g], tile * z.tq.d, chunk_begin(w.kt, w.ns, c), chunk_begin(w.kt, w.ns, c + 1), g_big[g] + tile * w.ns + c,
                             0, cu[first[g]], tokens, 0, S, 1, 0};
         } else {
             const int own = i - shared_total.x[kBigItems], r = last_at_most(r_big, B, own), S = g_taken[group_of[r]];
             const int P = pre[r] - S, n = cu[r + 1] - cu[r];
             const PartWork w = part_work(P + n, n, 0, z);
             if (w.ns <= 0) continue;  // (not reached)
-            const int local = own - r_big[r], t = local / w.ns, c = local - t * w.ns;
-            const int tile = w.tiles - 1 - t, q0 = tile * z.tq;
-            const int kt = key_tiles(P, q0, min(z.tq, n - q0), kBlockN), ns = min(w.ns, kt);
+            const int local = own - r_big[r], t = quick_div(local, w.ns), c = local - t * w.ns;
+            const int tile = w.tiles - 1 - t, q0 = tile * z.tq.d;
+            const int kt = key_tiles(P, q0, min(z.tq.d, n - q0), kBlockN), ns = min(w.ns, kt);
             it = SharedItem{r, q0, 0, 0, S > 0 || w.ns > 1 ? r_slot[r] + tile * w.ns + c : -1, P, cu[r], n, S / kPage, w.keys, 0, 0};
             if (c < ns) {
                 it.kt_begin = chunk_begin(kt, ns, c);
@@ -262,6 +291,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     for (int i = tid; i < a.num_runs; i += kPlanThreads) a.run_first[i] = -1;  // (a run may hold no key tile)
     __syncthreads();
     const int shared_pieces = shared_total.x[kParts] > 0 ? first_piece(shared_total.x[kParts], shared_total.x[kPlaces], z) : 0;
+#pragma nounroll
     for (int i = tid; i < a.pieces; i += kPlanThreads) {
         // the last part whose first piece is at most i (a number may be nobody's)
         const bool shared = i < shared_pieces;
@@ -272,18 +302,18 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         const PartWork w = part_work(shared ? S : P + n, n, at, z);
         const int c = i - (shared ? g_piece[o] : r_piece[o]);
         if (!w.small || c < 0 || c >= w.ns) continue;
-        const int run = run_of(at + kPieceCost, z.run) + c;
+        const int run = z.run.of(at + kPieceCost) + c;
         // key tiles of the run, from the part's first one
-        const int64_t begin = (int64_t)run * z.run - at - kPieceCost, end = begin + z.run;
+        const int64_t begin = (int64_t)run * z.run.d - at - kPieceCost, end = begin + z.run.d;
         // the run ends with this piece: the part goes on in the next, or the next part's first tile lies there
         const int64_t next = (int64_t)at + kPieceCost + w.kt;
-        const bool last = c + 1 < w.ns || next >= a.expect_places || run_of(next + kPieceCost, z.run) != run;
+        const bool last = c + 1 < w.ns || next >= a.expect_places || z.run.of(next + kPieceCost) != run;
         SharedItem it{shared ? first[g] : o, 0, (int)max(begin, (int64_t)0), (int)min(end, (int64_t)w.kt), i, P, shared ? cu[first[g]] : cu[o], n,
                       shared ? 0 : S / kPage, w.keys, shared, last};
         if (!shared && S == 0 && w.ns == 1) it.part = -1;
         a.small_items[i] = it;
         // the run's first piece: the part began in an earlier run, or the part before ended in one
-        const bool begins = c > 0 || at == 0 || run_of(at - 1, z.run) != run;
+        const bool begins = c > 0 || at == 0 || z.run.of(at - 1) != run;
         if (begins && run < a.num_runs) a.run_first[run] = i;
     }
     if (tid == 0) a.status[0] = 0;
@@ -294,7 +324,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
 size_t shared_scratch_ints(int batch) { return batch <= kPlanLdsBatch ? 1 : (size_t)kPlanArrays * ((size_t)batch + 1); }
 
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s) {
-    shared_plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
+    if (a.batch <= kPlanLdsBatch)
+        shared_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(a);
+    else
+        shared_plan_kernel<false><<<1, kPlanThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
