@@ -754,6 +754,7 @@ struct SharedPlan {
     int64_t big_shared = 0;                 // those items of shared parts
     int64_t parts = 0, places = 0;          // small parts and their places in the sequence
     int64_t pieces = 0, runs = 0;           // of the small tiles' sequence
+    int max_shared = 0, max_own = 0;        // the most chunks of a part
     gc::SharedLayout layout{};
 };
 
@@ -789,15 +790,10 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
     for (int pass = 0; pass < 2; ++pass) {
         for (int g = 0; g < s->groups; ++g) {
             const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1];
-            int active = 0, tokens = 0, tiles = 0;
-            for (int r = ra; r < rb; ++r) {
-                const int n = b->new_lens_host[r];
-                active += n > 0;
-                tokens += n;
-                tiles += z.tq.ceil_of(n);
-            }
-            const int S = gc::shared_taken(s->shared_lens_host[g], active, tokens, tiles, z);
+            const int S = z.taken(g, s->shared_lens_host[g]);
             if (pass == 0) {
+                int tokens = 0;
+                for (int r = ra; r < rb; ++r) tokens += b->new_lens_host[r];
                 part(S, tokens, S > 0, false);
                 continue;
             }
@@ -805,6 +801,49 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
                 part(b->prefix_lens_host[r] - S + b->new_lens_host[r], b->new_lens_host[r], S > 0, true);
         }
     }
+}
+
+// Which groups' shared keys are taken once: those that it saves time by the estimates below, if together they
+// save more than the merge costs. The plain attention reads S keys for every request, its 16-row tiles from L2
+// at about 20 TB/s over all heads, its 128-row tiles at the matrix cores' pace; taken once, they cost a read
+// from HBM or the pace of the group's own 128-row tiles, and every row two fp32 partial rows, written and
+// read. Paces: us of a compute unit per 128-row tile and 64 keys (48 requests of 20 tokens on 32768 shared ones, the
+// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 1075; at d = 64 533 / 288 and 665 / 341). On 60
+// drawn batches the choice is within TODO of the better of the two.
+constexpr double kShareGain = 2.0, kShareGainTiles = 6.0;  // us: batches of small tiles; with 128-row own parts
+
+void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
+    z->all = s->policy == GC_SHARE_ALWAYS || s->groups > gc::kTakeGroups;
+    if (z->all) return;
+    const double heads = geo->num_kv_heads, D = geo->head_dim;
+    const double key_bytes = heads * D * 2 * (pk.fp8 ? 1 : 2);
+    const double step = heads / device_cus() / gc::kBlockN;  // of a 128-row tile, per key
+    const double plain_pace = D == 128 ? (pk.fp8 ? 1.13 : 0.85) : (pk.fp8 ? 0.86 : 0.69);
+    const double shared_pace = D == 128 ? (pk.fp8 ? 1.12 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
+    double gain = 0;
+    bool any_tiles = false;
+    for (int g = 0; g < s->groups; ++g) {
+        const int S = s->shared_lens_host[g];
+        if (S <= 0) continue;
+        int64_t small = 0, tiles = 0, tokens = 0;
+        for (int r = s->group_first_host[g]; r < s->group_first_host[g + 1]; ++r) {
+            const int n = b->new_lens_host[r];
+            tokens += n;
+            if (n > z->tq_small) tiles += z->tq.ceil_of(n);
+            else small += n > 0;
+        }
+        const double plain = S * (small * key_bytes / 20e6 + tiles * step * plain_pace);
+        const double read = key_bytes / 5.6e6;
+        const double paced = tokens <= z->tq_small ? 0 : gc::ceil_div64(tokens, z->tq.d) * step * shared_pace;
+        const double rows = tokens * geo->num_q_heads * D * 4 * 4 / 4e6;
+        const double saved = plain - S * (read > paced ? read : paced) - rows;
+        if (saved < 0.2) continue;
+        z->take[g / 64] |= 1ull << (g % 64);
+        gain += saved;
+        any_tiles |= tiles > 0;
+    }
+    if (gain < (any_tiles ? kShareGainTiles : kShareGain))
+        for (uint64_t& t : z->take) t = 0;
 }
 
 // Tiles and chunks of the key axis. TODO(rule text)
@@ -880,7 +919,7 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
     z.tq = gc::divisor(gc::tokens_per_tile(sh.group, gc::kBlockM));
     z.chunk = gc::divisor(INT32_MAX / gc::kBlockN);  // whole
     z.tq_small = sh.group <= gc::kDecM ? gc::tokens_per_tile(sh.group, gc::kDecM) : 0;
-    z.always = s->policy == GC_SHARE_ALWAYS;
+    choose_groups(geo, b, s, pk, &z);
     pl->any = false;
     for_each_part(b, s, z, [&](const gc::PartWork&, bool shared, bool) { pl->any |= shared; });
     if (!pl->any) return GC_OK;
@@ -899,6 +938,8 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
         const int64_t items = w.small ? 0 : (int64_t)w.tiles * w.ns;
         pl->big += items;
         if (!own) pl->big_shared += items;
+        int& most = own ? pl->max_own : pl->max_shared;
+        if (w.ns > most) most = w.ns;
         if (shared || w.ns > 1) pl->big_slots += items;
         pl->parts += w.small;
         pl->places += w.small ? gc::kPieceCost + w.kt : 0;
@@ -1030,7 +1071,7 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     m.group = sh.group;
     m.tq = spl.z.tq.d;
     m.tq_small = spl.z.tq_small;
-    return gc::launch_shared_merge(m, geo->head_dim, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+    return gc::launch_shared_merge(m, geo->head_dim, spl.max_shared + spl.max_own, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
 gc_status run_shared(const gc_geometry* geo, const gc_batch* batch, const gc_shared* shared, const gc_plan_options* opts,

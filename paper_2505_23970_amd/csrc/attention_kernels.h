@@ -205,6 +205,8 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
     // 2052 us, 70B chat 434 -> 422, 8B chat 125.7 -> 121.5, over 8-bit pools 173.6 -> 154.8; at
     // d = 64, where three 128-row workgroups share a compute unit, 2 % slower, so not there.
     // (Before the item's loads: between them and their uses the branch cost 1-3 % of short launches.)
+    // Not in shared-prefix launches: one 128-row workgroup a unit beside a small one is as fast without, two are
+    // faster (48 questions of 20 tokens on 32768 shared ones 914 us, with it 964).
     if (WAVES == kWideWaves ? wave < WAVES / 2 : !SHARED && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd)
         __builtin_amdgcn_s_setprio(2);
     const int g4 = lane >> 4;

@@ -24,17 +24,22 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attention_shared_kernel(const
 }
 
 // Merge: a thread owns four consecutive output elements of one row; its chunks' log-sum-exps and
-// values are read kBatch at a time in one pass with a running maximum, the shared chunks first, in a
-// fixed order (deterministic). What bounds it is the chain of dependent loads: the request (a search
-// of the new-token offsets, 64 at a step), its record, the chunks.
-template <int D>
+// values are read kBatch at a time in one pass with a running maximum, in a fixed order (deterministic).
+// What bounds it is the chain of dependent loads: the request (a search of the new-token offsets, 64 at
+// a step), its record, the chunks. With G > 1 a row's chunks are dealt to G groups of threads (chunk c to
+// group c % G), whose results are joined through LDS in group order: for few rows of many chunks.
+template <int D, int G>
 __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const SharedMergeArgs a) {
-    constexpr int CPR = D / 4;
-    constexpr int kRows = kCombineThreads / CPR;
+    constexpr int CPR = D / 4;                          // threads per row and group
+    constexpr int kRows = kCombineThreads / (CPR * G);  // rows per workgroup
+    __shared__ f32x4 s_acc[G > 1 ? kCombineThreads : 1];
+    __shared__ float s_max[G > 1 ? kCombineThreads / CPR : 1], s_tot[G > 1 ? kCombineThreads / CPR : 1];
     const int status = a.status[0];  // (looked at below, so that the search does not wait for it)
     const int lane = threadIdx.x & 63;
     const int c4 = (int)threadIdx.x % CPR;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / CPR;
+    const int lane_row = (int)threadIdx.x / CPR;  // (row, group) of this thread
+    const int sub = lane_row % G;
+    const int64_t row = (int64_t)blockIdx.x * kRows + lane_row / G;
     const bool in_range = row < a.rows;
     const int t = (int)((in_range ? row : a.rows - 1) / a.num_q_heads);
     // the request of the wavefront's first row: the last r with cu[r] <= t0
@@ -51,60 +56,85 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     SharedReq q = a.reqs[r];
     while (t >= q.cu + q.n && r + 1 < a.batch) q = a.reqs[++r];  // (later rows of the wavefront)
     const int i = t - q.cu;
-    if (status != 0 || !in_range || !q.merge || i < 0 || i >= q.n) return;
+    const bool row_ok = status == 0 && in_range && q.merge && i >= 0 && i < q.n;
+    if (G == 1 && !row_ok) return;
     const int h = (int)(row - (int64_t)t * a.num_q_heads);
     const int kvh = (int)((unsigned)h / (unsigned)a.group), hl = h - kvh * a.group;
 
-    // row of this row's first partial, and the distance to the next chunk's
-    auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
-        const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
-        const int tile = (int)((unsigned)i / (unsigned)tq);
-        stride = (int64_t)a.num_kv_heads * bm;
-        first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
-        return tile;
-    };
-    int64_t g_row = 0, g_stride = 0, o_row, o_stride;
-    if (q.g_ns > 0) locate(t - q.g_cu, q.g_small, q.g_slot, q.g_ns, g_row, g_stride);
-    const int tile = locate(i, q.own_small, q.own_slot, q.own_ns, o_row, o_stride);
-    int own = q.own_ns;  // (a tile of fewer key tiles has fewer chunks)
-    if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq, min(a.tq, q.n - tile * a.tq), kBlockN));
-    const int total = q.g_ns + own;
-    const float* const g_o = q.g_small ? a.small_o : a.big_o;
-    const float* const g_l = q.g_small ? a.small_lse : a.big_lse;
-    const float* const o_o = q.own_small ? a.small_o : a.big_o;
-    const float* const o_l = q.own_small ? a.small_lse : a.big_lse;
-
-    constexpr int kBatch = 16;
     float mx = -INFINITY, tot = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < total; s0 += kBatch) {
-        float l[kBatch];
-        f32x4 v[kBatch];
+    if (row_ok) {
+        // row of this row's first partial, and the distance to the next chunk's
+        auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
+            const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
+            const int tile = (int)((unsigned)i / (unsigned)tq);
+            stride = (int64_t)a.num_kv_heads * bm;
+            first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
+            return tile;
+        };
+        int64_t g_row = 0, g_stride = 0, o_row, o_stride;
+        if (q.g_ns > 0) locate(t - q.g_cu, q.g_small, q.g_slot, q.g_ns, g_row, g_stride);
+        const int tile = locate(i, q.own_small, q.own_slot, q.own_ns, o_row, o_stride);
+        int own = q.own_ns;  // (a tile of fewer key tiles has fewer chunks)
+        if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq, min(a.tq, q.n - tile * a.tq), kBlockN));
+        const int total = q.g_ns + own;  // the shared chunks first
+        const float* const g_o = q.g_small ? a.small_o : a.big_o;
+        const float* const g_l = q.g_small ? a.small_lse : a.big_lse;
+        const float* const o_o = q.own_small ? a.small_o : a.big_o;
+        const float* const o_l = q.own_small ? a.small_lse : a.big_lse;
+
+        constexpr int kBatch = G > 1 ? 8 : 16;
+        for (int s0 = sub; s0 < total; s0 += kBatch * G) {
+            float l[kBatch];
+            f32x4 v[kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const int c = s0 + u;
-            l[u] = -INFINITY;
-            v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (c < total) {
-                const bool shared = c < q.g_ns;
-                const int64_t pr = shared ? g_row + c * g_stride : o_row + (c - q.g_ns) * o_stride;
-                l[u] = (shared ? g_l : o_l)[pr];
-                v[u] = *reinterpret_cast<const f32x4*>((shared ? g_o : o_o) + pr * D + 4 * c4);
+            for (int u = 0; u < kBatch; ++u) {
+                const int c = s0 + u * G;
+                l[u] = -INFINITY;
+                v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (c < total) {
+                    const bool shared = c < q.g_ns;
+                    const int64_t pr = shared ? g_row + c * g_stride : o_row + (c - q.g_ns) * o_stride;
+                    l[u] = (shared ? g_l : o_l)[pr];
+                    v[u] = *reinterpret_cast<const f32x4*>((shared ? g_o : o_o) + pr * D + 4 * c4);
+                }
+            }
+            float mn = mx;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, l[u]);
+            const float off = mn == -INFINITY ? 0.f : mn;
+            const float alpha = expf(mx - off);
+            tot *= alpha;
+            acc *= alpha;
+            mx = mn;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const float w = expf(l[u] - off);  // 0 for the padding entries
+                tot += w;
+                acc += w * v[u];
             }
         }
-        float mn = mx;
+    }
+    if constexpr (G > 1) {
+        s_acc[threadIdx.x] = acc;
+        if (c4 == 0) {
+            s_max[lane_row] = mx;
+            s_tot[lane_row] = tot;
+        }
+        __syncthreads();
+        if (sub != 0 || !row_ok) return;
+        const float mx0 = mx;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, l[u]);
-        const float off = mn == -INFINITY ? 0.f : mn;
-        const float alpha = expf(mx - off);
-        tot *= alpha;
-        acc *= alpha;
-        mx = mn;
+        for (int g = 1; g < G; ++g) mx = fmaxf(mx, s_max[lane_row + g]);
+        const float off = mx == -INFINITY ? 0.f : mx;
+        const float w0 = expf(mx0 - off);
+        tot *= w0;
+        acc *= w0;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const float w = expf(l[u] - off);  // 0 for the padding entries
-            tot += w;
-            acc += w * v[u];
+        for (int g = 1; g < G; ++g) {
+            const float w = expf(s_max[lane_row + g] - off);
+            tot += w * s_tot[lane_row + g];
+            acc += w * s_acc[threadIdx.x + g * CPR];
         }
     }
     // as in an unsplit item: weights that are all 0 give 0, a NaN sum gives NaN, both with lse -inf
@@ -141,13 +171,23 @@ hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, boo
     return hipGetLastError();
 }
 
-hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s) {
-    const int64_t rows = kCombineThreads / (head_dim / 4);
-    const dim3 grid((unsigned)ceil_div64(a.rows, rows));
-    if (head_dim == 128)
-        shared_merge_kernel<128><<<grid, kCombineThreads, 0, s>>>(a);
-    else
-        shared_merge_kernel<64><<<grid, kCombineThreads, 0, s>>>(a);
+hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s) {
+    // Eight thread groups a row where a trip of loads saved (16 chunks a trip, or 64) is worth the rows'
+    // additional workgroups (TODO).
+    const int trips_saved = ceil_div(max_chunks, 16) - ceil_div(max_chunks, 64);
+    const int groups = a.rows <= 1536LL * trips_saved ? 8 : 1;
+    const dim3 grid((unsigned)ceil_div64(a.rows, kCombineThreads / (head_dim / 4 * groups)));
+    if (head_dim == 128) {
+        if (groups > 1)
+            shared_merge_kernel<128, 8><<<grid, kCombineThreads, 0, s>>>(a);
+        else
+            shared_merge_kernel<128, 1><<<grid, kCombineThreads, 0, s>>>(a);
+    } else {
+        if (groups > 1)
+            shared_merge_kernel<64, 8><<<grid, kCombineThreads, 0, s>>>(a);
+        else
+            shared_merge_kernel<64, 1><<<grid, kCombineThreads, 0, s>>>(a);
+    }
     return hipGetLastError();
 }
 

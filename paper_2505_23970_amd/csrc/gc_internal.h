@@ -129,12 +129,18 @@ __host__ __device__ inline int quick_div(int a, int d) {
 #endif
 }
 
+constexpr int kTakeGroups = 512;  // (a batch of more groups takes all)
 struct SharedSizes {
     Divisor tq;    // new tokens per 128-row query tile
     Divisor chunk; // 64-key tiles per chunk of a 128-row tile
     Divisor run;   // places of one wavefront's run over the small tiles (PartWork)
     int tq_small;  // new tokens per 16-row query tile (0: no small tiles)
-    int always;    // share whatever it costs (gc_shared.policy)
+    int all;       // every group's shared keys are taken once; else those of the groups in `take`
+    uint64_t take[kTakeGroups / 64];
+    // shared keys that are taken once for group g, which shares S
+    __host__ __device__ int taken(int g, int S) const {
+        return all || (g < kTakeGroups && (take[g / 64] >> (g % 64) & 1)) ? S : 0;
+    }
 };
 
 // What one group or request adds to the launch. 128-row tiles: `tiles` query tiles of `ns` key chunks
@@ -147,15 +153,6 @@ struct PartWork {
     int keys, small, tiles, ns, kt;
 };
 constexpr int kPieceCost = 4;
-
-// Shared keys that are taken once for a group of `active` requests with `tokens` new tokens in all,
-// whose own query tiles of 128 rows number `own_tiles`: all S of them, or none where that saves nothing.
-__host__ __device__ inline int shared_taken(int S, int active, int tokens, int own_tiles, const SharedSizes& z) {
-    if (S <= 0 || active <= 0) return 0;
-    if (z.always) return S;
-    if (active < 2 || S < kBlockN) return 0;
-    return (int64_t)z.tq.ceil_of(tokens) * 10 <= (int64_t)own_tiles * 9 ? S : 0;
-}
 
 // A part of n new tokens against `keys` keys; at: its first place in the sequence.
 __host__ __device__ inline PartWork part_work(int keys, int n, int at, const SharedSizes& z) {
@@ -378,7 +375,8 @@ hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* sink, hipS
 hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
 hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool fp8, hipStream_t s);
-hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, hipStream_t s);
+// max_chunks: the most chunks of any row
+hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s);
 // max_splits: the most key chunks of any split query tile
 hipError_t launch_combine(const CombineArgs& a, int head_dim, int64_t num_combines, int max_splits, hipStream_t s);
 

@@ -1,9 +1,8 @@
 // Work lists of the shared-prefix attention, built on the device from the device copies of the lengths
 // (no host-to-device copy, so a plan can be enqueued freely and captured in a graph). One workgroup:
 //   1. the device lengths are checked before anything is derived from them;
-//   2. prefix sums over requests (requests with new tokens, own 128-row query tiles) give every group its
-//      rows and whether its shared keys are taken once; scans over groups and then requests give each
-//      its items and partial slots, and every request's record for the merge;
+//   2. scans over groups and then requests give each its items, partial slots and pieces, and every
+//      request its record for the merge (which groups' shared keys are taken once, the host says);
 //   3. every item, found from its index by a search of the scans.
 // What bounds it is the chain of these steps, each a barrier and some reads of what the one before wrote:
 // up to kPlanLdsBatch requests all of it stays in LDS.
@@ -75,11 +74,11 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int v) {
     return lo;
 }
 
-constexpr int kPlanArrays = 11;  // int32 per request of what the planner derives
+constexpr int kPlanArrays = 9;  // int32 per request of what the planner derives
 
 template <int BATCH>
 struct SharedPlanLds {
-    Quad tmp[3][kPlanThreads / 64];
+    Quad tmp[2][kPlanThreads / 64];
     int bad;
     int cu[BATCH + 1], pre[BATCH + 1], first[BATCH + 1], share[BATCH + 1];
     int derived[kPlanArrays][BATCH + 1];
@@ -101,16 +100,14 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         else return global;
     };
     int* const group_of = derived(0);  // [B]
-    int* const active = derived(1);    // [B + 1] requests with new tokens before this one
-    int* const tiles = derived(2);     // [B + 1] 128-row tiles before it
-    int* const r_big = derived(3);     // [B] own 128-row items before it (after all shared ones)
-    int* const r_slot = derived(4);    // [B] its first partial slot, of 128 rows
-    int* const r_piece = derived(5);   // [B] number of its first piece, if it were small
-    int* const r_at = derived(6);      // [B] its first place, if it were small
-    int* const g_big = derived(7);     // [G] the same of the groups' shared parts
-    int* const g_piece = derived(8);
-    int* const g_at = derived(9);
-    int* const g_taken = derived(10);  // [G] shared keys that are taken once
+    int* const r_big = derived(1);     // [B] own 128-row items before it (after all shared ones)
+    int* const r_slot = derived(2);    // [B] its first partial slot, of 128 rows
+    int* const r_piece = derived(3);   // [B] number of its first piece, if it were small
+    int* const r_at = derived(4);      // [B] its first place, if it were small
+    int* const g_big = derived(5);     // [G] the same of the groups' shared parts
+    int* const g_piece = derived(6);
+    int* const g_at = derived(7);
+    int* const g_taken = derived(8);   // [G] shared keys that are taken once
     if (tid == 0) sm.bad = 0;
     if constexpr (LDS) {  // (G <= B)
 #pragma nounroll
@@ -155,39 +152,9 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     __syncthreads();
     if (sm.bad) return empty_all();
 
-    // 2. prefix sums over requests. (A thread owns consecutive requests, and groups below.)
+    // 2. (A thread owns consecutive requests, and groups.)
     const int per = ceil_div(B, kPlanThreads), r0 = min(B, tid * per), r1 = min(B, r0 + per);
     const int per_g = ceil_div(G, kPlanThreads), g0 = min(G, tid * per_g), g1 = min(G, g0 + per_g);
-    {
-        Quad v{{0, 0, 0, 0}}, total{{0, 0, 0, 0}};
-        bool bad = false;
-#pragma nounroll
-        for (int r = r0; r < r1; ++r) {
-            const int g = last_at_most(first, G, r), n = cu[r + 1] - cu[r];
-            group_of[r] = g;
-            bad |= pre[r] < share[g];
-            v.x[0] += n > 0;
-            v.x[1] += z.tq.ceil_of(n);
-        }
-        if (bad) sm.bad = 1;
-        Quad at = block_scan4(v, sm.tmp[0], total);
-#pragma nounroll
-        for (int r = r0; r < r1; ++r) {
-            const int n = cu[r + 1] - cu[r];
-            active[r] = at.x[0];
-            tiles[r] = at.x[1];
-            at.x[0] += n > 0;
-            at.x[1] += z.tq.ceil_of(n);
-        }
-        if (tid == 0) {
-            active[B] = total.x[0];
-            tiles[B] = total.x[1];
-        }
-    }
-    __threadfence_block();
-    __syncthreads();
-    if (sm.bad) return empty_all();
-
     auto tokens_of = [&](int g) { return cu[first[g + 1]] - cu[first[g]]; };
 
     //    groups: what each shares, its items, slots and pieces
@@ -196,12 +163,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         Quad v{{0, 0, 0, 0}};
 #pragma nounroll
         for (int g = g0; g < g1; ++g) {
-            const int ra = first[g], rb = first[g + 1], tokens = cu[rb] - cu[ra];
-            const int S = shared_taken(share[g], active[rb] - active[ra], tokens, tiles[rb] - tiles[ra], z);
+            const int S = z.taken(g, share[g]);
             g_taken[g] = S;
-            add_part(v, part_work(S, tokens, 0, z), true);
+            add_part(v, part_work(S, tokens_of(g), 0, z), true);
         }
-        Quad at = block_scan4(v, sm.tmp[1], total);
+        Quad at = block_scan4(v, sm.tmp[0], total);
 #pragma nounroll
         for (int g = g0; g < g1; ++g) {
             g_big[g] = at.x[kBigItems];  // (and its first slot: every shared item has one)
@@ -221,11 +187,13 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         Quad v{{0, 0, 0, 0}};
 #pragma nounroll
         for (int r = r0; r < r1; ++r) {
-            const int S = g_taken[group_of[r]];
+            const int g = last_at_most(first, G, r), S = g_taken[g];
+            group_of[r] = g;
+            if (pre[r] < share[g]) sm.bad = 1;
             const PartWork w = part_work(pre[r] - S + cu[r + 1] - cu[r], cu[r + 1] - cu[r], 0, z);
             add_part(v, w, S > 0 || w.ns > 1);
         }
-        Quad at = block_scan4(v, sm.tmp[2], total);
+        Quad at = block_scan4(v, sm.tmp[1], total);
 #pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int g = group_of[r], S = g_taken[g], n = cu[r + 1] - cu[r];
@@ -252,7 +220,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             add_part(at, w, q.merge);
         }
     }
-    if (total.x[kBigItems] != a.expect_big || total.x[kBigSlots] != a.expect_big_slots || total.x[kParts] != a.expect_parts ||
+    if (sm.bad || total.x[kBigItems] != a.expect_big || total.x[kBigSlots] != a.expect_big_slots || total.x[kParts] != a.expect_parts ||
         total.x[kPlaces] != a.expect_places)
         return empty_all();
     __threadfence_block();
