@@ -856,13 +856,14 @@ struct SharedLoad {
         int tiles, kt;
     } part[kKept];
     int parts = 0, longest = 1;
-    int64_t units = 0, steps = 0, places = 0;  // 128-row tiles, their key tiles
+    int64_t units = 0, steps = 0, places = 0, small_tiles = 0;  // 128-row tiles, their key tiles; small key tiles
 };
 
 void shared_load(const gc_batch* b, const gc_shared* s, const gc::SharedSizes& z, SharedLoad* l) {
     for_each_part(b, s, z, [&](const gc::PartWork& w, bool, bool) {
         if (w.small) {
             l->places += gc::kPieceCost + w.kt;
+            l->small_tiles += w.kt;
         } else if (w.tiles > 0) {
             l->units += w.tiles;
             l->steps += (int64_t)w.tiles * w.kt;
@@ -882,6 +883,9 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     shared_load(b, s, *z, &l);
     int64_t slots = geo->head_dim == 128 ? cus : 2 * cus, big = 0;
     if (l.units * heads > slots) slots = 2 * cus;
+    // reading the small tiles takes longer than the 128-row ones
+    const double small_us = l.small_tiles * heads * (double)(gc::kDecN * geo->head_dim * 2 * (pk.fp8 ? 1 : 2)) / 5.6e6;
+    const bool by_load = small_us > l.steps * heads * 1.4 / cus;
     auto fits = [&](int c) {
         z->chunk = gc::divisor(c);
         big = 0;
@@ -897,7 +901,7 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
             for_each_part(b, s, *z, [&](const gc::PartWork& w, bool, bool) {
                 if (!w.small && w.tiles > 0) count(w.tiles, w.kt);
             });
-        return (l.steps + big * kItemSteps) * heads <= slots * (c + kItemSteps) && most * heads <= slots;
+        return (l.steps + big * kItemSteps) * heads <= slots * (c + kItemSteps) && (by_load || most * heads <= slots);
     };
     int lo = kMinChunk < l.longest ? kMinChunk : l.longest, hi = l.longest;
     while (lo < hi) {
@@ -909,7 +913,8 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     int64_t wgs = 2 * cus - big * heads;
     if (wgs < cus) wgs = cus;
     const int64_t waves = gc::shared_rings(pk.fp8) * wgs;
-    const int64_t run = waves >= heads ? gc::ceil_div64(l.places, waves / heads) : gc::ceil_div64(l.places * heads, waves);
+    int64_t run = waves >= heads ? gc::ceil_div64(l.places, waves / heads) : gc::ceil_div64(l.places * heads, waves);
+    if (by_load && big > 0) run = run * 2 / 3;
     z->run = gc::divisor(run > kMinRun ? (int)run : kMinRun);
 }
 

@@ -19,6 +19,15 @@
 //     partners), holds the eight (cos, sin) of its token in registers and goes through the heads, so it may
 //     write q_out over q. Pages with few new tokens (decode) put their threads on heads instead.
 // What bounds it: memory for prompts; for decode the chain lengths -> block id, rows and table -> stores.
+//   - Prompts: the workgroups of a page (its KV heads, its query heads) are launched side by side, on all
+//     XCDs, so that a token's projections are read in one sweep (30000 tokens of the 70B heads 243 us, page
+//     after page for each head 277, pages dealt to the XCDs 273). Decode batches, a token a page, are launched
+//     head by head: the workgroups of a page then share an XCD's L2 (96 tokens 5.0 us, 5.6 the other way).
+//   - q_out is written around the caches' retention (non-temporal): 1290 MB 231 us (243), 359 MB 61 (74), 46 MB
+//     9.8 (10.8). The queries are read that way as well where they exceed what the last-level cache keeps from one
+//     pass to the next: from 192 MB of them on (1290 MB 210 us against 231, 550 MB 94 / 99; but 359 MB 66 / 61,
+//     183 MB at d = 64 41 / 32).
+// At 1290 MB it moves 6.1 TB/s; a copy of as many bytes by the framework's tensor library 5.3.
 #include "append_body.h"
 
 namespace gc {
@@ -151,7 +160,7 @@ __device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm
 }
 
 // kRotQHeads query heads (group qg) of the tokens of one page.
-template <int D>
+template <int D, bool STREAM>
 __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int qg) {
     constexpr int U = D / 16;  // pairs of chunks per head
     constexpr int kBatch = 4;  // heads whose loads a thread keeps in flight
@@ -180,8 +189,10 @@ __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& a
         for (int b = 0; b < kBatch; ++b) {
             const int h = h0 + b * step;
             if (h < h_end) {
-                w0[b] = *reinterpret_cast<const u32x4*>(src + h * D + 8 * c0);
-                w1[b] = *reinterpret_cast<const u32x4*>(src + h * D + 8 * c1);
+                const u32x4* const p0 = reinterpret_cast<const u32x4*>(src + h * D + 8 * c0);
+                const u32x4* const p1 = reinterpret_cast<const u32x4*>(src + h * D + 8 * c1);
+                w0[b] = STREAM ? __builtin_nontemporal_load(p0) : *p0;
+                w1[b] = STREAM ? __builtin_nontemporal_load(p1) : *p1;
             }
         }
 #pragma unroll
@@ -206,18 +217,20 @@ __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& a
                 w0[b] = pack8(x);
                 w1[b] = pack8(y);
             }
-            *reinterpret_cast<u32x4*>(dst + h * D + 8 * c0) = w0[b];
-            *reinterpret_cast<u32x4*>(dst + h * D + 8 * c1) = w1[b];
+            __builtin_nontemporal_store(w0[b], reinterpret_cast<u32x4*>(dst + h * D + 8 * c0));
+            __builtin_nontemporal_store(w1[b], reinterpret_cast<u32x4*>(dst + h * D + 8 * c1));
         }
     }
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool STREAM>
 __global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(const RotaryArgs ra) {
     __shared__ AppendLds<D> lds;
     const AppendArgs& a = ra.a;
-    const int u = (int)(blockIdx.x % (unsigned)a.total_pages);
-    const int job = (int)(blockIdx.x / (unsigned)a.total_pages);
+    // blockIdx.x = page jobs + job, or job pages + page
+    const unsigned inner = ra.by_page ? ra.jobs : (unsigned)a.total_pages;
+    const unsigned hi = blockIdx.x / inner, lo = blockIdx.x - hi * inner;
+    const int u = (int)(ra.by_page ? hi : lo), job = (int)(ra.by_page ? lo : hi);
     PageUnit at;
     if (!locate_page<D>(a, lds, u, (int)gridDim.x, at)) return;
     const int lp = at.P / kPage + at.k;
@@ -228,7 +241,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(const Rot
     if (job < kv_jobs)
         rotary_kv<D, FP8>(ra, lds, at, lp, s0, s1, job);
     else
-        rotary_q<D>(ra, at, lp, s0, s1, job - kv_jobs);
+        rotary_q<D, STREAM>(ra, at, lp, s0, s1, job - kv_jobs);
 }
 
 }  // namespace
@@ -237,20 +250,26 @@ int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int 
     return pages * (ceil_div(num_kv_heads, append_heads(head_dim)) + (with_q ? ceil_div(num_q_heads, kRotQHeads) : 0));
 }
 
-hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, bool fp8, hipStream_t s) {
+template <int D, bool FP8>
+static void launch_rotary(const RotaryArgs& ra, bool stream, unsigned grid, hipStream_t s) {
+    if (stream)
+        append_rotary_kernel<D, FP8, true><<<grid, kAppendThreads, 0, s>>>(ra);
+    else
+        append_rotary_kernel<D, FP8, false><<<grid, kAppendThreads, 0, s>>>(ra);
+}
+
+hipError_t launch_append_rotary(const RotaryArgs& args, int head_dim, bool fp8, hipStream_t s) {
+    RotaryArgs ra = args;
     if (ra.a.total_pages <= 0) return hipSuccess;
-    const dim3 grid((unsigned)rotary_workgroups(ra.a.total_pages, ra.num_q_heads, ra.a.num_kv_heads, head_dim, ra.q != nullptr));
-    if (fp8) {
-        if (head_dim == 128)
-            append_rotary_kernel<128, true><<<grid, kAppendThreads, 0, s>>>(ra);
-        else
-            append_rotary_kernel<64, true><<<grid, kAppendThreads, 0, s>>>(ra);
-    } else {
-        if (head_dim == 128)
-            append_rotary_kernel<128, false><<<grid, kAppendThreads, 0, s>>>(ra);
-        else
-            append_rotary_kernel<64, false><<<grid, kAppendThreads, 0, s>>>(ra);
-    }
+    const bool with_q = ra.q != nullptr;
+    ra.jobs = (unsigned)rotary_workgroups(1, ra.num_q_heads, ra.a.num_kv_heads, head_dim, with_q);
+    ra.by_page = ra.a.total_tokens >= 2LL * ra.a.total_pages;
+    const bool stream = with_q && (int64_t)ra.a.total_tokens * ra.num_q_heads * head_dim * 2 >= (192LL << 20);
+    const unsigned grid = ra.jobs * (unsigned)ra.a.total_pages;
+    if (head_dim == 128)
+        fp8 ? launch_rotary<128, true>(ra, stream, grid, s) : launch_rotary<128, false>(ra, stream, grid, s);
+    else
+        fp8 ? launch_rotary<64, true>(ra, stream, grid, s) : launch_rotary<64, false>(ra, stream, grid, s);
     return hipGetLastError();
 }
 

@@ -259,6 +259,7 @@ struct RotaryArgs {
     const float* table;     // [num_positions][rotary_dim / 2][cos, sin]
     int64_t q_stride, k_stride, v_stride;
     int32_t num_q_heads, num_positions, rotary_dim, interleaved;
+    uint32_t jobs, by_page;  // workgroups of a page; launched page by page (else head by head)
 };
 
 struct PlanArgs {

@@ -174,6 +174,39 @@ def test_far_positions_follow_the_angles_in_64_bits():
     assert np.all(np.abs(H.from_dev_f32(got) - y) <= RR.bf16_bound(y, mag) + 2.0 ** -24 * (x + np.roll(x, 32, axis=-1)))
 
 
+@pytest.mark.parametrize("interleaved", [False, True], ids=["halves", "interleaved"])
+def test_prompts_beyond_the_cache(interleaved):
+    """Enough query bytes that they are read past the caches: 12300 tokens of 64 heads. Rows sampled."""
+    import torch
+    import paper_2505_23970_amd as gc
+    P, n = [5, 700, 0], [6001, 3, 6296]
+    T, Hq, D = sum(n), 64, 128
+    assert T * Hq * D * 2 >= 192 << 20
+    pages = [-(-(p + m) // 16) for p, m in zip(P, n)]
+    tables = np.zeros((3, max(pages)), np.int32)
+    order = np.random.default_rng(3).permutation(sum(pages)).astype(np.int32)
+    for r, k in enumerate(pages):
+        tables[r, :k], order = order[:k], order[k:]
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    qkv = torch.randn((T, Hq + 2, D), generator=gen, device="cuda", dtype=torch.bfloat16)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + 1], qkv[:, Hq + 1:]
+    kp = torch.zeros((sum(pages), 1, 16, D), dtype=torch.bfloat16, device="cuda")
+    vp = torch.zeros((sum(pages), 1, D, 16), dtype=torch.bfloat16, device="cuda")
+    table = random_table(6400, 96, 12)
+    got = gc.kv_append_rotary(q, k, v, kp, vp, gc.PagedBatch(P, n, tables), H_table(table), interleaved=interleaved)
+    pos = RR.positions_of(P, n)
+    rows = np.unique(np.concatenate([np.arange(40), np.arange(5990, 6020), np.arange(T - 40, T),
+                                     np.random.default_rng(5).integers(0, T, 300)]))
+    dev = torch.from_numpy(rows).cuda()
+    y, mag = RR.rotate(q[dev].double().cpu().numpy(), pos[rows], table, interleaved)
+    assert np.all(np.abs(got[dev].double().cpu().numpy() - y) <= RR.bf16_bound(y, mag))
+    y, mag = RR.rotate(k.double().cpu().numpy(), pos, table, interleaved)
+    at = np.concatenate([tables[r][np.arange(P[r], P[r] + n[r]) // 16] for r in range(3)]).astype(np.int64)
+    at, slot = torch.from_numpy(at).cuda(), torch.from_numpy(pos % 16).cuda()
+    assert np.all(np.abs(kp[at, :, slot].double().cpu().numpy() - y) <= RR.bf16_bound(y, mag))
+    assert torch.equal(vp[at, :, :, slot].view(torch.int16), v.contiguous().view(torch.int16))
+
+
 def test_bad_pages_and_nothing_new():
     """Ids outside the pool: nothing is written for those pages, the queries are rotated all the same."""
     import torch
