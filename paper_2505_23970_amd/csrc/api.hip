@@ -808,9 +808,13 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
 // at about 20 TB/s over all heads, its 128-row tiles at the matrix cores' pace; taken once, they cost a read
 // from HBM or the pace of the group's own 128-row tiles, and every row two fp32 partial rows, written and
 // read. Paces: us of a compute unit per 128-row tile and 64 keys (48 requests of 20 tokens on 32768 shared ones, the
-// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 1075; at d = 64 533 / 288 and 665 / 341). On 60
-// drawn batches the choice is within TODO of the better of the two.
+// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 1075; at d = 64 533 / 288 and 665 / 341).
+// Short launches of 128-row tiles are bound by their latency, which the finer chunks here make shorter: up to 64
+// tiles over all heads and 4096 of their key tiles, groups of 256 shared keys or more are taken (16.0 us / 13.2
+// for two requests of 3 tokens on 513, 18.8 / 15.5 for 27 on 796, 21.7 / 17.9 for 7 of 19 tokens; at 16384 key
+// tiles 117 / 128).
 constexpr double kShareGain = 2.0, kShareGainTiles = 6.0;  // us: batches of small tiles; with 128-row own parts
+constexpr int kShortTiles = 64, kShortSteps = 4096, kShortKeys = 256;
 
 void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
     z->all = s->policy == GC_SHARE_ALWAYS || s->groups > gc::kTakeGroups;
@@ -822,9 +826,10 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
     const double shared_pace = D == 128 ? (pk.fp8 ? 1.12 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
     double gain = 0;
     bool any_tiles = false;
+    double all_tiles = 0, all_steps = 0;  // of all requests, over all heads
+    uint64_t brief[gc::kTakeGroups / 64] = {};
     for (int g = 0; g < s->groups; ++g) {
         const int S = s->shared_lens_host[g];
-        if (S <= 0) continue;
         int64_t small = 0, tiles = 0, tokens = 0;
         for (int r = s->group_first_host[g]; r < s->group_first_host[g + 1]; ++r) {
             const int n = b->new_lens_host[r];
@@ -832,6 +837,10 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
             if (n > z->tq_small) tiles += z->tq.ceil_of(n);
             else small += n > 0;
         }
+        all_tiles += tiles * heads;
+        all_steps += tiles * heads * S / gc::kBlockN;
+        if (S <= 0) continue;
+        if (tiles >= 2 && S >= kShortKeys) brief[g / 64] |= 1ull << (g % 64);
         const double plain = S * (small * key_bytes / 20e6 + tiles * step * plain_pace);
         const double read = key_bytes / 5.6e6;
         const double paced = tokens <= z->tq_small ? 0 : gc::ceil_div64(tokens, z->tq.d) * step * shared_pace;
@@ -844,6 +853,8 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
     }
     if (gain < (any_tiles ? kShareGainTiles : kShareGain))
         for (uint64_t& t : z->take) t = 0;
+    if (all_tiles <= kShortTiles && all_steps <= kShortSteps)
+        for (int i = 0; i < gc::kTakeGroups / 64; ++i) z->take[i] |= brief[i];
 }
 
 // Tiles and chunks of the key axis. TODO(rule text)
@@ -914,7 +925,7 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     if (wgs < cus) wgs = cus;
     const int64_t waves = gc::shared_rings(pk.fp8) * wgs;
     int64_t run = waves >= heads ? gc::ceil_div64(l.places, waves / heads) : gc::ceil_div64(l.places * heads, waves);
-    if (by_load && big > 0) run = run * 2 / 3;
+    if (big * heads > cus) run = run * 2 / 3;
     z->run = gc::divisor(run > kMinRun ? (int)run : kMinRun);
 }
 
