@@ -857,7 +857,19 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
         for (int i = 0; i < gc::kTakeGroups / 64; ++i) z->take[i] |= brief[i];
 }
 
-// Tiles and chunks of the key axis. TODO(rule text)
+// Chunks of the key axis.
+//   - 128-row tiles at d = 128: one workgroup a compute unit, whose other half runs small tiles; alone, two would be
+//     8 % faster and write twice the partial rows (64 answers on 8192 shared tokens and hardly any of their own:
+//     33 us with 256 items, 36 with 512; 37 with 192). At d = 64 two (24 questions of 20 tokens on 4000: 40 us with
+//     360 and 480 shared items, 48 with 240). So the smallest chunk whose items make a whole number of such
+//     rounds: an item longer than two thirds of the chunk fills a slot, and all of them the slots by their
+//     key tiles and kItemSteps more each. Where reading the small tiles takes longer than that, the load alone
+//     decides (128 answers on 16k-token contexts: 304 items of 45 key tiles 132 us, 240 of 60 143).
+//   - At least kMinChunk key tiles (16 answers of the 8B model on 2000 tokens: 16.4 us with 4, 15.8 with 3, 16.6 with
+//     2, 17.4 with 6, 20.4 with 8).
+//   - Small tiles: equal runs, one for each of the wavefronts that the remaining workgroup slots hold, of at least
+//     kMinRun places. Where some units hold two 128-row workgroups, two thirds of that, because the rest of
+//     the small workgroups follow when the first end (132 us; 145 with whole runs).
 constexpr int kMinChunk = 4, kMinRun = 8, kItemSteps = 4;
 
 // The batch's work: 128-row parts (the first kKept of them kept) and the places of the small ones.
@@ -1082,11 +1094,10 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     m.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
     m.rows = sh.total_tokens * geo->num_q_heads;
     m.batch = b->batch;
-    m.num_q_heads = geo->num_q_heads;
     m.num_kv_heads = geo->num_kv_heads;
-    m.group = sh.group;
-    m.tq = spl.z.tq.d;
-    m.tq_small = spl.z.tq_small;
+    m.hq = gc::divisor(geo->num_q_heads);
+    m.group = gc::divisor(sh.group);
+    m.tq = spl.z.tq;
     return gc::launch_shared_merge(m, geo->head_dim, spl.max_shared + spl.max_own, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 

@@ -12,7 +12,15 @@
 // Work. Three launches: plan (once a batch), items, merge. One launch runs both kinds of items, so that
 // they overlap: 128-row items (64-key tiles through LDS; the shared parts, and own parts of many new
 // tokens), bound by the matrix cores and the softmax, and small items (one wavefront, 16 rows; own parts
-// of single tokens), bound by reading K and V. Workgroups of the two kinds are mixed evenly.
+// of single tokens), bound by reading K and V. A compute unit holds two workgroups, and the hardware
+// deals them out in index order, unit after unit: the 128-row ones come first, so that each gets a unit's one
+// half and small ones the other (mixed evenly instead, some units get two 128-row workgroups and others
+// none: 64 answers on 8192 shared tokens of the 70B heads, 400 of their own, 46 us, so 38).
+// What bounds it there, per launch: 256 128-row items of 16 key tiles take 26 us alone (1.4 us a tile; 1.0
+// with half the units at work, and a sixth less on zeros, so part of it is the power limit), the small items'
+// 126 MB 26 us at 4.9 TB/s; together 29 us where the pools are in the last-level cache (162 MB at 5.6 TB/s take
+// 29) and 47 where they come from HBM, where the two slow each other down: the 128-row items load each key
+// tile once per query tile, 134 MB through the same path as the small ones' 126.
 #include "attention_kernels.h"
 
 namespace gc {
@@ -41,7 +49,8 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     const int sub = lane_row % G;
     const int64_t row = (int64_t)blockIdx.x * kRows + lane_row / G;
     const bool in_range = row < a.rows;
-    const int t = (int)((in_range ? row : a.rows - 1) / a.num_q_heads);
+    const int64_t row_or_last = in_range ? row : a.rows - 1;
+    const int t = a.rows <= UINT32_MAX ? a.hq.of((uint32_t)row_or_last) : (int)(row_or_last / a.hq.d);
     // the request of the wavefront's first row: the last r with cu[r] <= t0
     const int t0 = __builtin_amdgcn_readfirstlane(t);
     int lo = 0, hi = a.batch;  // cu[lo] <= t0 < cu[hi]
@@ -58,25 +67,24 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     const int i = t - q.cu;
     const bool row_ok = status == 0 && in_range && q.merge && i >= 0 && i < q.n;
     if (G == 1 && !row_ok) return;
-    const int h = (int)(row - (int64_t)t * a.num_q_heads);
-    const int kvh = (int)((unsigned)h / (unsigned)a.group), hl = h - kvh * a.group;
+    const int h = (int)(row_or_last - (int64_t)t * a.hq.d);
+    const int kvh = a.group.of((uint32_t)h), hl = h - kvh * a.group.d;
 
     float mx = -INFINITY, tot = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (row_ok) {
         // row of this row's first partial, and the distance to the next chunk's
         auto locate = [&](int i, bool small, int slot, int ns, int64_t& first, int64_t& stride) -> int {
-            const int tq = small ? a.tq_small : a.tq, bm = small ? kDecM : kBlockM;
-            const int tile = (int)((unsigned)i / (unsigned)tq);
+            const int tile = small ? 0 : a.tq.of((uint32_t)i), bm = small ? kDecM : kBlockM;  // (a small part is one tile)
             stride = (int64_t)a.num_kv_heads * bm;
-            first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * tq) * a.group + hl;
+            first = ((int64_t)(slot + tile * ns) * a.num_kv_heads + kvh) * bm + (i - tile * a.tq.d) * a.group.d + hl;
             return tile;
         };
         int64_t g_row = 0, g_stride = 0, o_row, o_stride;
         if (q.g_ns > 0) locate(t - q.g_cu, q.g_small, q.g_slot, q.g_ns, g_row, g_stride);
         const int tile = locate(i, q.own_small, q.own_slot, q.own_ns, o_row, o_stride);
         int own = q.own_ns;  // (a tile of fewer key tiles has fewer chunks)
-        if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq, min(a.tq, q.n - tile * a.tq), kBlockN));
+        if (!q.own_small) own = min(own, key_tiles(q.P, tile * a.tq.d, min(a.tq.d, q.n - tile * a.tq.d), kBlockN));
         const int total = q.g_ns + own;  // the shared chunks first
         const float* const g_o = q.g_small ? a.small_o : a.big_o;
         const float* const g_l = q.g_small ? a.small_lse : a.big_lse;
@@ -172,8 +180,9 @@ hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, boo
 }
 
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s) {
-    // Eight thread groups a row where a trip of loads saved (16 chunks a trip, or 64) is worth the rows'
-    // additional workgroups (TODO).
+    // Eight thread groups a row where the trips of loads saved (16 chunks a trip, or 64) are worth the rows'
+    // additional workgroups. One group / eight, attention and merge: 64 rows of 131 chunks 32.3 us / 18.5, 512 of
+    // 38 20.2 / 17.0, 1200 of 28 22.6 / 22.3, 1600 of 25 23.9 / 25.1, 4096 of 12 53.7 / 57.7.
     const int trips_saved = ceil_div(max_chunks, 16) - ceil_div(max_chunks, 64);
     const int groups = a.rows <= 1536LL * trips_saved ? 8 : 1;
     const dim3 grid((unsigned)ceil_div64(a.rows, kCombineThreads / (head_dim / 4 * groups)));

@@ -341,7 +341,8 @@ struct SharedMergeArgs {
     const int32_t* status;
     const SharedReq* reqs;
     int64_t rows;  // T * Hq
-    int32_t batch, num_q_heads, num_kv_heads, group, tq, tq_small;
+    int32_t batch, num_kv_heads;
+    Divisor hq, group, tq;  // query heads; of a KV head; new tokens of a 128-row tile
 };
 
 struct CombineArgs {
