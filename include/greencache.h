@@ -343,7 +343,8 @@ typedef struct gc_shared {
  * As gc_prefix_prefill_workspace_size / _plan / _run / _attention (= plan + run) and their
  * 8-bit forms, over groups. Plans and workspaces are of their own kind (a plan made by
  * gc_shared_prefix_plan is run by gc_shared_prefix_run with the same batch, groups and
- * options), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1); gc_prefix_prefill_plan_status
+ * options; a run that takes groups once and finds no such plan in its workspace enqueues kernels
+ * that write nothing), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1); gc_prefix_prefill_plan_status
  * serves them too, and covers the groups' device arrays. Options: tiling GC_TILES_AUTO only
  * (else GC_ERR_UNSUPPORTED); kv_split_tiles > 0 cuts 128-row tiles into chunks of that many 64-key
  * tiles, and the small tiles of successive requests into runs of that many 32-key tiles, < 0 leaves

@@ -1023,6 +1023,21 @@ gc_status check_shared_workspace(const SharedPlan& spl, const Plan& pl, const vo
     return ws == nullptr || bytes < spl.layout.total ? GC_ERR_WORKSPACE : GC_OK;
 }
 
+// What a plan is made for: a run finds the plan's mark in the workspace or does nothing, so that a workspace
+// with another plan, or none, is no list of garbage items.
+uint64_t shared_mark(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh, const SharedPlan& p) {
+    uint64_t x = 0xcbf29ce484222325ull;
+    auto add = [&](int64_t v) { x = (x ^ (uint64_t)v) * 0x100000001b3ull ^ (x >> 29); };
+    for (int64_t v : {(int64_t)geo->num_q_heads, (int64_t)geo->num_kv_heads, (int64_t)geo->head_dim,
+                      (int64_t)geo->max_blocks_per_seq, (int64_t)b->batch, (int64_t)s->groups, sh.total_tokens, p.big,
+                      p.big_shared, p.big_slots, p.parts, p.places, p.pieces, p.runs, (int64_t)p.z.chunk.d,
+                      (int64_t)p.z.run.d, (int64_t)p.layout.total})
+        add(v);
+    for (uint64_t t : p.z.take) add((int64_t)t);
+    add(p.z.all);
+    return x;
+}
+
 gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh,
                               const SharedPlan& spl, void* ws, hipStream_t stream) {
     gc::SharedPlanArgs a{};
@@ -1031,6 +1046,8 @@ gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const g
     a.group_first = s->group_first_dev;
     a.shared_lens = s->shared_lens_dev;
     a.status = at<int32_t>(ws, gc::kStatusOffset);
+    a.plan_mark = at<uint64_t>(ws, gc::kMarkOffset);
+    a.mark = shared_mark(geo, b, s, sh, spl);
     a.scratch = at<int32_t>(ws, spl.layout.scratch_off);
     a.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
     a.big_items = at<gc::SharedItem>(ws, spl.layout.big_off);
@@ -1050,7 +1067,7 @@ gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const g
     return gc::launch_shared_plan(a, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
-gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh, const SharedPlan& spl,
+gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh, const SharedPlan& spl,
                              const void* q, const void* k_pool, const void* v_pool, float scale, void* out, float* lse,
                              void* ws, hipStream_t stream, const PoolKind& pk) {
     gc::SharedAttnArgs a{};
@@ -1081,6 +1098,8 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     a.runs = at<int32_t>(ws, spl.layout.runs_off);
     a.small = (int32_t)(spl.runs * geo->num_kv_heads);
     a.pieces = (int32_t)spl.pieces;
+    a.plan_mark = at<uint64_t>(ws, gc::kMarkOffset);
+    a.mark = shared_mark(geo, b, s, sh, spl);
     if (gc::launch_attention_shared(a, geo->head_dim, pk.fp8, stream) != hipSuccess) return GC_ERR_HIP;
     gc::SharedMergeArgs m{};
     m.out = a.out;
@@ -1091,6 +1110,8 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Sh
     m.small_lse = a.small_lse;
     m.cu_new_lens = b->cu_new_lens_dev;
     m.status = at<int32_t>(ws, gc::kStatusOffset);
+    m.plan_mark = a.plan_mark;
+    m.mark = a.mark;
     m.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
     m.rows = sh.total_tokens * geo->num_q_heads;
     m.batch = b->batch;
@@ -1123,7 +1144,7 @@ gc_status run_shared(const gc_geometry* geo, const gc_batch* batch, const gc_sha
                      : enqueue_plan(geo, batch, sh, pl, workspace, stream);
         if (st != GC_OK) return st;
     }
-    return spl.any ? enqueue_shared_run(geo, batch, sh, spl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk)
+    return spl.any ? enqueue_shared_run(geo, batch, shared, sh, spl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk)
                    : enqueue_run(geo, batch, sh, pl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk);
 }
 

@@ -42,7 +42,8 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     constexpr int kRows = kCombineThreads / (CPR * G);  // rows per workgroup
     __shared__ f32x4 s_acc[G > 1 ? kCombineThreads : 1];
     __shared__ float s_max[G > 1 ? kCombineThreads / CPR : 1], s_tot[G > 1 ? kCombineThreads / CPR : 1];
-    const int status = a.status[0];  // (looked at below, so that the search does not wait for it)
+    // (looked at below, so that the search does not wait for them)
+    const bool planned = a.status[0] == 0 && *a.plan_mark == a.mark;
     const int lane = threadIdx.x & 63;
     const int c4 = (int)threadIdx.x % CPR;
     const int lane_row = (int)threadIdx.x / CPR;  // (row, group) of this thread
@@ -63,9 +64,9 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     }
     int r = lo;
     SharedReq q = a.reqs[r];
-    while (t >= q.cu + q.n && r + 1 < a.batch) q = a.reqs[++r];  // (later rows of the wavefront)
+    while (planned && t >= q.cu + q.n && r + 1 < a.batch) q = a.reqs[++r];  // (later rows of the wavefront)
     const int i = t - q.cu;
-    const bool row_ok = status == 0 && in_range && q.merge && i >= 0 && i < q.n;
+    const bool row_ok = planned && in_range && q.merge && i >= 0 && i < q.n;
     if (G == 1 && !row_ok) return;
     const int h = (int)(row_or_last - (int64_t)t * a.hq.d);
     const int kvh = a.group.of((uint32_t)h), hl = h - kvh * a.group.d;

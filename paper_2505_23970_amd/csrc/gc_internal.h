@@ -204,6 +204,8 @@ inline int64_t append_pages_host(const int32_t* prefix, const int32_t* n, int ba
 
 // ---------------------------------------------------------------- workspace
 constexpr size_t kStatusOffset = 0;  // byte offset of the planner's status word in the workspace
+// A shared-prefix plan's mark in that block: a hash of what the plan was made for.
+constexpr size_t kMarkOffset = 128;
 // Work queues of the resident attention launch: kQueues ticket counters and one exit
 // counter (int32) in the workspace's leading 256-byte block, zeroed by the planner and
 // left at zero by every launch that uses them.
@@ -314,6 +316,8 @@ struct SharedAttnArgs : AttnArgs {  // items: the 128-row items
     int32_t shared_items, own_items;      // 128-row items of either kind, the shared ones first
     int32_t shared_per_xcd, big_wgs;      // workgroups of the shared ones on an XCD; of both kinds
     int32_t small, pieces;          // runs times KV heads; pieces
+    const uint64_t* plan_mark;      // what the plan was made for, in the workspace: not `mark`, no work
+    uint64_t mark;
 };
 
 struct SharedPlanArgs {
@@ -322,6 +326,8 @@ struct SharedPlanArgs {
     const int32_t* group_first;   // [groups + 1]
     const int32_t* shared_lens;   // [groups]
     int32_t* status;
+    uint64_t* plan_mark;          // receives `mark`
+    uint64_t mark;
     int32_t* scratch;             // shared_scratch_ints(batch)
     SharedReq* reqs;
     SharedItem* big_items;
@@ -339,6 +345,8 @@ struct SharedMergeArgs {
     const float *big_o, *big_lse, *small_o, *small_lse;
     const int32_t* cu_new_lens;
     const int32_t* status;
+    const uint64_t* plan_mark;
+    uint64_t mark;
     const SharedReq* reqs;
     int64_t rows;  // T * Hq
     int32_t batch, num_kv_heads;

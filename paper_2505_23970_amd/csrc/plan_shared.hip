@@ -108,7 +108,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     int* const g_piece = derived(6);
     int* const g_at = derived(7);
     int* const g_taken = derived(8);   // [G] shared keys that are taken once
-    if (tid == 0) sm.bad = 0;
+    if (tid == 0) {
+        sm.bad = 0;
+        *a.plan_mark = a.mark;
+    }
     if constexpr (LDS) {  // (G <= B)
 #pragma nounroll
         for (int r = tid; r <= B; r += kPlanThreads) {

@@ -307,3 +307,98 @@ def test_refusals():
     off = torch.empty(q.numel() + 4, dtype=torch.bfloat16, device="cuda")[4:].view_as(q)
     with pytest.raises(gc.GcError):
         gc.run_shared(off, kp, vp, r.groups, w.scale, ws)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_pools_beyond_4_gib(fp8):
+    """Block ids whose byte offsets exceed 2^32, through the rotary append and the attention: bitwise what the
+    unshifted run gives. The blocks that a wraparound of those offsets would reach hold NaN."""
+    import paper_2505_23970_amd as gc
+    import torch
+    sizes, shared, beyond, new = SH.batches()["groups"]
+    w = SH.build(sizes, shared, beyond, new, 16, 2, 128, seed=3200, name="shared_4gib")
+    table = gc.rotary_table(400, 64)
+    runs = [H.DeviceRunFp8(w, 0.02, 0.015) if fp8 else H.DeviceRun(w) for _ in range(2)]
+    shift = (1 << 32) // (w.num_kv_heads * 16 * w.head_dim * (1 if fp8 else 2))
+    for name in ("k_pool", "v_pool"):
+        small = getattr(runs[1], name)
+        big = torch.empty((shift + w.num_blocks,) + tuple(small.shape[1:]), dtype=small.dtype, device="cuda")
+        (big[:w.num_blocks] if fp8 else big[:w.num_blocks].view(torch.int16)).fill_(0x7F if fp8 else int(W.BF16_NAN))
+        big[shift:] = small
+        setattr(runs[1], name, big)
+    runs[1].batch = gc.PagedBatch(w.prefix_lens, w.new_lens, (w.block_tables + shift).astype(np.int32))
+    got = []
+    for run in runs:
+        groups = gc.SharedPrefixes(run.batch, sizes, shared, gc.SHARE_ALWAYS)
+        args = (run.q, run.k_new, run.v_new, run.k_pool, run.v_pool, run.batch, table)
+        q = gc.kv_append_rotary_fp8(*args, run.ks, run.vs) if fp8 else gc.kv_append_rotary(*args)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device="cuda")
+        call = gc.shared_prefix_attention_fp8 if fp8 else gc.shared_prefix_attention
+        out = call(q, run.k_pool, run.v_pool, groups, w.scale, *((run.ks, run.vs) if fp8 else ()), lse=lse, kv_split_tiles=1)
+        got.append((out.view(torch.int16), lse, run.k_pool[-w.num_blocks:].view(torch.uint8), run.v_pool[-w.num_blocks:].view(torch.uint8)))
+    assert not bool(got[0][0].view(torch.bfloat16).isnan().any())
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    del runs, got
+    torch.cuda.empty_cache()
+
+
+def test_runs_without_their_plan_write_nothing():
+    """A cleared workspace, the plain attention's plan, the other pool kind's plan, another split's plan."""
+    import paper_2505_23970_amd as gc
+    import torch
+    sizes, shared, beyond, new = SH.batches()["prompts"]
+    w = SH.build(sizes, shared, beyond, new, 16, 2, 128, seed=3300, name="shared_no_plan")
+    r = Run(w, sizes, shared)
+    q, kp, vp = r.run.q, r.run.k_pool, r.run.v_pool
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    fp8 = H.DeviceRunFp8(w, 0.02, 0.015)
+
+    def untouched(what):
+        out = torch.full_like(q, 7.0)
+        lse = torch.full(q.shape[:2], 7.0, device="cuda")
+        gc.run_shared(q, kp, vp, r.groups, w.scale, ws, out=out, lse=lse)
+        torch.cuda.synchronize()
+        assert bool((out == 7.0).all()) and bool((lse == 7.0).all()), what
+
+    for fill in (0, 0xFF, 0x01):
+        ws.fill_(fill)
+        untouched(f"filled with {fill}")
+    gc.plan(16, kp, vp, r.run.batch, ws)
+    untouched("plain plan")
+    gc.plan_shared(16, fp8.k_pool, fp8.v_pool, r.groups, ws, kv_split_tiles=None)
+    bf16_bytes = gc.shared_workspace_size(16, kp, vp, r.groups)
+    if gc.shared_workspace_size(16, fp8.k_pool, fp8.v_pool, r.groups) != bf16_bytes:
+        untouched("8-bit plan")
+    gc.plan_shared(16, kp, vp, r.groups, ws, kv_split_tiles=1)
+    untouched("another split")
+    gc.plan_shared(16, kp, vp, r.groups, ws)
+    out = gc.run_shared(q, kp, vp, r.groups, w.scale, ws)
+    r.check(out, None, r.reference())
+
+
+def test_masked_rows_of_a_request_see_only_their_keys():
+    """Planted keys: one that would take over the softmax lies at the last shared key, at the first own one, at each
+    new token. Row i must show it from there on, no earlier row and no other request anything of it."""
+    import paper_2505_23970_amd as gc
+    import torch
+    sizes, shared, beyond, new = [3], [48], [0, 3, 20], [5, 5, 5]
+    for where in ("last_shared", "first_own", "new_2"):
+        w = SH.build(sizes, shared, beyond, new, 8, 2, 64, seed=3400, name=f"shared_planted_{where}")
+        r = Run(w, sizes, shared)
+        kp, vp = r.run.k_pool, r.run.v_pool
+        req = 1
+        pos = {"last_shared": 47, "first_own": 48, "new_2": int(w.prefix_lens[req]) + 2}[where]
+        block, slot = int(w.block_tables[req][pos // 16]), pos % 16
+        r.run.q.fill_(1.0)
+        kp[block, :, slot, :] = 4.0     # score 4 * 64 / 8 = 32 above everything random here
+        vp[block, :, :, slot] = 1000.0
+        out = gc.shared_prefix_attention(r.run.q, kp, vp, r.groups, w.scale, kv_split_tiles=1)
+        seen = (out.float().abs() > 500).all(dim=2).all(dim=1).cpu().numpy()
+        none = (out.float().abs() < 500).all(dim=2).all(dim=1).cpu().numpy()
+        want = np.zeros(15, bool)
+        if where == "last_shared":
+            want[:] = True
+        else:
+            want[5 + (0 if where == "first_own" else 2):10] = True
+        assert np.array_equal(seen, want) and np.array_equal(none, ~want), where
