@@ -343,16 +343,18 @@ typedef struct gc_shared {
  * As gc_prefix_prefill_workspace_size / _plan / _run / _attention (= plan + run) and their
  * 8-bit forms, over groups. Plans and workspaces are of their own kind (a plan made by
  * gc_shared_prefix_plan is run by gc_shared_prefix_run with the same batch, groups and
- * options; a run that takes groups once and finds no such plan in its workspace enqueues kernels
- * that write nothing), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1); gc_prefix_prefill_plan_status
- * serves them too, and covers the groups' device arrays. Options: tiling GC_TILES_AUTO only
- * (else GC_ERR_UNSUPPORTED); kv_split_tiles > 0 cuts 128-row tiles into chunks of that many 64-key
- * tiles, and the small tiles of successive requests into runs of that many 32-key tiles, < 0 leaves
- * 128-row tiles whole and makes a run as long as the longest small tile. Everything else, layouts, results in `out` and `lse`, sharing of a
- * workspace by runs, errors, is as for those calls; further errors: GC_ERR_NULL_ARG for a
- * missing array, GC_ERR_BAD_SHAPE for groups or shared lengths outside the above and for q, pools or
- * out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_BLOCK_TABLE for a shared length
- * past the block-table row.
+ * options; a run that takes groups once and finds no such plan in its workspace enqueues
+ * kernels that write nothing), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1);
+ * gc_prefix_prefill_plan_status serves them too, and covers the groups' device arrays.
+ * Options: tiling GC_TILES_AUTO only (else GC_ERR_UNSUPPORTED); kv_split_tiles > 0 cuts
+ * 128-row tiles into chunks of that many 64-key tiles, and the small tiles of successive
+ * requests into runs of that many 32-key tiles, < 0 leaves 128-row tiles whole and makes a
+ * run as long as the longest small tile. Everything else, layouts, results in `out` and
+ * `lse`, sharing of a workspace by runs, errors, is as for those calls; further errors:
+ * GC_ERR_NULL_ARG for a missing array, GC_ERR_BAD_SHAPE for groups or shared lengths outside
+ * the above, for q, pools or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE)
+ * and for a batch of more work than one launch holds, GC_ERR_BLOCK_TABLE for a shared
+ * length past the block-table row.
  */
 gc_status gc_shared_prefix_workspace_size(const gc_geometry* geo, const gc_batch* batch,
                                           const gc_shared* shared, const gc_plan_options* opts,
@@ -418,12 +420,13 @@ typedef struct gc_new_rows {
  *   rows  : the projections; device memory, 16-byte aligned
  *   q_out : device bf16 [T][Hq][D], 16-byte aligned: the q argument of the attention
  *           calls. It may be rows->q where that is packed (q_stride == Hq * D), and
- *           otherwise overlaps none of the inputs (else GC_ERR_BAD_SHAPE)
+ *           otherwise overlaps neither the inputs nor the pools (else GC_ERR_BAD_SHAPE)
  * A cached prefix is in the pool with its rotation, so restoring it (gc_kv_append)
  * and appending to it mix freely. Errors: those of gc_kv_append, and GC_ERR_NULL_ARG
  * for a missing table, rows->k or rows->v, or one of q and q_out without the other;
  * GC_ERR_BAD_SHAPE for a rotary_dim, stride or alignment outside the above and for a
- * table with fewer rows than the batch has positions.
+ * table with fewer rows than the batch has positions; GC_ERR_UNSUPPORTED for a batch of
+ * more work than one launch holds.
  */
 gc_status gc_kv_append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
                               const gc_new_rows* rows, void* q_out, void* k_pool, void* v_pool,

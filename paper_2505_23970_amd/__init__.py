@@ -606,9 +606,9 @@ def _require_rows(t, name, shape, device):
     T, heads, D = shape
     # one test for what every valid call passes, the tests one by one for the others
     if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.device == device:
-        st = t.stride()
-        if T > 1 and st[2] == 1 and st[1] == D and st[0] >= heads * D and st[0] % 8 == 0:
-            return st[0]
+        between, heads_apart, step = t.stride()
+        if T > 1 and step == 1 and heads_apart == D and between >= heads * D and between % 8 == 0:
+            return between
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device != device:
@@ -629,15 +629,15 @@ def _require_rows(t, name, shape, device):
     return st[0]
 
 
-def _here(device, stream, call):
-    """call() with the batch's device as the current one, which a launch goes to."""
-    torch = _t()
+def _here(device, stream, call, *args):
+    """call(*args, stream) with the batch's device as the current one, which a launch goes to."""
+    cuda = _t().cuda
     if stream is not None and stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the batch on {device}")
-    if torch.cuda.current_device() == device.index:
-        return call()
-    with torch.cuda.device(device):
-        return call()
+    if cuda.current_device() == device.index:
+        return call(*args, _stream_handle(stream))
+    with cuda.device(device):
+        return call(*args, _stream_handle(stream))
 
 
 def _empty_on(stream, *size, **kw):
@@ -660,7 +660,7 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
     _require(table, torch.float32, "table", device)
     if table.dim() != 3 or table.shape[2] != 2:
         raise ValueError("table must be [positions][rotary_dim / 2][2]")
-    T = batch.total_new
+    T = int(batch.cu_new_lens[-1])
     _, Hkv, _, D = k_pool.shape
     kv_shape = (T, Hkv, D)
     k_stride = _require_rows(k_new, "k_new", kv_shape, device)
@@ -682,9 +682,9 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
     geo = _geo_from_pools(k_pool, v_pool, Hq, batch)
     rot = Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1],
                  PAIRS_INTERLEAVED if interleaved else PAIRS_HALVES)
-    st = _here(device, stream, lambda: getattr(lib, fn)(
-        ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(rot), ctypes.byref(rows), out_at, *scales,
-        k_pool.data_ptr(), v_pool.data_ptr(), _stream_handle(stream)))
+    byref = ctypes.byref
+    st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), byref(rot), byref(rows), out_at, *scales,
+               k_pool.data_ptr(), v_pool.data_ptr())
     _check(fn, st, lib)
     return q_out
 
@@ -721,6 +721,8 @@ class SharedPrefixes:
         import torch
         sizes = np.ascontiguousarray(group_sizes, dtype=np.int32)
         self.shared_lens = np.ascontiguousarray(shared_lens, dtype=np.int32)
+        if not (np.array_equal(sizes, group_sizes) and np.array_equal(self.shared_lens, shared_lens)):
+            raise ValueError("group_sizes and shared_lens must be whole numbers of 32 bits")
         if sizes.ndim != 1 or self.shared_lens.shape != sizes.shape:
             raise ValueError("group_sizes and shared_lens must be one list each, of one length")
         if int(sizes.sum()) != batch.batch or (sizes <= 0).any():
@@ -749,7 +751,7 @@ def shared_workspace_size(num_q_heads, k_pool, v_pool, shared: SharedPrefixes, k
     geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
     out = ctypes.c_size_t(0)
     # (the plan goes by the device's compute units)
-    st = _here(batch.device, None, lambda: lib.gc_shared_prefix_workspace_size(
+    st = _here(batch.device, None, lambda _: lib.gc_shared_prefix_workspace_size(
         ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(shared.desc()), _opts(kv_split_tiles),
         k_pool.dtype == _t().uint8, ctypes.byref(out)))
     _check("gc_shared_prefix_workspace_size", st, lib)
@@ -769,9 +771,9 @@ def plan_shared(num_q_heads, k_pool, v_pool, shared: SharedPrefixes, workspace, 
     batch = shared.batch
     _require(workspace, torch.uint8, "workspace", batch.device)
     geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
-    st = _here(batch.device, stream, lambda: lib.gc_shared_prefix_plan(
-        ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(shared.desc()), _opts(kv_split_tiles),
-        k_pool.dtype == torch.uint8, workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    st = _here(batch.device, stream, lib.gc_shared_prefix_plan, ctypes.byref(geo), ctypes.byref(batch.desc()),
+               ctypes.byref(shared.desc()), _opts(kv_split_tiles), k_pool.dtype == torch.uint8, workspace.data_ptr(),
+               workspace.numel())
     _check("gc_shared_prefix_plan", st, lib)
 
 
@@ -786,10 +788,9 @@ def _shared_call(fn, q, k_pool, v_pool, shared, scale, scales, workspace, out, l
     if out is None:
         out = _empty_on(stream, q.shape, dtype=torch.bfloat16, device=batch.device)
     geo, out = _attn_args(q, k_pool, v_pool, batch, out, lse, workspace, pool_dtype)
-    st = _here(batch.device, stream, lambda: getattr(lib, fn)(
-        ctypes.byref(geo), ctypes.byref(batch.desc()), ctypes.byref(shared.desc()), _opts(kv_split_tiles),
-        q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *scales, float(scale), out.data_ptr(),
-        lse.data_ptr() if lse is not None else None, workspace.data_ptr(), workspace.numel(), _stream_handle(stream)))
+    st = _here(batch.device, stream, getattr(lib, fn), ctypes.byref(geo), ctypes.byref(batch.desc()),
+               ctypes.byref(shared.desc()), _opts(kv_split_tiles), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), *scales,
+               float(scale), out.data_ptr(), lse.data_ptr() if lse is not None else None, workspace.data_ptr(), workspace.numel())
     _check(fn, st, lib)
     return out
 

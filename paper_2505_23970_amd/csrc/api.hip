@@ -610,16 +610,18 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
             (int64_t)batch->prefix_lens_host[r] + batch->new_lens_host[r] > rot->num_positions)
             return GC_ERR_BAD_SHAPE;
     if (with_q) {
-        const int64_t out = T * q_row * 2;
+        const int64_t out = T * q_row * 2, pool = (int64_t)geo->num_blocks * gc::kPage * kv_row * (pk.fp8 ? 1 : 2);
         const bool in_place = q_out == rows->q && rows->q_stride == q_row;
         if ((!in_place && overlap(q_out, out, rows->q, span_bytes(T, rows->q_stride, q_row))) ||
             overlap(q_out, out, rows->k, span_bytes(T, rows->k_stride, kv_row)) ||
-            overlap(q_out, out, rows->v, span_bytes(T, rows->v_stride, kv_row)))
+            overlap(q_out, out, rows->v, span_bytes(T, rows->v_stride, kv_row)) ||
+            overlap(q_out, out, rot->table_dev, (int64_t)rot->num_positions * rot->rotary_dim * 4) ||
+            overlap(q_out, out, k_pool, pool) || overlap(q_out, out, v_pool, pool))
             return GC_ERR_BAD_SHAPE;
     }
     gc::RotaryArgs ra{};
     ra.a = append_args(geo, batch, sh, rows->k, rows->v, k_pool, v_pool, pk);
-    if (gc::rotary_workgroups(ra.a.total_pages, geo->num_q_heads, geo->num_kv_heads, geo->head_dim, with_q) >= (int64_t)INT32_MAX)
+    if (gc::rotary_workgroups(ra.a.total_pages, geo->num_q_heads, geo->num_kv_heads, geo->head_dim, with_q) > gc::kMaxWorkgroups)
         return GC_ERR_UNSUPPORTED;
     ra.q = static_cast<const uint16_t*>(rows->q);
     ra.q_out = static_cast<uint16_t*>(q_out);
@@ -976,9 +978,9 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
         pl->pieces = pl->parts + (pl->places - 1) / z.run.d;
         pl->runs = gc::ceil_div64(pl->places, z.run.d);
     }
-    const int64_t most = (int64_t)INT32_MAX / geo->num_kv_heads - 64;
-    if (pl->big > most || pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run.d ||
-        sh.total_tokens * geo->num_q_heads / 8 >= INT32_MAX)
+    const int64_t most = gc::kMaxWorkgroups / geo->num_kv_heads - 64;
+    if (pl->big + pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run.d ||
+        sh.total_tokens * geo->num_q_heads / 8 >= gc::kMaxWorkgroups)
         return GC_ERR_BAD_SHAPE;
     gc::SharedLayout& l = pl->layout;
     size_t off = 256;  // (the status word leads, as in the plain workspace)
@@ -1088,8 +1090,6 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const gc
     a.max_blocks = geo->max_blocks_per_seq;
     a.scale_log2 = (float)((double)scale * (double)pk.k_scale * 1.4426950408889634074);
     a.v_scale = pk.v_scale;
-    a.prefer_span = (uint32_t)device_cus();
-    a.prefer_odd = 0;
     a.small_items = at<gc::SharedItem>(ws, spl.layout.small_off);
     a.small_o = at<float>(ws, spl.layout.small_o_off);
     a.small_lse = at<float>(ws, spl.layout.small_lse_off);

@@ -36,7 +36,3 @@ def batches():
         "many": ([70, 30], [96, 144], rng.integers(0, 60, 100).tolist(), rng.choice([0, 1, 1, 1, 2], 100).tolist()),
     }
 
-
-def effective(w, sizes, shared):
-    first = np.concatenate([[0], np.cumsum(sizes)])
-    return [(int(first[g]), int(first[g + 1]), int(shared[g])) for g in range(len(sizes))]

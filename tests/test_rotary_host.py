@@ -53,6 +53,9 @@ def test_shapes(lib):
     assert status(lib, rot=rot) == -2
     assert status(lib, g=geo(D=96)) == -3
     assert status(lib, b=HostBatch([4], [-3])) == -2
+    # more workgroups than a launch has threads for
+    assert status(lib, g=geo(NB=1 << 30, maxb=1 << 26), b=HostBatch([0], [(1 << 30) - 64]), num_positions=1 << 30,
+                  k=1 << 50, v=1 << 51, q=1 << 52, q_out=1 << 53) == -3
 
 
 def test_strides_alignment_and_overlap(lib):
@@ -67,6 +70,8 @@ def test_strides_alignment_and_overlap(lib):
     assert status(lib, q_out=0x100000, q_stride=2048) == -2        # in place over strided rows
     assert status(lib, q_out=0x200000) == -2                       # over k
     assert status(lib, q_out=0x300200) == -2                       # over v
+    assert status(lib, q_out=0x1100) == -2                         # over the table
+    assert status(lib, q_out=0x20000) == -2                        # over the pools
 
 
 def test_scales(lib):

@@ -59,6 +59,9 @@ def test_groups_and_shared_lengths(lib):
     s = GOOD()
     s.desc.reserved[5] = 1
     assert size(lib, geo(), B(), s)[0] == -2
+    # more rows than the merge's launch has threads for
+    big = HostBatch([64], [1 << 28])
+    assert size(lib, geo(NB=1 << 30, maxb=1 << 25), big, HostShared([0, 1], [64]))[0] == -2
     # the shared pages must lie in the table row, also of a group without new tokens
     assert size(lib, geo(maxb=3), HostBatch([80, 8], [0, 1]), HostShared([0, 1, 2], [80, 0]))[0] == -4
 
@@ -127,3 +130,16 @@ def test_what_the_policy_takes(lib, P, n, first, lens, taken):
     assert st == 0 and always != plain_size(lib, g, b)
     if taken and len(lens) == 1:
         assert auto == always
+
+
+def test_groups_of_the_binding():
+    batch = gc.PagedBatch([40, 40], [1, 1], np.zeros((2, 4), np.int32), device="cpu")
+    gc.SharedPrefixes(batch, np.array([2]), np.array([32]))
+    for sizes, lens in (([2], [[32]]), ([1], [32]), ([2, 0], [32, 0]), ([3, -1], [32, 0]), ([2], [32, 0]), ([2], [16.5]),
+                        ([2], np.array([(1 << 32) + 32])), (np.array([(1 << 32) + 2]), [32])):
+        with pytest.raises(ValueError):
+            gc.SharedPrefixes(batch, sizes, lens)
+    batch = gc.PagedBatch([40, 40], [1, 1], [[1, 2, 3, 4], [1, 5, 3, 4]], device="cpu")
+    gc.SharedPrefixes(batch, [2], [16])
+    with pytest.raises(ValueError):
+        gc.SharedPrefixes(batch, [2], [32])
