@@ -243,6 +243,8 @@ def traffic_sources(kernel_source):
     own = [kernel_source]
     if kernel_source in (csrc + "attention.hip", csrc + "attention_plain.hip"):
         own.append(csrc + "attention_kernels.h")
+    if kernel_source == csrc + "attention_small.hip":
+        own.append(csrc + "attention_small_body.h")
     return own + [csrc + "plan_body.h", csrc + "api.hip", csrc + "gc_internal.h", "paper_2505_23970_amd/build.py"]
 
 

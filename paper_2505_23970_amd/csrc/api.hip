@@ -810,7 +810,7 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
 // at about 20 TB/s over all heads, its 128-row tiles at the matrix cores' pace; taken once, they cost a read
 // from HBM or the pace of the group's own 128-row tiles, and every row two fp32 partial rows, written and
 // read. Paces: us of a compute unit per 128-row tile and 64 keys (48 requests of 20 tokens on 32768 shared ones, the
-// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 1075; at d = 64 533 / 288 and 665 / 341).
+// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 988; at d = 64 533 / 288 and 665 / 341).
 // Short launches of 128-row tiles are bound by their latency, which the finer chunks here make shorter: up to 64
 // tiles over all heads and 4096 of their key tiles, groups of 256 shared keys or more are taken (16.0 us / 13.2
 // for two requests of 3 tokens on 513, 18.8 / 15.5 for 27 on 796, 21.7 / 17.9 for 7 of 19 tokens; at 16384 key
@@ -825,7 +825,7 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
     const double key_bytes = heads * D * 2 * (pk.fp8 ? 1 : 2);
     const double step = heads / device_cus() / gc::kBlockN;  // of a 128-row tile, per key
     const double plain_pace = D == 128 ? (pk.fp8 ? 1.13 : 0.85) : (pk.fp8 ? 0.86 : 0.69);
-    const double shared_pace = D == 128 ? (pk.fp8 ? 1.12 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
+    const double shared_pace = D == 128 ? (pk.fp8 ? 1.03 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
     double gain = 0;
     bool any_tiles = false;
     double all_tiles = 0, all_steps = 0;  // of all requests, over all heads

@@ -122,16 +122,16 @@ __device__ __forceinline__ void widen_e4m3x16(const u32x4 c, u32x4& lo, u32x4& h
 
 // One work item (a workgroup of WAVES wavefronts): the item of launch index bid (blockIdx.x
 // in the regular launch), i.e. work item bid / Hkv for KV head bid % Hkv. SHARED: an item of a
-// shared-prefix launch (SharedItem): its keys start at page page0 of the table row, and all of
+// shared-prefix launch (SharedItem), ROWS rows a wavefront: its keys start at page page0 of the table row, and all of
 // them are visible to every row where `full` is set; the launch's small items run here too, in
 // the same LDS.
-template <int D, int WAVES, bool FP8, int WGS = 8 / WAVES, bool SHARED = false, typename Args = AttnArgs>
+template <int D, int WAVES, bool FP8, int WGS = 8 / WAVES, bool SHARED = false, int ROWS = kRowsPerWave, typename Args = AttnArgs>
 __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid) {
-    constexpr int kBlockRows = WAVES * kRowsPerWave;  // query rows of a work item
+    constexpr int kBlockRows = WAVES * ROWS;  // query rows of a work item
     constexpr int KS = D / 32;                      // k-steps of QK^T
     constexpr int DB = D / 16;                      // 16-row blocks of O^T
-    constexpr int RB = kRowsPerWave / 16;           // 16-row query blocks per wavefront
-    static_assert(RB == 2, "row blocks");
+    constexpr int RB = ROWS / 16;           // 16-row query blocks per wavefront
+    static_assert(RB == 1 || RB == 2, "row blocks");
     constexpr int kPageBytes = kPage * D * 2;       // one (block, KV head) page of K or V
     constexpr int kTileBytes = kBlockN * D * 2;     // four pages
     constexpr int kKbPerPage = kPageBytes / 1024;   // 1 KiB pieces per page
@@ -206,8 +206,9 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
     // 2052 us, 70B chat 434 -> 422, 8B chat 125.7 -> 121.5, over 8-bit pools 173.6 -> 154.8; at
     // d = 64, where three 128-row workgroups share a compute unit, 2 % slower, so not there.
     // (Before the item's loads: between them and their uses the branch cost 1-3 % of short launches.)
-    // Not in shared-prefix launches: one 128-row workgroup a unit beside a small one is as fast without, two are
-    // faster (48 questions of 20 tokens on 32768 shared ones 914 us, with it 964).
+    // Not between the 4-wavefront workgroups of shared-prefix launches: one a unit beside a small one is as fast
+    // without, two are faster (48 questions of 20 tokens on 32768 shared ones 914 us, with it 964). Between the
+    // halves of the 8-wavefront ones it is 1 % faster.
     if (WAVES == kWideWaves ? wave < WAVES / 2 : !SHARED && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd)
         __builtin_amdgcn_s_setprio(2);
     const int g4 = lane >> 4;
@@ -235,14 +236,14 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
     const bool full = item_full(it);
     const int ntok = min(a.tq, n - it.q0);
 
-    // this lane's query rows, 16 rb + j16 of the wavefront's 32: token t of the tile, query
+    // this lane's query rows, 16 rb + j16 of the wavefront's 32 (16): token t of the tile, query
     // head kvh * g + hl
     bool row_ok[RB];
     int lim[RB];  // last key the row may see
     int64_t qrow[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int m = wave * kRowsPerWave + 16 * rb + j16;
+        const int m = wave * ROWS + 16 * rb + j16;
         const int t = (int)((unsigned)m / (unsigned)a.group);
         row_ok[rb] = t < ntok;
         lim[rb] = P + it.q0 + (row_ok[rb] ? t : 0);
@@ -484,7 +485,8 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         // first on the 8-wavefront tiles; on the 4-wavefront ones the first half's, then a
         // quarter of the second half's after every quarter of the first half's products
         // (a pair after every fragment: 2 % slower on wide tiles, 10 % on the 8B chat batch).
-        constexpr bool kAllFirst = WAVES == kWideWaves;
+        // 8 wavefronts of 16 rows: as on the 4-wavefront ones (100 answers over 8-bit pools 59.3 us, all first 61.3).
+        constexpr bool kAllFirst = WAVES == kWideWaves && RB == 2;
 #pragma unroll
         for (int hb = 0; hb < (kAllFirst ? 2 : 1); ++hb)
 #pragma unroll
@@ -653,7 +655,7 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         step(1);
         if (++kt >= it.kt_end) break;
     }
-    if (exact || !__syncthreads_or(!(l_run[0] <= 0x1p100f) || !(l_run[1] <= 0x1p100f))) break;
+    if (exact || !__syncthreads_or(!(l_run[0] <= 0x1p100f) || !(l_run[RB - 1] <= 0x1p100f))) break;
     exact = true;
     }
 
@@ -679,7 +681,7 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         // of one token's query heads are adjacent in the output.
         constexpr int kOutRow = 2 * D;                  // bytes per row
         constexpr int CH = kOutRow / 16;                // 16-byte chunks per row
-        constexpr int kStage = kRowsPerWave * kOutRow;  // bytes per wavefront
+        constexpr int kStage = ROWS * kOutRow;  // bytes per wavefront
         constexpr int kPerBuf = kTileBytes / kStage;    // wavefronts per tile buffer
         static_assert(kPerBuf * 4 >= WAVES && kPerBuf * kStage == kTileBytes, "stage layout");
         const int sb = wave / kPerBuf;
@@ -701,10 +703,10 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         wave_lds_sync();
         constexpr int kRowsPerStore = 64 / CH;
 #pragma unroll
-        for (int i = 0; i < kRowsPerWave / kRowsPerStore; ++i) {
+        for (int i = 0; i < ROWS / kRowsPerStore; ++i) {
             const int rr = i * kRowsPerStore + lane / CH, ch = lane % CH;
             const u32x4 v = *reinterpret_cast<const u32x4*>(stage + rr * kOutRow + (ch ^ (rr & (CH - 1))) * 16);
-            const int mr = wave * kRowsPerWave + rr;  // the stored row's token and head
+            const int mr = wave * ROWS + rr;  // the stored row's token and head
             const int tr = mr / a.group;
             if (tr < ntok) {
                 const int64_t qr = (int64_t)(cu + it.q0 + tr) * a.num_q_heads + kvh * a.group + (mr - tr * a.group);
@@ -718,16 +720,16 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         constexpr int kOutRow = 4 * D;                        // bytes per fp32 row
         constexpr int CH = kOutRow / 16;                      // 16-byte chunks per row
         constexpr int kStage = 4 * kTileBytes / WAVES;        // stage bytes per wavefront
-        constexpr int kRows = kStage / kOutRow < kRowsPerWave ? kStage / kOutRow : kRowsPerWave;
-        static_assert(kRows >= 2 && kRowsPerWave % kRows == 0 && (kRows * CH) % 64 == 0, "partial stage");
+        constexpr int kRows = kStage / kOutRow < ROWS ? kStage / kOutRow : ROWS;
+        static_assert(kRows >= 2 && ROWS % kRows == 0 && (kRows * CH) % 64 == 0, "partial stage");
         constexpr int kPerBuf = kTileBytes / kStage;
         const int sb = wave / kPerBuf;
         unsigned char* stage = (sb == 0 ? k_lds0 : sb == 1 ? v_lds0 : sb == 2 ? k_lds1 : v_lds1) +
                                (wave % kPerBuf) * kStage;
-        const int64_t prow0 = ((int64_t)it.part * a.num_kv_heads + kvh) * kBlockRows + wave * kRowsPerWave;
+        const int64_t prow0 = ((int64_t)it.part * a.num_kv_heads + kvh) * kBlockRows + wave * ROWS;
         constexpr int kSw = CH < 16 ? CH : 16;                // chunk swizzle span
 #pragma unroll
-        for (int r0 = 0; r0 < kRowsPerWave; r0 += kRows) {
+        for (int r0 = 0; r0 < ROWS; r0 += kRows) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int sr = 16 * rb + j16 - r0;

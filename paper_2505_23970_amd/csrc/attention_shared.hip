@@ -26,9 +26,22 @@
 namespace gc {
 namespace {
 
+// Wavefronts of a workgroup, for 128-row tiles: 4 of 32 rows, or 8 of 16. With 8, the wavefronts that share a SIMD
+// compute products and weights in turn where only one such workgroup is on the unit, and 512 threads share
+// the widening of a tile's codes; every key and value is read from LDS twice as often, and 128 registers must do,
+// which spills around the items. Over 8-bit pools at d = 128 (8 wavefronts / 4): 100 answers on four documents 59.3 us / 67.1,
+// 48 questions of 20 tokens on 32768 shared ones 988 / 1065, 8 of 60 tokens on 4096 62.7 / 74.2. Over bf16 pools
+// 64 answers on 8192 tokens 55.2 / 54.1, 128 on 16384 142 / 133, 200 on 32768 at 8 heads 44.9 / 45.9; at d = 64 in 8 bits 40 single
+// tokens on 6000 26.8 / 26.2, 24 questions of 20 tokens in bf16 39.0 / 40.7 and 48 on 32768 632 / 599.
+template <int D, bool FP8, int W>
+__global__ __launch_bounds__(W * 64, W / 2) void attention_shared_kernel(const SharedAttnArgs a) {
+    attention_body<D, W, FP8, 2, true, kBlockM / W>(a, blockIdx.x);
+}
+
 template <int D, bool FP8>
-__global__ __launch_bounds__(kAttnThreads, 2) void attention_shared_kernel(const SharedAttnArgs a) {
-    attention_body<D, kWaves, FP8, 2, true>(a, blockIdx.x);
+void launch_items(const SharedAttnArgs& a, unsigned workgroups, hipStream_t s) {
+    constexpr int W = FP8 && D == 128 ? 8 : kWaves;
+    attention_shared_kernel<D, FP8, W><<<workgroups, W * 64, 0, s>>>(a);
 }
 
 // Merge: a thread owns four consecutive output elements of one row; its chunks' log-sum-exps and
@@ -165,18 +178,11 @@ hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, boo
     a.big_wgs = (int)((a.shared_per_xcd + ceil_div64(a.own_items * heads, kQueues)) * kQueues);
     const int64_t small = ceil_div64(a.small, shared_rings(fp8));
     if (a.big_wgs + small == 0) return hipSuccess;
-    const dim3 grid((unsigned)(a.big_wgs + small));
-    if (fp8) {
-        if (head_dim == 128)
-            attention_shared_kernel<128, true><<<grid, kAttnThreads, 0, s>>>(a);
-        else
-            attention_shared_kernel<64, true><<<grid, kAttnThreads, 0, s>>>(a);
-    } else {
-        if (head_dim == 128)
-            attention_shared_kernel<128, false><<<grid, kAttnThreads, 0, s>>>(a);
-        else
-            attention_shared_kernel<64, false><<<grid, kAttnThreads, 0, s>>>(a);
-    }
+    const unsigned grid = (unsigned)(a.big_wgs + small);
+    if (head_dim == 128)
+        fp8 ? launch_items<128, true>(a, grid, s) : launch_items<128, false>(a, grid, s);
+    else
+        fp8 ? launch_items<64, true>(a, grid, s) : launch_items<64, false>(a, grid, s);
     return hipGetLastError();
 }
 

@@ -19,7 +19,7 @@ constexpr int kBlockN = 64;
 constexpr int kDecM = 16;
 constexpr int kDecN = 32;
 constexpr int kPage = 16;
-constexpr int64_t kMaxWorkgroups = UINT32_MAX / 256;  // of 256 threads, in one launch
+constexpr int64_t kMaxWorkgroups = UINT32_MAX / 512;  // of up to 512 threads, in one launch
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kAttnThreads = kWaves * 64;
 // Wide prefill tiles: 8 wavefronts, 256 query rows per work item (one workgroup
