@@ -402,3 +402,41 @@ def test_masked_rows_of_a_request_see_only_their_keys():
         else:
             want[5 + (0 if where == "first_own" else 2):10] = True
         assert np.array_equal(seen, want) and np.array_equal(none, ~want), where
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("D,Hq", [(128, 8), (64, 16)])
+def test_score_jumps_beyond_the_exponent_slack(D, Hq, fp8):
+    """Keys that score 0, a later one that scores 100 and more above them, one that scores as much more again: the
+    last takes all the weight (the others' are exp of at most -100, nothing in fp32), so each row is its value. In
+    tiles of 128 rows the weights' sum passes fp32 at the jump, and the items run again with the exact maxima; the
+    single tokens' small tiles take it as they go. The output: that value times its scale in fp32 (2^-24, two
+    products), rounded to bf16 (2^-8)."""
+    import paper_2505_23970_amd as gc
+    import torch
+    sizes, shared, beyond, new = [3, 2], [320, 0], [40, 0, 70, 200, 90], [20, 1, 30, 40, 1]
+    w = SH.build(sizes, shared, beyond, new, Hq, 1, D, seed=3500, name=f"shared_jump_d{D}")
+    r = Run(w, sizes, shared, fp8)
+    kp, vp = r.run.k_pool, r.run.v_pool
+    r.run.q.fill_(1.0)
+    kp.zero_()
+    # one key's element value x gives the score x * D * scale; e4m3 codes: 0x7E is 448, 0x76 is 224
+    ks, vs = (r.run.ks, r.run.vs) if fp8 else (1.0, 1.0)
+    scale = 120.0 / (D * (224 * ks if fp8 else 224.0))
+    want = torch.empty(sum(new), D, device="cuda")
+    at = 0
+    for req, n in enumerate(new):
+        table = w.block_tables[req]
+        for pos, code in ((100 if req < 3 else 70, 0x76), (290 if req < 3 else 85, 0x7E)):
+            kp[int(table[pos // 16]), 0, pos % 16] = code if fp8 else float(224 if code == 0x76 else 448)
+        v = vp[int(table[pos // 16]), 0, :, pos % 16]
+        want[at:at + n] = v.view(torch.float8_e4m3fn).float() * vs if fp8 else v.float()
+        at += n
+    for split in (None, 1, -1):
+        args = (r.run.q, kp, vp, r.groups, scale) + ((ks, vs) if fp8 else ())
+        lse = torch.empty(sum(new), Hq, device="cuda")
+        out = (gc.shared_prefix_attention_fp8 if fp8 else gc.shared_prefix_attention)(*args, lse=lse, kv_split_tiles=split)
+        err = (out.float() - want[:, None, :]).abs()
+        assert bool((err <= want[:, None, :].abs() * (2.0 ** -8 + 2.0 ** -22)).all()), (split, float(err.max()))
+        # the score itself: a sum of D equal products (exact), times scale, log2 e and ln 2 in fp32: five roundings
+        assert bool(((lse - 240.0).abs() <= 240.0 * 2.0 ** -20).all()), split
