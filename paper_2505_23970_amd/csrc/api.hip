@@ -1,6 +1,7 @@
 // Host side of the C ABI declared in include/greencache.h: argument checks,
 // work-split policy, workspace layout and kernel launches. Every check runs
 // before the first HIP call, so invalid calls enqueue nothing.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <mutex>
@@ -1116,6 +1117,7 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const gc
     m.rows = sh.total_tokens * geo->num_q_heads;
     m.batch = b->batch;
     m.num_kv_heads = geo->num_kv_heads;
+    m.single = sh.total_tokens == b->batch && std::all_of(b->new_lens_host, b->new_lens_host + b->batch, [](int32_t n) { return n == 1; });
     m.hq = gc::divisor(geo->num_q_heads);
     m.group = gc::divisor(sh.group);
     m.tq = spl.z.tq;

@@ -164,9 +164,12 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
             unsigned char* const r0 = FP8 ? (w == 0 ? k_lds0 : w == 1 ? v_lds0 : w == 2 ? k_lds1 : v_lds1) : (w == 0 ? k_lds0 : k_lds1);
             unsigned char* const r1 = FP8 ? r0 + kTile : (w == 0 ? v_lds0 : v_lds1);
             kvh = (int)(at % (unsigned)a.num_kv_heads);
-            if (*a.plan_mark != a.mark) return;
+            const uint64_t mark = *a.plan_mark;  // (one wait for both)
+            int id = a.runs[at / (unsigned)a.num_kv_heads];
+            asm volatile("" ::"s"(mark), "s"(id));
+            if (mark != a.mark) return;
             // (the bound holds whatever the plan wrote)
-            for (int id = a.runs[at / (unsigned)a.num_kv_heads]; id >= 0 && id < a.pieces; ++id) {
+            for (; id >= 0 && id < a.pieces; ++id) {
                 const SharedItem it = a.small_items[id];
                 small_body<D, FP8, true>(s, it, kvh, r0, r1);
                 if (it.last) break;
@@ -218,13 +221,15 @@ __device__ __forceinline__ void attention_body(const Args& a, const unsigned bid
         item = bid / (unsigned)a.num_kv_heads;
     }
     using Item = std::conditional_t<SHARED, SharedItem, WorkItem>;
+    uint64_t mark = 0;
+    if constexpr (SHARED) mark = *a.plan_mark;
     const Item it = reinterpret_cast<const Item*>(a.items)[item];
     // all eight fields in one load (else the fields the test below needs are loaded
     // first and the rest after it, a second dependent round trip)
     asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P),
                  "s"(it.cu), "s"(it.n));
     if constexpr (SHARED)
-        if (*a.plan_mark != a.mark) return;
+        if (mark != a.mark) return;
     if (it.r < 0 || it.kt_begin >= it.kt_end) return;
     // (the planner repeats the request's lengths in the item: one load for all of them)
     const int r = it.r;

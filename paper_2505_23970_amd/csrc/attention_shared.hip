@@ -65,9 +65,9 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
     const bool in_range = row < a.rows;
     const int64_t row_or_last = in_range ? row : a.rows - 1;
     const int t = a.rows <= UINT32_MAX ? a.hq.of((uint32_t)row_or_last) : (int)(row_or_last / a.hq.d);
-    // the request of the wavefront's first row: the last r with cu[r] <= t0
+    // the request of the wavefront's first row: the last r with cu[r] <= t0 (one token each: t0 itself, a load less)
     const int t0 = __builtin_amdgcn_readfirstlane(t);
-    int lo = 0, hi = a.batch;  // cu[lo] <= t0 < cu[hi]
+    int lo = a.single ? t0 : 0, hi = a.single ? t0 + 1 : a.batch;  // cu[lo] <= t0 < cu[hi]
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64;
         const int at = lo + step * (lane + 1);

@@ -351,6 +351,7 @@ struct SharedMergeArgs {
     const SharedReq* reqs;
     int64_t rows;  // T * Hq
     int32_t batch, num_kv_heads;
+    int32_t single;  // every request has one new token
     Divisor hq, group, tq;  // query heads; of a KV head; new tokens of a 128-row tile
 };
 
