@@ -607,8 +607,11 @@ def _require_rows(t, name, shape, device):
     # one test for what every valid call passes, the tests one by one for the others
     if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.device == device:
         between, heads_apart, step = t.stride()
-        if T > 1 and step == 1 and heads_apart == D and between >= heads * D and between % 8 == 0:
-            return between
+        if step == 1 and heads_apart == D:
+            if T == 1:
+                return heads * D
+            if T > 1 and between >= heads * D and between % 8 == 0:
+                return between
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.device != device:
@@ -631,12 +634,13 @@ def _require_rows(t, name, shape, device):
 
 def _here(device, stream, call, *args):
     """call(*args, stream) with the batch's device as the current one, which a launch goes to."""
-    cuda = _t().cuda
+    torch = _t()
     if stream is not None and stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the batch on {device}")
-    if cuda.current_device() == device.index:
-        return call(*args, _stream_handle(stream))
-    with cuda.device(device):
+    index = device.index
+    if torch.cuda.current_device() == index:
+        return call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    with torch.cuda.device(device):
         return call(*args, _stream_handle(stream))
 
 
