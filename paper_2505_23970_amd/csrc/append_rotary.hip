@@ -15,9 +15,11 @@
 // Work. A workgroup owns one destination page (up to 16 tokens of one request) of either
 //   - one KV head (two at D = 64): keys in 16-byte chunks, one per thread, whose partner chunk in the other
 //     half comes from the lane that holds it; values as in the plain append (append_body.h);
-//   - or kRotQHeads query heads: a thread owns a pair of 16-byte chunks (elements j .. j + 7 and their
-//     partners), holds the eight (cos, sin) of its token in registers and goes through the heads, so it may
-//     write q_out over q. Pages with few new tokens (decode) put their threads on heads instead.
+//   - or kRotQHeads query heads: a thread owns two 16-byte chunks (elements j .. j + 7 and their
+//     partners, or two that need no other), holds the eight (cos, sin) of its token in registers and goes through
+//     the heads, so it may write q_out over q. Pages with few new tokens (decode) put their threads on heads
+//     instead. Neighbouring lanes take neighbouring chunks and then heads, whatever the pairs (pairs side by side:
+//     16000 tokens of the 70B heads 92 us, 121 with a thread's two chunks adjacent and slots before heads).
 // What bounds it: memory for prompts; for decode the chain lengths -> block id, rows and table -> stores.
 //   - Prompts: the workgroups of a page (its KV heads, its query heads) are launched side by side, on all
 //     XCDs, so that a token's projections are read in one sweep (30000 tokens of the 70B heads 243 us, page
@@ -27,7 +29,8 @@
 //     9.8 (10.8). The queries are read that way as well where they exceed what the last-level cache keeps from one
 //     pass to the next: from 192 MB of them on (1290 MB 210 us against 231, 550 MB 94 / 99; but 359 MB 66 / 61,
 //     183 MB at d = 64 41 / 32).
-// At 1290 MB it moves 6.1 TB/s; a copy of as many bytes by the framework's tensor library 5.3.
+// At 1290 MB it moves 5.7 TB/s (228 us), and 6.1 where the last-level cache holds a part of the inputs; a copy of as
+// many bytes by the framework's tensor library 4.8 to 5.3.
 #include "append_body.h"
 
 namespace gc {
@@ -62,7 +65,7 @@ __device__ __forceinline__ u32x4 pack8(const float (&y)[8]) {
 
 // (cos, sin) of N consecutive pairs.
 template <int N>
-__device__ __forceinline__ void load_angles(const float* at, float (&cs)[N], float (&sn)[N]) {
+__device__ __forceinline__ void load_angles(const float* at, float* cs, float* sn) {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
         const f32x4 w = *reinterpret_cast<const f32x4*>(at + 4 * i);
@@ -109,17 +112,10 @@ __device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm
         v = *reinterpret_cast<const u32x4*>(a.v_new + row * ra.v_stride + h * D + c * 8);
         if (turned) {
             const float* table = ra.table + (int64_t)pos * ra.rotary_dim;
-            if (ra.interleaved) {
-                float c4[4], s4[4];
-                load_angles<4>(table + 8 * c, c4, s4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    cs[j] = c4[j];
-                    sn[j] = s4[j];
-                }
-            } else {
+            if (ra.interleaved)
+                load_angles<4>(table + 8 * c, cs, sn);
+            else
                 load_angles<8>(table + 16 * (c < half ? c : c - half), cs, sn);
-            }
         }
     }
     float x[8];
@@ -165,25 +161,33 @@ __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& a
     constexpr int U = D / 16;  // pairs of chunks per head
     constexpr int kBatch = 4;  // heads whose loads a thread keeps in flight
     const int slots = s1 - s0;
-    const int span = slots <= 1 ? 1 : slots <= 2 ? 2 : slots <= 4 ? 4 : slots <= 8 ? 8 : 16;  // threads over slots
+    // Threads go over the slots, each over heads `step` apart: a head's lanes side by side, then `step` heads.
+    const int span = slots <= 1 ? 1 : slots <= 2 ? 2 : slots <= 4 ? 4 : slots <= 8 ? 8 : 16;
     const int u = threadIdx.x % U;
     const int rest = threadIdx.x / U;
-    const int s = s0 + rest % span;
     const int step = kAppendThreads / (U * span);
+    const int s = s0 + rest / step;
     const int64_t row = (int64_t)at.cu + (int64_t)lp * kPage - at.P + s;
     const int pos = lp * kPage + s;
     if (s >= s1 || row < 0 || row >= ra.a.total_tokens || pos >= ra.num_positions) return;
     const int half = ra.rotary_dim / 16;
-    const bool turned = u < half;
-    // this thread's two chunks, 8 elements each
-    const int c0 = turned && !ra.interleaved ? u : 2 * u;
-    const int c1 = turned && !ra.interleaved ? u + half : 2 * u + 1;
+    // This thread's two chunks, 8 elements each: so that the lanes of a head read and write adjacent ones.
+    // Halves: the partners, or two of the rest; side by side: one of the head's lower half and one of its upper.
+    const int c0 = ra.interleaved || u < half ? u : u + half;
+    const int c1 = c0 + (ra.interleaved ? U : u < half ? half : U - half);
+    const bool turned0 = c0 < 2 * half, turned1 = c1 < 2 * half;
     float cs[8] = {}, sn[8] = {};
-    if (turned) load_angles<8>(ra.table + (int64_t)pos * ra.rotary_dim + 16 * u, cs, sn);
+    const float* const table = ra.table + (int64_t)pos * ra.rotary_dim;
+    if (!ra.interleaved) {
+        if (turned0) load_angles<8>(table + 16 * u, cs, sn);
+    } else {
+        if (turned0) load_angles<4>(table + 8 * c0, cs, sn);
+        if (turned1) load_angles<4>(table + 8 * c1, cs + 4, sn + 4);
+    }
     const int h_end = min((qg + 1) * kRotQHeads, ra.num_q_heads);
     const uint16_t* src = ra.q + row * ra.q_stride;
     uint16_t* dst = ra.q_out + row * ra.num_q_heads * D;
-    for (int h0 = qg * kRotQHeads + rest / span; h0 < h_end; h0 += kBatch * step) {
+    for (int h0 = qg * kRotQHeads + rest % step; h0 < h_end; h0 += kBatch * step) {
         u32x4 w0[kBatch], w1[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
@@ -199,24 +203,22 @@ __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& a
         for (int b = 0; b < kBatch; ++b) {
             const int h = h0 + b * step;
             if (h >= h_end) break;
-            if (turned) {
-                float x[8], y[8];
-                widen8(w0[b], x);
-                widen8(w1[b], y);
-                if (ra.interleaved) {
-                    turn_adjacent(x, cs, sn);
-                    turn_adjacent(y, cs + 4, sn + 4);
-                } else {
+            float x[8], y[8];
+            widen8(w0[b], x);
+            widen8(w1[b], y);
+            if (ra.interleaved) {
+                turn_adjacent(x, cs, sn);
+                turn_adjacent(y, cs + 4, sn + 4);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float lo = x[j], hi = y[j];
-                        x[j] = fmaf(lo, cs[j], -(hi * sn[j]));
-                        y[j] = fmaf(hi, cs[j], lo * sn[j]);
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    const float lo = x[j], hi = y[j];
+                    x[j] = fmaf(lo, cs[j], -(hi * sn[j]));
+                    y[j] = fmaf(hi, cs[j], lo * sn[j]);
                 }
-                w0[b] = pack8(x);
-                w1[b] = pack8(y);
             }
+            if (turned0) w0[b] = pack8(x);
+            if (turned1) w1[b] = pack8(y);
             __builtin_nontemporal_store(w0[b], reinterpret_cast<u32x4*>(dst + h * D + 8 * c0));
             __builtin_nontemporal_store(w1[b], reinterpret_cast<u32x4*>(dst + h * D + 8 * c1));
         }
