@@ -793,7 +793,7 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
     for (int pass = 0; pass < 2; ++pass) {
         for (int g = 0; g < s->groups; ++g) {
             const int ra = s->group_first_host[g], rb = s->group_first_host[g + 1];
-            const int S = z.taken(g, s->shared_lens_host[g]);
+            const int S = z.taken(g, s->shared_lens_host[g], z.take);
             if (pass == 0) {
                 int tokens = 0;
                 for (int r = ra; r < rb; ++r) tokens += b->new_lens_host[r];

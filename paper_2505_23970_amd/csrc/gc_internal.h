@@ -138,9 +138,9 @@ struct SharedSizes {
     int tq_small;  // new tokens per 16-row query tile (0: no small tiles)
     int all;       // every group's shared keys are taken once; else those of the groups in `take`
     uint64_t take[kTakeGroups / 64];
-    // shared keys that are taken once for group g, which shares S
-    __host__ __device__ int taken(int g, int S) const {
-        return all || (g < kTakeGroups && (take[g / 64] >> (g % 64) & 1)) ? S : 0;
+    // shared keys that are taken once for group g, which shares S (words: `take`, or a copy of it)
+    __host__ __device__ int taken(int g, int S, const uint64_t* words) const {
+        return all || (g < kTakeGroups && (words[g / 64] >> (g % 64) & 1)) ? S : 0;
     }
 };
 

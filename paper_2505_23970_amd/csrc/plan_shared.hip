@@ -18,6 +18,8 @@ namespace {
 struct Quad {
     int x[4];
 };
+// (200 requests with 700 small pieces 7.6 us, 9.8 with 256 threads; fewer pieces the same)
+constexpr int kSharedPlanThreads = 1024;
 enum { kBigItems, kBigSlots, kParts, kPlaces };  // kParts, kPlaces: small parts and their places
 
 // Inclusive scan over a wavefront: within rows of 16 lanes, then the rows' totals passed on (as lane
@@ -33,8 +35,8 @@ __device__ __forceinline__ int wave_scan(int x) {
 }
 
 // Exclusive scan of four values per thread over the workgroup, from `base`; base receives the totals on
-// top. (Each call has its own tmp, so that one barrier does.)
-__device__ __forceinline__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThreads / 64], Quad& base) {
+// top. Values behind the first `waves` wavefronts are 0. (Each call has its own tmp, so that one barrier does.)
+__device__ __forceinline__ Quad block_scan4(const Quad v, Quad (&tmp)[kSharedPlanThreads / 64], const int waves, Quad& base) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Quad s = v;
 #pragma unroll
@@ -43,7 +45,7 @@ __device__ __forceinline__ Quad block_scan4(const Quad v, Quad (&tmp)[kPlanThrea
     __syncthreads();
     Quad at = base;
 #pragma nounroll
-    for (int w = 0; w < kPlanThreads / 64; ++w)
+    for (int w = 0; w < waves; ++w)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int t = tmp[w].x[k];
@@ -78,8 +80,9 @@ constexpr int kPlanArrays = 9;  // int32 per request of what the planner derives
 
 template <int BATCH>
 struct SharedPlanLds {
-    Quad tmp[2][kPlanThreads / 64];
-    int bad;
+    Quad tmp[2][kSharedPlanThreads / 64];
+    int bad, wave_bad[kSharedPlanThreads / 64];
+    uint64_t take[kTakeGroups / 64];
     int cu[BATCH + 1], pre[BATCH + 1], first[BATCH + 1], share[BATCH + 1];
     int derived[kPlanArrays][BATCH + 1];
 };
@@ -87,10 +90,10 @@ struct SharedPlanLds {
 // LDS: batches of up to kPlanLdsBatch requests. (Pointers that may be either make every access a flat one:
 // with one kernel for both the plan of 64 requests took 9.4 us instead of 8.7, before the scans changed.)
 template <bool LDS>
-__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedPlanArgs a) {
+__global__ __launch_bounds__(kSharedPlanThreads) void shared_plan_kernel(const SharedPlanArgs a) {
     __shared__ SharedPlanLds<LDS ? kPlanLdsBatch : 1> sm;
     const int tid = threadIdx.x, B = a.batch, G = a.groups;
-    const SharedSizes z = a.z;
+    const SharedSizes& z = a.z;
     auto derived = [&](int k) -> int* {
         if constexpr (LDS) return sm.derived[k];
         else return a.scratch + (size_t)k * (B + 1);
@@ -108,20 +111,6 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
     int* const g_piece = derived(6);
     int* const g_at = derived(7);
     int* const g_taken = derived(8);   // [G] shared keys that are taken once
-    if (tid == 0) {
-        sm.bad = 0;
-        *a.plan_mark = a.mark;
-    }
-    if constexpr (LDS) {  // (G <= B)
-#pragma nounroll
-        for (int r = tid; r <= B; r += kPlanThreads) {
-            sm.cu[r] = a.cu_new_lens[r];
-            if (r < B) sm.pre[r] = a.prefix_lens[r];
-            if (r <= G) sm.first[r] = a.group_first[r];
-            if (r < G) sm.share[r] = a.shared_lens[r];
-        }
-    }
-    __syncthreads();
     const int* const cu = either(sm.cu, a.cu_new_lens);
     const int* const pre = either(sm.pre, a.prefix_lens);
     const int* const first = either(sm.first, a.group_first);
@@ -129,35 +118,50 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
 
     auto empty_all = [&] {
         const SharedItem none{-1, 0, 0, 0, -1, 0, 0, 0, 0, 0, 0, 1};
-        for (int i = tid; i < a.expect_big; i += kPlanThreads) a.big_items[i] = none;
-        for (int i = tid; i < a.pieces; i += kPlanThreads) a.small_items[i] = none;
-        for (int i = tid; i < a.num_runs; i += kPlanThreads) a.run_first[i] = 0;
+        for (int i = tid; i < a.expect_big; i += kSharedPlanThreads) a.big_items[i] = none;
+        for (int i = tid; i < a.pieces; i += kSharedPlanThreads) a.small_items[i] = none;
+        for (int i = tid; i < a.num_runs; i += kSharedPlanThreads) a.run_first[i] = 0;
         if (tid == 0) a.status[0] = 1;
     };
 
-    // 1. the lengths must describe the batch the host checked
+    // 1. the lengths must describe the batch the host checked (up to kPlanLdsBatch requests they go to LDS on the way)
+    // (from LDS: indexed by a lane's group, the arguments would be copied to private memory first, 1.0 us)
+    if (tid < kTakeGroups / 64) sm.take[tid] = z.take[tid];
+    if (tid == 0) {
+        sm.bad = 0;
+        *a.plan_mark = a.mark;
+    }
     {
-        bool bad = tid == 0 && (cu[0] != 0 || cu[B] != a.total_tokens || first[0] != 0 || first[G] != B);
+        bool bad = false;
 #pragma nounroll
-        for (int r = tid; r < B; r += kPlanThreads) {
-            const int P = pre[r], n = (int)((uint32_t)cu[r + 1] - (uint32_t)cu[r]);
-            const uint32_t keys = (uint32_t)P + (uint32_t)n;
-            bad |= P < 0 || cu[r] < 0 || cu[r + 1] < cu[r] || keys > (uint32_t)(INT32_MAX - kBlockN) ||
-                   (n > 0 && (keys + kPage - 1) / kPage > (uint32_t)a.max_blocks);
+        for (int r = tid; r <= B; r += kSharedPlanThreads) {  // (and group r: 1 <= G <= B)
+            // (all loads before the first use: one round trip)
+            const int c = a.cu_new_lens[r], next = a.cu_new_lens[min(r + 1, B)], P = a.prefix_lens[min(r, B - 1)];
+            const int f = a.group_first[min(r, G)], f_next = a.group_first[min(r + 1, G)], S = a.shared_lens[min(r, G - 1)];
+            const uint32_t n = (uint32_t)next - (uint32_t)c, keys = (uint32_t)P + n;
+            bad |= (r == 0 && c != 0) || (r == B && c != a.total_tokens) || (r == 0 && f != 0) || (r == G && f != B);
+            bad |= r < B && (P < 0 || c < 0 || next < c || keys > (uint32_t)(INT32_MAX - kBlockN) ||
+                             (n > 0 && (keys + kPage - 1) / kPage > (uint32_t)a.max_blocks));
+            bad |= r < G && (S < 0 || S % kPage != 0 || S / kPage > a.max_blocks || f < 0 || f_next <= f || f_next > B);
+            if constexpr (LDS) {
+                sm.cu[r] = c;
+                if (r < B) sm.pre[r] = P;
+                if (r <= G) sm.first[r] = f;
+                if (r < G) sm.share[r] = S;
+            }
         }
-#pragma nounroll
-        for (int g = tid; g < G; g += kPlanThreads) {
-            const int S = share[g];
-            bad |= S < 0 || S % kPage != 0 || S / kPage > a.max_blocks || first[g] < 0 || first[g + 1] <= first[g] || first[g + 1] > B;
-        }
-        if (bad) sm.bad = 1;
+        const int any = __any(bad);
+        if ((tid & 63) == 0) sm.wave_bad[tid / 64] = any;
     }
     __syncthreads();
-    if (sm.bad) return empty_all();
+    int bad = 0;
+#pragma unroll
+    for (int w = 0; w < kSharedPlanThreads / 64; ++w) bad |= sm.wave_bad[w];
+    if (bad) return empty_all();
 
     // 2. (A thread owns consecutive requests, and groups.)
-    const int per = ceil_div(B, kPlanThreads), r0 = min(B, tid * per), r1 = min(B, r0 + per);
-    const int per_g = ceil_div(G, kPlanThreads), g0 = min(G, tid * per_g), g1 = min(G, g0 + per_g);
+    const int per = ceil_div(B, kSharedPlanThreads), r0 = min(B, tid * per), r1 = min(B, r0 + per);
+    const int per_g = ceil_div(G, kSharedPlanThreads), g0 = min(G, tid * per_g), g1 = min(G, g0 + per_g);
     auto tokens_of = [&](int g) { return cu[first[g + 1]] - cu[first[g]]; };
 
     //    groups: what each shares, its items, slots and pieces
@@ -166,11 +170,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         Quad v{{0, 0, 0, 0}};
 #pragma nounroll
         for (int g = g0; g < g1; ++g) {
-            const int S = z.taken(g, share[g]);
+            const int S = z.taken(g, share[g], sm.take);
             g_taken[g] = S;
             add_part(v, part_work(S, tokens_of(g), 0, z), true);
         }
-        Quad at = block_scan4(v, sm.tmp[0], total);
+        Quad at = block_scan4(v, sm.tmp[0], ceil_div(G, 64 * per_g), total);
 #pragma nounroll
         for (int g = g0; g < g1; ++g) {
             g_big[g] = at.x[kBigItems];  // (and its first slot: every shared item has one)
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
             const PartWork w = part_work(pre[r] - S + cu[r + 1] - cu[r], cu[r + 1] - cu[r], 0, z);
             add_part(v, w, S > 0 || w.ns > 1);
         }
-        Quad at = block_scan4(v, sm.tmp[1], total);
+        Quad at = block_scan4(v, sm.tmp[1], ceil_div(B, 64 * per), total);
 #pragma nounroll
         for (int r = r0; r < r1; ++r) {
             const int g = group_of[r], S = g_taken[g], n = cu[r + 1] - cu[r];
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
 
     // 3. items (positions are in range when the totals agree; never write outside all the same)
 #pragma nounroll
-    for (int i = tid; i < a.expect_big; i += kPlanThreads) {
+    for (int i = tid; i < a.expect_big; i += kSharedPlanThreads) {
         SharedItem it;
         if (i < shared_total.x[kBigItems]) {
             const int g = last_at_most(g_big, G, i), S = g_taken[g], tokens = tokens_of(g);
@@ -259,11 +263,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const SharedP
         if (it.part >= a.expect_big_slots) it.r = -1;
         a.big_items[i] = it;
     }
-    for (int i = tid; i < a.num_runs; i += kPlanThreads) a.run_first[i] = -1;  // (a run may hold no key tile)
+    for (int i = tid; i < a.num_runs; i += kSharedPlanThreads) a.run_first[i] = -1;  // (a run may hold no key tile)
     __syncthreads();
     const int shared_pieces = shared_total.x[kParts] > 0 ? first_piece(shared_total.x[kParts], shared_total.x[kPlaces], z) : 0;
 #pragma nounroll
-    for (int i = tid; i < a.pieces; i += kPlanThreads) {
+    for (int i = tid; i < a.pieces; i += kSharedPlanThreads) {
         // the last part whose first piece is at most i (a number may be nobody's)
         const bool shared = i < shared_pieces;
         const int o = shared ? last_at_most(g_piece, G, i) : last_at_most(r_piece, B, i);
@@ -296,9 +300,9 @@ size_t shared_scratch_ints(int batch) { return batch <= kPlanLdsBatch ? 1 : (siz
 
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s) {
     if (a.batch <= kPlanLdsBatch)
-        shared_plan_kernel<true><<<1, kPlanThreads, 0, s>>>(a);
+        shared_plan_kernel<true><<<1, kSharedPlanThreads, 0, s>>>(a);
     else
-        shared_plan_kernel<false><<<1, kPlanThreads, 0, s>>>(a);
+        shared_plan_kernel<false><<<1, kSharedPlanThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
