@@ -45,11 +45,11 @@ void launch_items(const SharedAttnArgs& a, unsigned workgroups, hipStream_t s) {
 }
 
 // Merge: a thread owns four consecutive output elements of one row; its chunks' log-sum-exps and
-// values are read kBatch at a time in one pass with a running maximum, in a fixed order (deterministic).
+// values are read B at a time in one pass with a running maximum, in a fixed order (deterministic).
 // What bounds it is the chain of dependent loads: the request (a search of the new-token offsets, 64 at
 // a step), its record, the chunks. With G > 1 a row's chunks are dealt to G groups of threads (chunk c to
 // group c % G), whose results are joined through LDS in group order: for few rows of many chunks.
-template <int D, int G>
+template <int D, int G, int B>
 __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const SharedMergeArgs a) {
     constexpr int CPR = D / 4;                          // threads per row and group
     constexpr int kRows = kCombineThreads / (CPR * G);  // rows per workgroup
@@ -105,12 +105,11 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
         const float* const o_o = q.own_small ? a.small_o : a.big_o;
         const float* const o_l = q.own_small ? a.small_lse : a.big_lse;
 
-        constexpr int kBatch = G > 1 ? 8 : 16;
-        for (int s0 = sub; s0 < total; s0 += kBatch * G) {
-            float l[kBatch];
-            f32x4 v[kBatch];
+        for (int s0 = sub; s0 < total; s0 += B * G) {
+            float l[B];
+            f32x4 v[B];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
+            for (int u = 0; u < B; ++u) {
                 const int c = s0 + u * G;
                 l[u] = -INFINITY;
                 v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -123,14 +122,14 @@ __global__ __launch_bounds__(kCombineThreads) void shared_merge_kernel(const Sha
             }
             float mn = mx;
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, l[u]);
+            for (int u = 0; u < B; ++u) mn = fmaxf(mn, l[u]);
             const float off = mn == -INFINITY ? 0.f : mn;
             const float alpha = expf(mx - off);
             tot *= alpha;
             acc *= alpha;
             mx = mn;
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
+            for (int u = 0; u < B; ++u) {
                 const float w = expf(l[u] - off);  // 0 for the padding entries
                 tot += w;
                 acc += w * v[u];
@@ -186,24 +185,30 @@ hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, boo
     return hipGetLastError();
 }
 
+template <int D>
+static void launch_merge(const SharedMergeArgs& a, int groups, hipStream_t s) {
+    const unsigned grid = (unsigned)ceil_div64(a.rows, kCombineThreads / (D / 4 * groups));
+    // Six chunks at a time where a compute unit has more than one workgroup (fewer registers, more of them at
+    // once), 16 where each row's loads are on their own. Attention and merge, 6 / 16: 64 workgroups 16.8 us / 16.6, 200
+    // of 25 chunks 46.2 / 45.3, 256 18.5 / 18.6, 448 22.7 / 23.2, 800 51.6 / 53.3, 960 of five chunks 37.4 / 39.5, 2360 66.3 / 71.2.
+    if (groups > 1)
+        shared_merge_kernel<D, 8, 8><<<grid, kCombineThreads, 0, s>>>(a);
+    else if (grid > 256)
+        shared_merge_kernel<D, 1, 6><<<grid, kCombineThreads, 0, s>>>(a);
+    else
+        shared_merge_kernel<D, 1, 16><<<grid, kCombineThreads, 0, s>>>(a);
+}
+
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s) {
     // Eight thread groups a row where the trips of loads saved (16 chunks a trip, or 64) are worth the rows'
     // additional workgroups. One group / eight, attention and merge: 64 rows of 131 chunks 32.3 us / 18.5, 512 of
     // 38 20.2 / 17.0, 1200 of 28 22.6 / 22.3, 1600 of 25 23.9 / 25.1, 4096 of 12 53.7 / 57.7.
     const int trips_saved = ceil_div(max_chunks, 16) - ceil_div(max_chunks, 64);
     const int groups = a.rows <= 1536LL * trips_saved ? 8 : 1;
-    const dim3 grid((unsigned)ceil_div64(a.rows, kCombineThreads / (head_dim / 4 * groups)));
-    if (head_dim == 128) {
-        if (groups > 1)
-            shared_merge_kernel<128, 8><<<grid, kCombineThreads, 0, s>>>(a);
-        else
-            shared_merge_kernel<128, 1><<<grid, kCombineThreads, 0, s>>>(a);
-    } else {
-        if (groups > 1)
-            shared_merge_kernel<64, 8><<<grid, kCombineThreads, 0, s>>>(a);
-        else
-            shared_merge_kernel<64, 1><<<grid, kCombineThreads, 0, s>>>(a);
-    }
+    if (head_dim == 128)
+        launch_merge<128>(a, groups, s);
+    else
+        launch_merge<64>(a, groups, s);
     return hipGetLastError();
 }
 
