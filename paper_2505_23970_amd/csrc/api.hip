@@ -867,13 +867,23 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
 //     360 and 480 shared items, 48 with 240). So the smallest chunk whose items make a whole number of such
 //     rounds: an item longer than two thirds of the chunk fills a slot, and all of them the slots by their
 //     key tiles and kItemSteps more each. Where reading the small tiles takes longer than that, the load alone
-//     decides (128 answers on 16k-token contexts: 304 items of 45 key tiles 132 us, 240 of 60 143).
+//     decides (128 answers on 16k-token contexts: 304 items of 45 key tiles 132 us, 240 of 60 143), and an item
+//     may take 0.7 of that reading (64 answers on 4000 tokens and 300 of their own 30.1 us, with the smallest such chunk
+//     33.7; 135 on 6000 and 1500 243 / 274; 183 at d = 64 31.4 / 43.6).
+//   - Without many small tiles, from kLongSteps key tiles a slot on, two workgroups a unit at d = 128 too: their partial
+//     rows are few beside that (13 questions of 11 tokens on 13300 over 8-bit pools 69.0 us, one a unit 76.9; 57 answers on
+//     26835 79.0 / 77.1).
+//   - More query tiles than slots: no chunk longer than a third of the longest part, or than a fifth where that has
+//     more than 64 key tiles. Whole parts run in step, two workgroups a unit at the same phase (48 questions of 20 tokens on 32768
+//     1074 us, whole 1431; over 8-bit pools 1206 / 1626; 40 of 30 on 8000 at d = 64 113 / 119).
+//   - A few items more than slots are a round more: up to a quarter longer chunks where that avoids it (16 questions of 10
+//     tokens on 3000 at d = 64 21.8 us / 24.1, 5 of 29 on 13055 38.1 / 42.5).
 //   - At least kMinChunk key tiles (16 answers of the 8B model on 2000 tokens: 16.4 us with 4, 15.8 with 3, 16.6 with
 //     2, 17.4 with 6, 20.4 with 8).
 //   - Small tiles: equal runs, one for each of the wavefronts that the remaining workgroup slots hold, of at least
 //     kMinRun places. Where some units hold two 128-row workgroups, two thirds of that, because the rest of
 //     the small workgroups follow when the first end (132 us; 145 with whole runs).
-constexpr int kMinChunk = 4, kMinRun = 8, kItemSteps = 4;
+constexpr int kMinChunk = 4, kMinRun = 8, kItemSteps = 4, kLongSteps = 20;
 
 // The batch's work: 128-row parts (the first kKept of them kept) and the places of the small ones.
 struct SharedLoad {
@@ -908,10 +918,11 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     SharedLoad l;
     shared_load(b, s, *z, &l);
     int64_t slots = geo->head_dim == 128 ? cus : 2 * cus, big = 0;
-    if (l.units * heads > slots) slots = 2 * cus;
-    // reading the small tiles takes longer than the 128-row ones
     const double small_us = l.small_tiles * heads * (double)(gc::kDecN * geo->head_dim * 2 * (pk.fp8 ? 1 : 2)) / 5.6e6;
-    const bool by_load = small_us > l.steps * heads * 1.4 / cus;
+    const double big_us = l.steps * heads * 1.4 / cus;
+    const bool by_load = small_us > big_us;  // reading the small tiles takes longer than the 128-row ones
+    const bool rounds = l.units * heads > slots;
+    if (rounds || (small_us < 0.1 * big_us && l.steps * heads >= 2 * cus * kLongSteps)) slots = 2 * cus;
     auto fits = [&](int c) {
         z->chunk = gc::divisor(c);
         big = 0;
@@ -936,6 +947,21 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
         else lo = mid + 1;
     }
     fits(lo);
+    if (rounds) {
+        const int third = gc::ceil_div(l.longest, 3), fifth = gc::ceil_div(l.longest, 5);
+        const int most = third < 64 ? third : fifth > 64 ? fifth : 64;
+        if (lo > most) lo = most;
+    }
+    if (by_load) {
+        const int as_long = (int)(0.7 * small_us / (geo->head_dim == 128 ? 1.4 : 0.75));
+        if (as_long > lo) lo = as_long < l.longest ? as_long : l.longest;
+    }
+    fits(lo);
+    if (!rounds && !by_load && slots == 2 * cus && big * heads > slots && big * heads <= slots * 5 / 4) {
+        const int before = lo;
+        while (big * heads > slots && lo < l.longest && lo * 4 < before * 5) fits(++lo);
+        if (big * heads > slots) fits(before);
+    }
     int64_t wgs = 2 * cus - big * heads;
     if (wgs < cus) wgs = cus;
     const int64_t waves = gc::shared_rings(pk.fp8) * wgs;
