@@ -808,10 +808,11 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
 
 // Which groups' shared keys are taken once: those that it saves time by the estimates below, if together they
 // save more than the merge costs. The plain attention reads S keys for every request, its 16-row tiles from L2
-// at about 20 TB/s over all heads, its 128-row tiles at the matrix cores' pace; taken once, they cost a read
-// from HBM or the pace of the group's own 128-row tiles, and every row two fp32 partial rows, written and
-// read. Paces: us of a compute unit per 128-row tile and 64 keys (48 requests of 20 tokens on 32768 shared ones, the
-// plain attention / this one: 1316 us / 914, 8-bit pools 1763 / 988; at d = 64 533 / 288 and 665 / 341).
+// at about 20 TB/s over all heads (13 of 8-bit codes: 136 answers on 641 tokens 31.6 us, taken once 25.5), its
+// 128-row tiles at the matrix cores' pace; taken once, they cost a read from HBM or the pace of the group's own
+// 128-row tiles, and every row two fp32 partial rows, written and read. Paces: us of a compute unit per 128-row
+// tile and 64 keys (48 requests of 20 tokens on 32768 shared ones, the plain attention / this one: 1316 us /
+// 1074, 8-bit pools 1763 / 1206; at d = 64 533 / 288 and 665 / 341).
 // Short launches of 128-row tiles are bound by their latency, which the finer chunks here make shorter: up to 64
 // tiles over all heads and 4096 of their key tiles, groups of 256 shared keys or more are taken (16.0 us / 13.2
 // for two requests of 3 tokens on 513, 18.8 / 15.5 for 27 on 796, 21.7 / 17.9 for 7 of 19 tokens; at 16384 key
@@ -824,6 +825,7 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
     if (z->all) return;
     const double heads = geo->num_kv_heads, D = geo->head_dim;
     const double key_bytes = heads * D * 2 * (pk.fp8 ? 1 : 2);
+    const double l2 = pk.fp8 ? 13e6 : 20e6;                  // bytes in a us
     const double step = heads / device_cus() / gc::kBlockN;  // of a 128-row tile, per key
     const double plain_pace = D == 128 ? (pk.fp8 ? 1.13 : 0.85) : (pk.fp8 ? 0.86 : 0.69);
     const double shared_pace = D == 128 ? (pk.fp8 ? 1.03 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
@@ -844,7 +846,7 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
         all_steps += tiles * heads * S / gc::kBlockN;
         if (S <= 0) continue;
         if (tiles >= 2 && S >= kShortKeys) brief[g / 64] |= 1ull << (g % 64);
-        const double plain = S * (small * key_bytes / 20e6 + tiles * step * plain_pace);
+        const double plain = S * (small * key_bytes / l2 + tiles * step * plain_pace);
         const double read = key_bytes / 5.6e6;
         const double paced = tokens <= z->tq_small ? 0 : gc::ceil_div64(tokens, z->tq.d) * step * shared_pace;
         const double rows = tokens * geo->num_q_heads * D * 4 * 4 / 4e6;
