@@ -431,6 +431,7 @@ gc::PlanArgs plan_args(const gc_geometry* geo, const gc_batch* b, const Shape& s
     a.combines = at<gc::CombineItem>(ws, pl.layout.combine_off);
     a.status = at<int32_t>(ws, pl.layout.status_off);
     a.queues = at<int32_t>(ws, pl.layout.queue_off);
+    a.shared_mark = at<int32_t>(ws, gc::kMarkOffset);
     a.batch = b->batch;
     a.tq = sh.tq;
     a.chunk = pl.chunk;
@@ -1066,7 +1067,7 @@ uint64_t shared_mark(const gc_geometry* geo, const gc_batch* b, const gc_shared*
         add(v);
     for (uint64_t t : p.z.take) add((int64_t)t);
     add(p.z.all);
-    return x;
+    return x != 0 ? x : 1;
 }
 
 gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh,

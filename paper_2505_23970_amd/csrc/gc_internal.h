@@ -205,7 +205,8 @@ inline int64_t append_pages_host(const int32_t* prefix, const int32_t* n, int ba
 
 // ---------------------------------------------------------------- workspace
 constexpr size_t kStatusOffset = 0;  // byte offset of the planner's status word in the workspace
-// A shared-prefix plan's mark in that block: a hash of what the plan was made for.
+// A shared-prefix plan's mark in that block: a hash of what the plan was made for, never 0. A plain plan
+// sets it to 0, since its items lie where a shared plan's records and items were.
 constexpr size_t kMarkOffset = 128;
 // Work queues of the resident attention launch: kQueues ticket counters and one exit
 // counter (int32) in the workspace's leading 256-byte block, zeroed by the planner and
@@ -273,6 +274,7 @@ struct PlanArgs {
     CombineItem* combines;    // [combines]
     int32_t* status;          // status[0] = 0 when the device lengths matched the host's
     int32_t* queues;          // [kQueues + 1] work-queue counters, zeroed here
+    int32_t* shared_mark;     // [2] the mark of a shared-prefix plan that was here before, zeroed here
     int32_t batch, tq, chunk, block_n;
     int32_t expect_items, expect_combines, expect_partials;
     int32_t total_tokens;     // the host's T (= cu_new_lens[batch] on the device)
