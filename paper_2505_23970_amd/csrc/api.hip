@@ -760,6 +760,7 @@ struct SharedPlan {
     int64_t pieces = 0, runs = 0;           // of the small tiles' sequence
     int max_shared = 0, max_own = 0;        // the most chunks of a part
     gc::SharedLayout layout{};
+    uint64_t mark = 0;                      // (see shared_mark)
 };
 
 gc_status check_shared(const gc_geometry* geo, const gc_batch* b, const gc_shared* s) {
@@ -1033,6 +1034,26 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
     return GC_OK;
 }
 
+// What a plan is made for: a run finds the plan's mark in the workspace or does nothing, so that a workspace
+// with another plan, or none, is no list of garbage items. A hash of every length and group (the next step of a
+// decoding loop has the same totals, and its items end a key later), the pool kind and what the host chose.
+uint64_t shared_mark(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, const Shape& sh,
+                     const SharedPlan& p) {
+    uint64_t x = 0xcbf29ce484222325ull;
+    auto add = [&](int64_t v) { x = (x ^ (uint64_t)v) * 0x100000001b3ull ^ (x >> 29); };
+    auto add2 = [&](int32_t u, int32_t v) { add((int64_t)u << 32 | (uint32_t)v); };
+    for (int64_t v : {(int64_t)geo->num_q_heads, (int64_t)geo->num_kv_heads, (int64_t)geo->head_dim,
+                      (int64_t)geo->max_blocks_per_seq, (int64_t)b->batch, (int64_t)s->groups, (int64_t)pk.fp8, sh.total_tokens,
+                      p.big, p.big_shared, p.big_slots, p.parts, p.places, p.pieces, p.runs, (int64_t)p.z.chunk.d,
+                      (int64_t)p.z.run.d, (int64_t)p.layout.total})
+        add(v);
+    for (uint64_t t : p.z.take) add((int64_t)t);
+    add(p.z.all);
+    for (int r = 0; r < b->batch; ++r) add2(b->prefix_lens_host[r], b->new_lens_host[r]);
+    for (int g = 0; g < s->groups; ++g) add2(s->group_first_host[g], s->shared_lens_host[g]);
+    return x != 0 ? x : 1;
+}
+
 // Every check that needs no tensors, and the plan. Where no group shares, the plain attention's shape and plan.
 gc_status shared_checked(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,
                          const PoolKind& pk, Shape* sh, SharedPlan* spl, Plan* pl) {
@@ -1045,29 +1066,16 @@ gc_status shared_checked(const gc_geometry* geo, const gc_batch* b, const gc_sha
     if (st != GC_OK || sh->total_tokens == 0) return st;
     if (s->group_first_dev == nullptr || s->shared_lens_dev == nullptr) return GC_ERR_NULL_ARG;
     st = make_shared_plan(geo, b, s, o, *sh, pk, spl);
-    if (st != GC_OK || spl->any) return st;
-    return plan_checked(geo, b, o, sh, pl);
+    if (st != GC_OK) return st;
+    if (!spl->any) return plan_checked(geo, b, o, sh, pl);
+    spl->mark = shared_mark(geo, b, s, pk, *sh, *spl);
+    return GC_OK;
 }
 
 gc_status check_shared_workspace(const SharedPlan& spl, const Plan& pl, const void* ws, size_t bytes) {
     if (!aligned16(ws)) return GC_ERR_WORKSPACE;
     if (!spl.any) return check_workspace(pl, ws, bytes);
     return ws == nullptr || bytes < spl.layout.total ? GC_ERR_WORKSPACE : GC_OK;
-}
-
-// What a plan is made for: a run finds the plan's mark in the workspace or does nothing, so that a workspace
-// with another plan, or none, is no list of garbage items.
-uint64_t shared_mark(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh, const SharedPlan& p) {
-    uint64_t x = 0xcbf29ce484222325ull;
-    auto add = [&](int64_t v) { x = (x ^ (uint64_t)v) * 0x100000001b3ull ^ (x >> 29); };
-    for (int64_t v : {(int64_t)geo->num_q_heads, (int64_t)geo->num_kv_heads, (int64_t)geo->head_dim,
-                      (int64_t)geo->max_blocks_per_seq, (int64_t)b->batch, (int64_t)s->groups, sh.total_tokens, p.big,
-                      p.big_shared, p.big_slots, p.parts, p.places, p.pieces, p.runs, (int64_t)p.z.chunk.d,
-                      (int64_t)p.z.run.d, (int64_t)p.layout.total})
-        add(v);
-    for (uint64_t t : p.z.take) add((int64_t)t);
-    add(p.z.all);
-    return x != 0 ? x : 1;
 }
 
 gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh,
@@ -1079,7 +1087,7 @@ gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const g
     a.shared_lens = s->shared_lens_dev;
     a.status = at<int32_t>(ws, gc::kStatusOffset);
     a.plan_mark = at<uint64_t>(ws, gc::kMarkOffset);
-    a.mark = shared_mark(geo, b, s, sh, spl);
+    a.mark = spl.mark;
     a.scratch = at<int32_t>(ws, spl.layout.scratch_off);
     a.reqs = at<gc::SharedReq>(ws, spl.layout.reqs_off);
     a.big_items = at<gc::SharedItem>(ws, spl.layout.big_off);
@@ -1099,8 +1107,8 @@ gc_status enqueue_shared_plan(const gc_geometry* geo, const gc_batch* b, const g
     return gc::launch_shared_plan(a, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
-gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const Shape& sh, const SharedPlan& spl,
-                             const void* q, const void* k_pool, const void* v_pool, float scale, void* out, float* lse,
+gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh, const SharedPlan& spl, const void* q,
+                             const void* k_pool, const void* v_pool, float scale, void* out, float* lse,
                              void* ws, hipStream_t stream, const PoolKind& pk) {
     gc::SharedAttnArgs a{};
     a.q = static_cast<const uint16_t*>(q);
@@ -1129,7 +1137,7 @@ gc_status enqueue_shared_run(const gc_geometry* geo, const gc_batch* b, const gc
     a.small = (int32_t)(spl.runs * geo->num_kv_heads);
     a.pieces = (int32_t)spl.pieces;
     a.plan_mark = at<uint64_t>(ws, gc::kMarkOffset);
-    a.mark = shared_mark(geo, b, s, sh, spl);
+    a.mark = spl.mark;
     if (gc::launch_attention_shared(a, geo->head_dim, pk.fp8, stream) != hipSuccess) return GC_ERR_HIP;
     gc::SharedMergeArgs m{};
     m.out = a.out;
@@ -1175,7 +1183,7 @@ gc_status run_shared(const gc_geometry* geo, const gc_batch* batch, const gc_sha
                      : enqueue_plan(geo, batch, sh, pl, workspace, stream);
         if (st != GC_OK) return st;
     }
-    return spl.any ? enqueue_shared_run(geo, batch, shared, sh, spl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk)
+    return spl.any ? enqueue_shared_run(geo, batch, sh, spl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk)
                    : enqueue_run(geo, batch, sh, pl, q, k_pool, v_pool, scale, out, lse, workspace, stream, pk);
 }
 
