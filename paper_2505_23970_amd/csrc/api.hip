@@ -957,8 +957,8 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
         if (lo > most) lo = most;
     }
     if (by_load) {
-        const int as_long = (int)(0.7 * small_us / (geo->head_dim == 128 ? 1.4 : 0.75));
-        if (as_long > lo) lo = as_long < l.longest ? as_long : l.longest;
+        const double as_long = 0.7 * small_us / (geo->head_dim == 128 ? 1.4 : 0.75);
+        if (as_long > lo) lo = as_long < l.longest ? (int)as_long : l.longest;
     }
     fits(lo);
     if (!rounds && !by_load && slots == 2 * cus && big * heads > slots && big * heads <= slots * 5 / 4) {
@@ -971,7 +971,8 @@ void choose_shared_chunks(const gc_geometry* geo, const gc_batch* b, const gc_sh
     const int64_t waves = gc::shared_rings(pk.fp8) * wgs;
     int64_t run = waves >= heads ? gc::ceil_div64(l.places, waves / heads) : gc::ceil_div64(l.places * heads, waves);
     if (big * heads > cus) run = run * 2 / 3;
-    z->run = gc::divisor(run > kMinRun ? (int)run : kMinRun);
+    // (long before the upper bound the places are more than a launch takes)
+    z->run = gc::divisor((int)std::min<int64_t>(std::max<int64_t>(run, kMinRun), INT32_MAX / 2));
 }
 
 gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const gc_plan_options* o,

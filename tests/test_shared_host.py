@@ -143,3 +143,12 @@ def test_groups_of_the_binding():
     gc.SharedPrefixes(batch, [2], [16])
     with pytest.raises(ValueError):
         gc.SharedPrefixes(batch, [2], [32])
+
+
+def test_runs_of_more_places_than_32_bits_hold(lib):
+    """48 requests of 2^31 - 113 cached tokens at 32768 heads: equal runs of 2^37 places, whose low 32 bits are all 0.
+    More work than a launch holds; no division by the truncated length."""
+    g = geo(Hq=32768, Hkv=32768, NB=1 << 20, maxb=1 << 27)
+    b = HostBatch([2 ** 31 - 113] * 48, [1] * 48)
+    assert size(lib, g, b, HostShared([0, 48], [16], policy=gc.SHARE_ALWAYS))[0] == -2
+    assert size(lib, g, b, HostShared([0, 48], [16], policy=gc.SHARE_AUTO)) == (0, plain_size(lib, g, b))
