@@ -1012,7 +1012,9 @@ gc_status make_shared_plan(const gc_geometry* geo, const gc_batch* b, const gc_s
     }
     const int64_t most = gc::kMaxWorkgroups / geo->num_kv_heads - 64;
     if (pl->big + pl->pieces > most || pl->places > (int64_t)INT32_MAX - z.run.d ||
-        sh.total_tokens * geo->num_q_heads / 8 >= gc::kMaxWorkgroups)
+        sh.total_tokens * geo->num_q_heads / 8 >= gc::kMaxWorkgroups ||
+        gc::shared_merge_workgroups(sh.total_tokens * geo->num_q_heads, geo->head_dim, pl->max_shared + pl->max_own) >
+            (int64_t)UINT32_MAX / gc::kCombineThreads)
         return GC_ERR_BAD_SHAPE;
     gc::SharedLayout& l = pl->layout;
     size_t off = 256;  // (the status word leads, as in the plain workspace)

@@ -185,13 +185,25 @@ hipError_t launch_attention_shared(const SharedAttnArgs& args, int head_dim, boo
     return hipGetLastError();
 }
 
+// Thread groups of a row in the merge: eight where the trips of loads saved (16 chunks a trip, or 64) are worth the
+// rows' additional workgroups. One group / eight, attention and merge: 64 rows of 131 chunks 32.3 us / 18.5, 512 of
+// 38 20.2 / 17.0, 1200 of 28 22.6 / 22.3, 1600 of 25 23.9 / 25.1, 4096 of 12 53.7 / 57.7.
+static int merge_groups(int64_t rows, int max_chunks) {
+    const int trips_saved = ceil_div(max_chunks, 16) - ceil_div(max_chunks, 64);
+    return rows <= 1536LL * trips_saved ? 8 : 1;
+}
+
+int64_t shared_merge_workgroups(int64_t rows, int head_dim, int max_chunks) {
+    return ceil_div64(rows, kCombineThreads / (head_dim / 4 * merge_groups(rows, max_chunks)));
+}
+
 template <int D>
-static void launch_merge(const SharedMergeArgs& a, int groups, hipStream_t s) {
-    const unsigned grid = (unsigned)ceil_div64(a.rows, kCombineThreads / (D / 4 * groups));
+static void launch_merge(const SharedMergeArgs& a, int max_chunks, hipStream_t s) {
+    const unsigned grid = (unsigned)shared_merge_workgroups(a.rows, D, max_chunks);
     // Six chunks at a time where a compute unit has more than one workgroup (fewer registers, more of them at
     // once), 16 where each row's loads are on their own. Attention and merge, 6 / 16: 64 workgroups 16.8 us / 16.6, 200
     // of 25 chunks 46.2 / 45.3, 256 18.5 / 18.6, 448 22.7 / 23.2, 800 51.6 / 53.3, 960 of five chunks 37.4 / 39.5, 2360 66.3 / 71.2.
-    if (groups > 1)
+    if (merge_groups(a.rows, max_chunks) > 1)
         shared_merge_kernel<D, 8, 8><<<grid, kCombineThreads, 0, s>>>(a);
     else if (grid > 256)
         shared_merge_kernel<D, 1, 6><<<grid, kCombineThreads, 0, s>>>(a);
@@ -200,15 +212,10 @@ static void launch_merge(const SharedMergeArgs& a, int groups, hipStream_t s) {
 }
 
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s) {
-    // Eight thread groups a row where the trips of loads saved (16 chunks a trip, or 64) are worth the rows'
-    // additional workgroups. One group / eight, attention and merge: 64 rows of 131 chunks 32.3 us / 18.5, 512 of
-    // 38 20.2 / 17.0, 1200 of 28 22.6 / 22.3, 1600 of 25 23.9 / 25.1, 4096 of 12 53.7 / 57.7.
-    const int trips_saved = ceil_div(max_chunks, 16) - ceil_div(max_chunks, 64);
-    const int groups = a.rows <= 1536LL * trips_saved ? 8 : 1;
     if (head_dim == 128)
-        launch_merge<128>(a, groups, s);
+        launch_merge<128>(a, max_chunks, s);
     else
-        launch_merge<64>(a, groups, s);
+        launch_merge<64>(a, max_chunks, s);
     return hipGetLastError();
 }
 

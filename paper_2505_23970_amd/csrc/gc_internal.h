@@ -390,6 +390,7 @@ hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
 hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool fp8, hipStream_t s);
 // max_chunks: the most chunks of any row
+int64_t shared_merge_workgroups(int64_t rows, int head_dim, int max_chunks);  // at most UINT32_MAX / kCombineThreads
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s);
 // max_splits: the most key chunks of any split query tile
 hipError_t launch_combine(const CombineArgs& a, int head_dim, int64_t num_combines, int max_splits, hipStream_t s);

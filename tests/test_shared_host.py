@@ -152,3 +152,12 @@ def test_runs_of_more_places_than_32_bits_hold(lib):
     b = HostBatch([2 ** 31 - 113] * 48, [1] * 48)
     assert size(lib, g, b, HostShared([0, 48], [16], policy=gc.SHARE_ALWAYS))[0] == -2
     assert size(lib, g, b, HostShared([0, 48], [16], policy=gc.SHARE_AUTO)) == (0, plain_size(lib, g, b))
+
+
+def test_more_merge_workgroups_than_a_launch_takes(lib):
+    """20 million rows beside one of 312501 chunks: the merge deals a row's chunks to eight thread groups, a workgroup a
+    row at d = 128. Refused before the plan and the items are on the stream; half the rows fit."""
+    for requests, status in ((200000, -2), (100000, 0)):
+        b = HostBatch([64] * requests + [20_000_000], [100] * requests + [1])
+        g = geo(Hq=1, Hkv=1, NB=1 << 20, maxb=1 << 21)
+        assert size(lib, g, b, HostShared([0, requests + 1], [16]), gc.PlanOptions(1, 0))[0] == status
