@@ -323,8 +323,8 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
  */
 typedef enum gc_share_policy {
     GC_SHARE_AUTO = 0,  /* take a group's shared keys once where that saves time (an estimate by
-                           lengths, heads and pool type; a batch of more than 512 groups takes
-                           all); a batch without such a group runs as the plain attention */
+                           lengths, heads and pool type; of more than 512 groups all or none); a
+                           batch without such a group runs as the plain attention */
     GC_SHARE_ALWAYS = 1 /* take them once whatever it costs (tests, measurements) */
 } gc_share_policy;
 

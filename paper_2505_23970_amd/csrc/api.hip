@@ -819,15 +819,21 @@ void for_each_part(const gc_batch* b, const gc_shared* s, const gc::SharedSizes&
 // tiles over all heads and 4096 of their key tiles, groups of 256 shared keys or more are taken (16.0 us / 13.2
 // for two requests of 3 tokens on 513, 18.8 / 15.5 for 27 on 796, 21.7 / 17.9 for 7 of 19 tokens; at 16384 key
 // tiles 117 / 128).
+// More than kTakeGroups groups (a choice of single ones would not fit the kernel's argument): all or none, by the
+// sum of what each saves or loses, with the plain attention's reads at the memory's rate too: that many prefixes are not
+// in L2 when the next request of a group comes (520 pairs of answers on 2000 tokens 1504 us / 1019). Against the better of
+// both ways 60 such batches take 1.05 times the time, all taken 1.40, none 1.27.
 constexpr double kShareGain = 2.0, kShareGainTiles = 6.0;  // us: batches of small tiles; with 128-row own parts
 constexpr int kShortTiles = 64, kShortSteps = 4096, kShortKeys = 256;
 
 void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s, const PoolKind& pk, gc::SharedSizes* z) {
-    z->all = s->policy == GC_SHARE_ALWAYS || s->groups > gc::kTakeGroups;
+    z->all = s->policy == GC_SHARE_ALWAYS;
     if (z->all) return;
+    const bool many = s->groups > gc::kTakeGroups;
     const double heads = geo->num_kv_heads, D = geo->head_dim;
     const double key_bytes = heads * D * 2 * (pk.fp8 ? 1 : 2);
-    const double l2 = pk.fp8 ? 13e6 : 20e6;                  // bytes in a us
+    const double hbm = 5.6e6;                                // bytes in a us
+    const double l2 = many ? hbm : pk.fp8 ? 13e6 : 20e6;
     const double step = heads / device_cus() / gc::kBlockN;  // of a 128-row tile, per key
     const double plain_pace = D == 128 ? (pk.fp8 ? 1.13 : 0.85) : (pk.fp8 ? 0.86 : 0.69);
     const double shared_pace = D == 128 ? (pk.fp8 ? 1.03 : 0.95) : (pk.fp8 ? 0.71 : 0.62);
@@ -846,17 +852,21 @@ void choose_groups(const gc_geometry* geo, const gc_batch* b, const gc_shared* s
         }
         all_tiles += tiles * heads;
         all_steps += tiles * heads * S / gc::kBlockN;
-        if (S <= 0) continue;
-        if (tiles >= 2 && S >= kShortKeys) brief[g / 64] |= 1ull << (g % 64);
+        if (S <= 0 || tokens == 0) continue;
+        if (!many && tiles >= 2 && S >= kShortKeys) brief[g / 64] |= 1ull << (g % 64);
         const double plain = S * (small * key_bytes / l2 + tiles * step * plain_pace);
-        const double read = key_bytes / 5.6e6;
+        const double read = key_bytes / hbm;
         const double paced = tokens <= z->tq_small ? 0 : gc::ceil_div64(tokens, z->tq.d) * step * shared_pace;
         const double rows = tokens * geo->num_q_heads * D * 4 * 4 / 4e6;
         const double saved = plain - S * (read > paced ? read : paced) - rows;
-        if (saved < 0.2) continue;
-        z->take[g / 64] |= 1ull << (g % 64);
+        if (!many && saved < 0.2) continue;
+        if (!many) z->take[g / 64] |= 1ull << (g % 64);
         gain += saved;
         any_tiles |= tiles > 0;
+    }
+    if (many) {
+        z->all = gain >= (any_tiles ? kShareGainTiles : kShareGain);
+        return;
     }
     if (gain < (any_tiles ? kShareGainTiles : kShareGain))
         for (uint64_t& t : z->take) t = 0;

@@ -130,7 +130,7 @@ __host__ __device__ inline int quick_div(int a, int d) {
 #endif
 }
 
-constexpr int kTakeGroups = 512;  // (a batch of more groups takes all)
+constexpr int kTakeGroups = 512;  // (a batch of more groups takes all or none)
 struct SharedSizes {
     Divisor tq;    // new tokens per 128-row query tile
     Divisor chunk; // 64-key tiles per chunk of a 128-row tile

@@ -161,3 +161,26 @@ def test_more_merge_workgroups_than_a_launch_takes(lib):
         b = HostBatch([64] * requests + [20_000_000], [100] * requests + [1])
         g = geo(Hq=1, Hkv=1, NB=1 << 20, maxb=1 << 21)
         assert size(lib, g, b, HostShared([0, requests + 1], [16]), gc.PlanOptions(1, 0))[0] == status
+
+
+@pytest.mark.parametrize("sizes,lens,n,taken", [
+    ([1] * 513, [640] * 513, 1, False),                # requests alone: 304 us, taken 372
+    ([2] * 520, [64] * 520, 1, False),                 # four pages of two requests each: 175, 219
+    ([1] * 520, [512] * 520, 20, False),               # query tiles of one request: 477, 1204
+    ([2] * 520, [1008] * 520, 20, False),              # 1441, 2330
+    ([2] * 520 + [1] * 3000, [2000] * 520 + [2000] * 3000, [1] * 1040 + [0] * 3000, True),   # members without new tokens
+    ([2] * 520, [2000] * 520, 1, True),                # 1504, 1019
+    ([8] * 520, [1024] * 520, 1, True),                # 2648, 1217
+    ([100] + [1] * 600, [8192] + [16] * 600, 1, True),   # one group gains more than the others lose: 229, 155
+    ([20] + [1] * 600, [1024] + [512] * 600, 1, False),  # and less: 297, 368
+])
+def test_what_the_policy_takes_of_many_groups(lib, sizes, lens, n, taken):
+    """More groups than the policy chooses from one by one: all or none (us at 64 and 8 heads, d = 128, bf16)."""
+    P = np.repeat(lens, sizes) + 160
+    g, b = geo(Hq=64, Hkv=8, NB=1000000, maxb=600), HostBatch(P, np.broadcast_to(n, P.shape))
+    first = np.concatenate([[0], np.cumsum(sizes)])
+    st, auto = size(lib, g, b, HostShared(first, lens, policy=gc.SHARE_AUTO))
+    assert st == 0
+    assert (auto != plain_size(lib, g, b)) == taken
+    if taken:
+        assert auto == size(lib, g, b, HostShared(first, lens, policy=gc.SHARE_ALWAYS))[1]
