@@ -324,7 +324,8 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
 typedef enum gc_share_policy {
     GC_SHARE_AUTO = 0,  /* take a group's shared keys once where that saves time (an estimate by
                            lengths, heads and pool type; of more than 512 groups all or none); a
-                           batch without such a group runs as the plain attention */
+                           batch without such a group, or of more work than one launch holds
+                           that way, runs as the plain attention */
     GC_SHARE_ALWAYS = 1 /* take them once whatever it costs (tests, measurements) */
 } gc_share_policy;
 
@@ -353,7 +354,7 @@ typedef struct gc_shared {
  * `lse`, sharing of a workspace by runs, errors, is as for those calls; further errors:
  * GC_ERR_NULL_ARG for a missing array, GC_ERR_BAD_SHAPE for groups or shared lengths outside
  * the above, for q, pools or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE)
- * and for a batch of more work than one launch holds, GC_ERR_BLOCK_TABLE for a shared
+ * and for a batch of more work than one launch holds (GC_SHARE_ALWAYS), GC_ERR_BLOCK_TABLE for a shared
  * length past the block-table row.
  */
 gc_status gc_shared_prefix_workspace_size(const gc_geometry* geo, const gc_batch* batch,

@@ -1079,7 +1079,8 @@ gc_status shared_checked(const gc_geometry* geo, const gc_batch* b, const gc_sha
     if (st != GC_OK || sh->total_tokens == 0) return st;
     if (s->group_first_dev == nullptr || s->shared_lens_dev == nullptr) return GC_ERR_NULL_ARG;
     st = make_shared_plan(geo, b, s, o, *sh, pk, spl);
-    if (st != GC_OK) return st;
+    if (st != GC_OK && s->policy == GC_SHARE_ALWAYS) return st;
+    if (st != GC_OK) spl->any = false;  // more work than its launches hold: the plain attention may take it
     if (!spl->any) return plan_checked(geo, b, o, sh, pl);
     spl->mark = shared_mark(geo, b, s, pk, *sh, *spl);
     return GC_OK;

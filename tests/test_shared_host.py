@@ -184,3 +184,11 @@ def test_what_the_policy_takes_of_many_groups(lib, sizes, lens, n, taken):
     assert (auto != plain_size(lib, g, b)) == taken
     if taken:
         assert auto == size(lib, g, b, HostShared(first, lens, policy=gc.SHARE_ALWAYS))[1]
+
+
+def test_a_batch_past_the_launch_limit_is_left_to_the_plain_attention(lib):
+    """52500 questions of 20 tokens on one document: more rows than the merge's launch takes, which the plain attention
+    does not have. The policy leaves it the batch; taken whatever it costs, it is refused."""
+    g, b = geo(Hq=64, Hkv=8, NB=1 << 20, maxb=1 << 12), HostBatch([33000] * 52500, [20] * 52500)
+    assert size(lib, g, b, HostShared([0, 52500], [32768], policy=gc.SHARE_AUTO)) == (0, plain_size(lib, g, b))
+    assert size(lib, g, b, HostShared([0, 52500], [32768], policy=gc.SHARE_ALWAYS))[0] == -2
