@@ -312,8 +312,11 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
  * Shared prefixes. Requests that reuse the same context (a system prompt, a document
  * that many ask about) hold the same pool pages at the head of their block-table rows.
  * The calls below read those pages once for all of a group's queries instead of once
- * per request; their results are those of the plain attention calls up to the order
- * of the sums.
+ * per request; their results are those of the plain attention calls up to the order of
+ * the sums and the rounding of the softmax weights. Those are bf16 in every tiling; on small
+ * tiles a row's largest is exactly 1, on 128-row tiles, which shared keys take, it is rounded like
+ * the others, so that single tokens come out as prompts do (relative error against 64 bits,
+ * of norms: 0.0018 to 0.0021, from the plain call 0.0017 to 0.0018; rounding `out` alone 0.0016).
  *   Groups are consecutive requests; every request is in one (alone, with shared
  *   length 0, where it shares nothing). The first shared_lens[g] tokens of every request of
  *   group g, a multiple of page_size and at most the least P_r of the group, are the
@@ -345,7 +348,9 @@ typedef struct gc_shared {
  * 8-bit forms, over groups. Plans and workspaces are of their own kind (a plan made by
  * gc_shared_prefix_plan is run by gc_shared_prefix_run with the same batch, groups and
  * options; a run that takes groups once and finds no such plan in its workspace enqueues
- * kernels that write nothing), and those of bf16 and of 8-bit pools differ (fp8: 0 or 1);
+ * kernels that write nothing; where the policy leaves the batch to the plain attention the
+ * plan is a plain one, and a run needs it there as gc_prefix_prefill_run does), and those of
+ * bf16 and of 8-bit pools differ (fp8: 0 or 1);
  * gc_prefix_prefill_plan_status serves them too, and covers the groups' device arrays.
  * Options: tiling GC_TILES_AUTO only (else GC_ERR_UNSUPPORTED); kv_split_tiles > 0 cuts
  * 128-row tiles into chunks of that many 64-key tiles, and the small tiles of successive
@@ -396,7 +401,7 @@ typedef enum gc_rotary_pairs {
 } gc_rotary_pairs;
 
 typedef struct gc_rotary {
-    const float* table_dev; /* device fp32 [num_positions][rotary_dim / 2][2]: cos, sin */
+    const float* table_dev; /* device fp32 [num_positions][rotary_dim / 2][2]: cos, sin; 16-byte aligned */
     int32_t num_positions;  /* every position of the batch, max(P_r + n_r) of them, must have a row */
     int32_t rotary_dim;     /* rotated elements of a head: a multiple of 16, 16 .. head_dim */
     int32_t pairs;          /* a gc_rotary_pairs value; other values: GC_ERR_BAD_SHAPE */

@@ -9,6 +9,15 @@
 // so the shared set may be computed for all rows of the group at once: rows of other requests are
 // further rows of the same matrix products, with no mask.
 //
+// Rounding. As everywhere in this framework the weights enter the second product as bf16, the row sums (fp32) add the
+// rounded ones, partial rows and log-sum-exps are fp32. 128-row items keep the offset of a row's first tile
+// (attention_kernels.h), so that its heaviest weight is rounded too, where the plain attention of single tokens
+// (16-row tiles, the running maximum) has it at exactly 1. With the running maximum here as well, relative error
+// against 64 bits and time, without / with: 64 answers on 8192 tokens 0.0021 / 0.0018, 52.6 / 53.7 us; 200 on 32768 at
+// 8 heads 0.0021 / 0.0017, 46.8 / 52.1; 100 over 8-bit pools 0.0018 / 0.0017, 65.2 / 65.3; 24 questions at d = 64
+// 0.0021 / 0.0018, 44.5 / 50.4, prompts whose plain attention has 0.0021 too. Rounding the output to bf16 alone
+// is 0.0016, so the time was kept.
+//
 // Work. Three launches: plan (once a batch), items, merge. One launch runs both kinds of items, so that
 // they overlap: 128-row items (64-key tiles through LDS; the shared parts, and own parts of many new
 // tokens), bound by the matrix cores and the softmax, and small items (one wavefront, 16 rows; own parts
