@@ -316,7 +316,7 @@ gc_status gc_prefix_prefill_prepare_fp8(const gc_geometry* geo, const gc_batch* 
  * the sums and the rounding of the softmax weights. Those are bf16 in every tiling; on small
  * tiles a row's largest is exactly 1, on 128-row tiles, which shared keys take, it is rounded like
  * the others, so that single tokens come out as prompts do (relative error against 64 bits,
- * of norms: 0.0018 to 0.0021, from the plain call 0.0017 to 0.0018; rounding `out` alone 0.0016).
+ * of norms: 0.0018 to 0.0022, from the plain call 0.0017 to 0.0018; rounding `out` alone 0.0016).
  *   Groups are consecutive requests; every request is in one (alone, with shared
  *   length 0, where it shares nothing). The first shared_lens[g] tokens of every request of
  *   group g, a multiple of page_size and at most the least P_r of the group, are the
