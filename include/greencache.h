@@ -446,6 +446,79 @@ gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch,
                                   void* k_pool8, void* v_pool8, hipStream_t stream);
 
 /*
+ * 4-bit KV pools. A cached token takes 0.53 bytes per element instead of 2 (bf16 pools) or 1
+ * (8-bit pools): nearly four times the context in a given pool, and a quarter of the bytes that the
+ * memory-bound attention reads.
+ *   Pool layout:
+ *     k_pool4  uint8 [num_blocks][num_kv_heads][page_size][head_dim / 2]
+ *     v_pool4  uint8 [num_blocks][num_kv_heads][page_size][head_dim / 2]
+ *     scales4  uint8 [num_blocks][num_kv_heads][page_size][head_dim / 32][2]
+ *   Byte i of a row holds the codes of elements 2 i (bits 0 .. 3) and 2 i + 1 (bits 4 .. 7). Value
+ *   pages are not transposed here, unlike the other pools': a byte belongs to one token. The scales
+ *   are those of 32 elements of a token's key ([0]) and value ([1]).
+ *   A code is an OCP 4-bit floating-point E2M1 number (sign, 2 exponent bits with bias 1, 1 mantissa
+ *   bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), a scale an OCP E8M0 number: exponent code c stands for
+ *   2^(c - 127), 255 for NaN. An element is code value * scale, a bf16 number exactly for the codes
+ *   that the append writes (c in 3 .. 252); a block of scale 255 is NaN throughout.
+ *   All three are 16-byte aligned (else GC_ERR_BAD_SHAPE).
+ */
+
+/*
+ * gc_kv_append into 4-bit pools. For each block of 32 elements with largest magnitude A the scale is
+ * the least power of two s with A < 7 s (2^-124 <= s <= 2^125), and element x is stored as the E2M1
+ * code nearest to x / s, ties to the even code, saturated at 6 (infinities are the largest numbers);
+ * the sign is kept, of zeros too. A block that holds a NaN gets the scale 255 and codes 0. Slots,
+ * ordering and host/device sources as gc_kv_append (k_new and v_new 16-byte aligned). Rows that
+ * gc_kv_read_fp4 returns are stored as the same codes and scales again. Errors as gc_kv_append, and
+ * GC_ERR_UNSUPPORTED for a batch of more work than one launch holds.
+ */
+gc_status gc_kv_append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_new, const void* v_new,
+                           void* k_pool4, void* v_pool4, void* scales4, hipStream_t stream);
+
+/* gc_kv_append_rotary into 4-bit pools: a rotated key element is the exact x_a cos -+ x_b sin of the table's
+ * numbers rounded to fp32, then stored as above. q_out, errors and everything else as there. */
+gc_status gc_kv_append_rotary_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                                  const gc_new_rows* rows, void* q_out, void* k_pool4, void* v_pool4, void* scales4,
+                                  hipStream_t stream);
+
+/*
+ * Read rows out of a pool: the inverse of the append (§2.2: a context's KV on its way to the cache's
+ * host tier, which gc_kv_append restores from; or to a pool of another kind). For every request r,
+ * new token i of the batch and KV head h, what the pools hold at position P_r + i goes to
+ * k_out[cu_r + i][h] and v_out[cu_r + i][h]: a whole context is read with prefix_lens = 0 and
+ * new_lens = its length. (A request's row needs its pages up to the last position read.)
+ *   k_out, v_out : bf16 [T][Hkv][D], device memory or pinned host memory, 16-byte aligned, over
+ *                  neither each other nor the pools (else GC_ERR_BAD_SHAPE, pools likewise)
+ * bf16 pools: bit for bit. 8-bit pools: bf16 nearest to fl32(code value * scale), ties to even; 4-bit
+ * pools: exact; NaN codes and blocks give NaN. Rows of a page whose block id is outside the
+ * pool keep their contents. Errors as gc_kv_append (pools and outputs are required), and
+ * GC_ERR_UNSUPPORTED for a batch of more work than one launch holds.
+ */
+gc_status gc_kv_read(const gc_geometry* geo, const gc_batch* batch, const void* k_pool, const void* v_pool,
+                     void* k_out, void* v_out, hipStream_t stream);
+gc_status gc_kv_read_fp8(const gc_geometry* geo, const gc_batch* batch, const void* k_pool8, const void* v_pool8,
+                         float k_scale, float v_scale, void* k_out, void* v_out, hipStream_t stream);
+gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_pool4, const void* v_pool4,
+                         const void* scales4, void* k_out, void* v_out, hipStream_t stream);
+
+/*
+ * gc_prefix_prefill_run and gc_prefix_prefill_attention (plan and run) over 4-bit pools: the same attention with
+ * every key and value element as the number it stands for. Plans, workspaces, tilings and options are
+ * those of the other pools (gc_prefix_prefill_plan and gc_prefix_prefill_workspace_size serve all). A value
+ * block that is NaN makes those rows NaN that see its token, in its elements. Errors as those calls, and
+ * GC_ERR_BAD_SHAPE for q or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_UNSUPPORTED for a batch of more work
+ * than one launch holds. Shared prefixes (gc_shared_prefix_*) are over bf16 and 8-bit pools only.
+ */
+gc_status gc_prefix_prefill_run_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
+                                    const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
+                                    float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream);
+gc_status gc_prefix_prefill_attention_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
+                                          const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
+                                          float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream);
+
+/*
  * Calibration, not part of the attention path: read every byte of `buf`
  * (device memory, `bytes` a multiple of 16) once as a streaming reduction,
  * writing GC_READ_PROBE_SINK_WORDS 32-bit words to `sink` (device). Timing it

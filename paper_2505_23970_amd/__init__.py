@@ -24,6 +24,8 @@ STATUS_NAMES = {0: "GC_OK", -1: "GC_ERR_NULL_ARG", -2: "GC_ERR_BAD_SHAPE", -3: "
 GC_ERR_LENGTHS = -7
 
 EXPORTED = ("gc_kv_append", "gc_kv_append_rotary", "gc_kv_append_rotary_fp8",
+            "gc_kv_append_fp4", "gc_kv_append_rotary_fp4", "gc_kv_read", "gc_kv_read_fp8", "gc_kv_read_fp4",
+            "gc_prefix_prefill_run_fp4", "gc_prefix_prefill_attention_fp4",
             "gc_prefix_prefill_workspace_size", "gc_prefix_prefill_plan",
             "gc_prefix_prefill_run", "gc_prefix_prefill_attention", "gc_kv_append_fp8",
             "gc_prefix_prefill_run_fp8", "gc_prefix_prefill_attention_fp8", "gc_prefix_prefill_prepare",
@@ -145,6 +147,19 @@ def load_library(path: str | None = None):
     lib.gc_kv_append_rotary.argtypes = [G, Bp, Ro, Nr, vp, vp, vp, vp]
     lib.gc_kv_append_rotary_fp8.restype = i32
     lib.gc_kv_append_rotary_fp8.argtypes = [G, Bp, Ro, Nr, vp, f32, f32, vp, vp, vp]
+    lib.gc_kv_append_fp4.restype = i32
+    lib.gc_kv_append_fp4.argtypes = [G, Bp, vp, vp, vp, vp, vp, vp]
+    lib.gc_kv_append_rotary_fp4.restype = i32
+    lib.gc_kv_append_rotary_fp4.argtypes = [G, Bp, Ro, Nr, vp, vp, vp, vp, vp]
+    lib.gc_kv_read.restype = i32
+    lib.gc_kv_read.argtypes = [G, Bp, vp, vp, vp, vp, vp]
+    lib.gc_kv_read_fp8.restype = i32
+    lib.gc_kv_read_fp8.argtypes = [G, Bp, vp, vp, f32, f32, vp, vp, vp]
+    lib.gc_kv_read_fp4.restype = i32
+    lib.gc_kv_read_fp4.argtypes = [G, Bp, vp, vp, vp, vp, vp, vp]
+    for fn in (lib.gc_prefix_prefill_run_fp4, lib.gc_prefix_prefill_attention_fp4):
+        fn.restype = i32
+        fn.argtypes = [G, Bp, O, vp, vp, vp, vp, f32, vp, vp, vp, ctypes.c_size_t, vp]
     lib.gc_prefix_prefill_prepare.restype = i32
     lib.gc_prefix_prefill_prepare.argtypes = [G, Bp, O, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.gc_prefix_prefill_prepare_fp8.restype = i32
@@ -269,6 +284,19 @@ def _geo_from_pools(k_pool, v_pool, q_heads, batch: PagedBatch):
     return Geometry(int(q_heads), Hkv, D, S, NB, batch.max_blocks_per_seq)
 
 
+def _geo_from_pools4(k_pool4, v_pool4, q_heads, batch: PagedBatch):
+    NB, Hkv, S, half = k_pool4.shape
+    if v_pool4.shape != k_pool4.shape:
+        raise ValueError(f"v_pool4 must have k_pool4's shape [NB][Hkv][S][D / 2] = {tuple(k_pool4.shape)}, got {tuple(v_pool4.shape)}")
+    return Geometry(int(q_heads), Hkv, 2 * half, S, NB, batch.max_blocks_per_seq)
+
+
+def _geo_for_plan(k_pool, v_pool, q_heads, batch: PagedBatch):
+    """The geometry of pools of any kind (value pages of 4-bit pools are not transposed)."""
+    four = k_pool.dtype == _t().uint8 and k_pool.shape == v_pool.shape
+    return (_geo_from_pools4 if four else _geo_from_pools)(k_pool, v_pool, q_heads, batch)
+
+
 def _opts(kv_split_tiles, tiling=None):
     if kv_split_tiles is None and tiling is None:
         return None
@@ -327,7 +355,7 @@ def kv_restore(k_src, v_src, k_pool, v_pool, batch: PagedBatch, stream=None):
 def workspace_size(num_q_heads, k_pool, v_pool, batch: PagedBatch, kv_split_tiles=None,
                    tiling=None) -> int:
     lib = load_library()
-    geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
+    geo = _geo_for_plan(k_pool, v_pool, num_q_heads, batch)
     out = ctypes.c_size_t(0)
     st = lib.gc_prefix_prefill_workspace_size(ctypes.byref(geo), ctypes.byref(batch.desc()),
                                               _opts(kv_split_tiles, tiling), ctypes.byref(out))
@@ -370,7 +398,7 @@ def plan(num_q_heads, k_pool, v_pool, batch: PagedBatch, workspace, kv_split_til
     torch = _t()
     lib = load_library()
     _require(workspace, torch.uint8, "workspace", batch.device)
-    geo = _geo_from_pools(k_pool, v_pool, num_q_heads, batch)
+    geo = _geo_for_plan(k_pool, v_pool, num_q_heads, batch)
     st = lib.gc_prefix_prefill_plan(ctypes.byref(geo), ctypes.byref(batch.desc()),
                                     _opts(kv_split_tiles, tiling), workspace.data_ptr(),
                                     workspace.numel(), _stream_handle(stream))
@@ -654,18 +682,23 @@ def _empty_on(stream, *size, **kw):
         return torch.empty(*size, **kw)
 
 
-def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, interleaved, stream, scales):
+def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, interleaved, stream, scales, scales4=None):
     torch = _t()
     lib = load_library()
     device = batch.device
-    pool_dtype = torch.uint8 if scales else torch.bfloat16
-    _require(k_pool, pool_dtype, "k_pool", device)
-    _require(v_pool, pool_dtype, "v_pool", device)
+    if scales4 is None:
+        pool_dtype = torch.uint8 if scales else torch.bfloat16
+        _require(k_pool, pool_dtype, "k_pool", device)
+        _require(v_pool, pool_dtype, "v_pool", device)
+    else:
+        _require_pools4(k_pool, v_pool, scales4, device)
     _require(table, torch.float32, "table", device)
     if table.dim() != 3 or table.shape[2] != 2:
         raise ValueError("table must be [positions][rotary_dim / 2][2]")
     T = int(batch.cu_new_lens[-1])
     _, Hkv, _, D = k_pool.shape
+    if scales4 is not None:
+        D *= 2
     kv_shape = (T, Hkv, D)
     k_stride = _require_rows(k_new, "k_new", kv_shape, device)
     v_stride = _require_rows(v_new, "v_new", kv_shape, device)
@@ -683,12 +716,12 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
     elif q_out is not None:
         raise ValueError("q_out without q")
     rows = NewRows(q_at, k_new.data_ptr(), v_new.data_ptr(), q_stride, k_stride, v_stride)
-    geo = _geo_from_pools(k_pool, v_pool, Hq, batch)
+    geo = (_geo_from_pools if scales4 is None else _geo_from_pools4)(k_pool, v_pool, Hq, batch)
     rot = Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1],
                  PAIRS_INTERLEAVED if interleaved else PAIRS_HALVES)
     byref = ctypes.byref
-    st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), byref(rot), byref(rows), out_at, *scales,
-               k_pool.data_ptr(), v_pool.data_ptr())
+    pools = (k_pool.data_ptr(), v_pool.data_ptr()) + (() if scales4 is None else (scales4.data_ptr(),))
+    st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), byref(rot), byref(rows), out_at, *scales, *pools)
     _check(fn, st, lib)
     return q_out
 
@@ -710,6 +743,170 @@ def kv_append_rotary_fp8(q, k_new, v_new, k_pool8, v_pool8, batch: PagedBatch, t
     """kv_append_rotary into 8-bit pools: the rotated keys are quantised from fp32, the queries stay bf16."""
     return _append_rotary("gc_kv_append_rotary_fp8", q, k_new, v_new, k_pool8, v_pool8, batch, table, q_out,
                           interleaved, stream, (float(k_scale), float(v_scale)))
+
+
+# ----------------------------------------------------------------- 4-bit pools
+# Pools are uint8 tensors of E2M1 codes, two a byte, [NB][Hkv][16][D / 2] for keys and for values, with a uint8
+# tensor [NB][Hkv][16][D / 32][2] of scales (E8M0 exponents, one for 32 elements of a token's key and value each).
+# See include/greencache.h. plan, workspace_size and alloc_workspace take them as they take the other pools.
+
+def alloc_pools_fp4(num_blocks, num_kv_heads, head_dim, device="cuda"):
+    """k_pool4, v_pool4 and scales4 of num_blocks pages of 16 tokens, holding zeros."""
+    torch = _t()
+    if head_dim % 32:
+        raise ValueError("head_dim must be a multiple of 32")
+    shape = (int(num_blocks), int(num_kv_heads), 16)
+    codes = [torch.zeros(*shape, head_dim // 2, dtype=torch.uint8, device=device) for _ in range(2)]
+    return (*codes, torch.full((*shape, head_dim // 32, 2), 127, dtype=torch.uint8, device=device))
+
+
+def _require_pools4(k_pool4, v_pool4, scales4, device):
+    torch = _t()
+    _require(k_pool4, torch.uint8, "k_pool4", device)
+    _require(v_pool4, torch.uint8, "v_pool4", device)
+    _require(scales4, torch.uint8, "scales4", device)
+    if k_pool4.dim() != 4:
+        raise ValueError("k_pool4 must be [NB][Hkv][16][D / 2]")
+    NB, Hkv, S, half = k_pool4.shape
+    if scales4.shape != (NB, Hkv, S, half // 16, 2):
+        raise ValueError(f"scales4 must be [NB][Hkv][S][D / 32][2] = {(NB, Hkv, S, half // 16, 2)}, got {tuple(scales4.shape)}")
+
+
+def kv_append_fp4(k_new, v_new, k_pool4, v_pool4, scales4, batch: PagedBatch, stream=None):
+    """Quantise the new tokens' K/V ([T][Hkv][D] bf16) into the 4-bit pools in place. k_new and v_new may be
+    pinned host tensors, which the GPU reads directly over PCIe."""
+    torch = _t()
+    lib = load_library()
+    device = batch.device
+    _require_pools4(k_pool4, v_pool4, scales4, device)
+    geo = _geo_from_pools4(k_pool4, v_pool4, k_pool4.shape[1], batch)
+    shape = (int(batch.cu_new_lens[-1]), geo.num_kv_heads, geo.head_dim)
+    _require_host_or_device_rows(k_new, "k_new", shape, device)
+    _require_host_or_device_rows(v_new, "v_new", shape, device)
+    byref = ctypes.byref
+    st = _here(device, stream, lib.gc_kv_append_fp4, byref(geo), byref(batch._desc), k_new.data_ptr(), v_new.data_ptr(),
+               k_pool4.data_ptr(), v_pool4.data_ptr(), scales4.data_ptr())
+    _check("gc_kv_append_fp4", st, lib)
+
+
+def kv_append_rotary_fp4(q, k_new, v_new, k_pool4, v_pool4, scales4, batch: PagedBatch, table, q_out=None,
+                         interleaved=False, stream=None):
+    """kv_append_rotary into 4-bit pools: the rotated keys are quantised from fp32, the queries stay bf16."""
+    return _append_rotary("gc_kv_append_rotary_fp4", q, k_new, v_new, k_pool4, v_pool4, batch, table, q_out,
+                          interleaved, stream, (), scales4)
+
+
+def run_fp4(q, k_pool4, v_pool4, scales4, batch: PagedBatch, scale, workspace, out=None, lse=None, kv_split_tiles=None,
+            stream=None, tiling=None):
+    """run over 4-bit pools, from a plan made by plan (with these pools or others of the same geometry)."""
+    return _attention_fp4("gc_prefix_prefill_run_fp4", q, k_pool4, v_pool4, scales4, batch, scale, workspace, out, lse,
+                          kv_split_tiles, stream, tiling)
+
+
+def prefix_prefill_attention_fp4(q, k_pool4, v_pool4, scales4, batch: PagedBatch, scale, workspace=None, out=None,
+                                 lse=None, kv_split_tiles=None, stream=None, tiling=None):
+    """prefix_prefill_attention over 4-bit pools."""
+    return _attention_fp4("gc_prefix_prefill_attention_fp4", q, k_pool4, v_pool4, scales4, batch, scale, workspace, out,
+                          lse, kv_split_tiles, stream, tiling)
+
+
+def _attention_fp4(fn, q, k_pool4, v_pool4, scales4, batch, scale, workspace, out, lse, kv_split_tiles, stream, tiling):
+    torch = _t()
+    lib = load_library()
+    device = batch.device
+    _require_pools4(k_pool4, v_pool4, scales4, device)
+    _require(q, torch.bfloat16, "q", device)
+    T, Hq, D = q.shape
+    geo = _geo_from_pools4(k_pool4, v_pool4, Hq, batch)
+    if T != int(batch.cu_new_lens[-1]) or D != geo.head_dim:
+        raise ValueError("q must be [T][Hq][D] matching the batch and pools")
+    if workspace is None:
+        n = _here(device, None, lambda _: workspace_size(Hq, k_pool4, v_pool4, batch, kv_split_tiles, tiling))
+        workspace = _empty_on(stream, max(n, 256), dtype=torch.uint8, device=device)
+    _require(workspace, torch.uint8, "workspace", device)
+    if out is None:
+        out = _empty_on(stream, (T, Hq, D), dtype=torch.bfloat16, device=device)
+    _require(out, torch.bfloat16, "out", device)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if lse is not None:
+        _require(lse, torch.float32, "lse", device)
+        if lse.shape != (T, Hq):
+            raise ValueError("lse must be [T][Hq] float32")
+    byref = ctypes.byref
+    st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), _opts(kv_split_tiles, tiling), q.data_ptr(),
+               k_pool4.data_ptr(), v_pool4.data_ptr(), scales4.data_ptr(), float(scale), out.data_ptr(),
+               lse.data_ptr() if lse is not None else None, workspace.data_ptr(), workspace.numel())
+    _check(fn, st, lib)
+    return out
+
+
+# ----------------------------------------------------------------- rows out of a pool
+
+def _require_host_or_device_rows(t, name, shape, device):
+    """Contiguous bf16 rows [T][heads][D] on the batch's device or in pinned host memory."""
+    torch = _t()
+    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.is_contiguous() and t.device == device:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16 (got {t.dtype})")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be [T][heads][D] = {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device.type == "cpu":
+        if not t.is_pinned():
+            raise ValueError(f"{name} is in pageable host memory: the GPU reaches only pinned host memory")
+    elif t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _read(fn, k_pool, v_pool, geo, batch, pools, k_out, v_out, stream):
+    torch = _t()
+    lib = load_library()
+    device = batch.device
+    shape = (int(batch.cu_new_lens[-1]), geo.num_kv_heads, geo.head_dim)
+    if k_out is None:
+        k_out = _empty_on(stream, shape, dtype=torch.bfloat16, device=device)
+    if v_out is None:
+        v_out = _empty_on(stream, shape, dtype=torch.bfloat16, device=device)
+    _require_host_or_device_rows(k_out, "k_out", shape, device)
+    _require_host_or_device_rows(v_out, "v_out", shape, device)
+    byref = ctypes.byref
+    st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), k_pool.data_ptr(), v_pool.data_ptr(), *pools,
+               k_out.data_ptr(), v_out.data_ptr())
+    _check(fn, st, lib)
+    return k_out, v_out
+
+
+def kv_read(k_pool, v_pool, batch: PagedBatch, k_out=None, v_out=None, stream=None):
+    """The K/V rows ([T][Hkv][D] bf16, returned; made where None) that the pools hold at the batch's new positions
+    P_r .. P_r + n_r - 1: the inverse of kv_append. k_out and v_out may be pinned host tensors, which the GPU writes
+    directly over PCIe (the cache's CPU tier, which kv_restore reads). A whole context is a batch with prefix
+    lengths 0 and its length as new tokens."""
+    torch = _t()
+    _require(k_pool, torch.bfloat16, "k_pool", batch.device)
+    _require(v_pool, torch.bfloat16, "v_pool", batch.device)
+    geo = _geo_from_pools(k_pool, v_pool, k_pool.shape[1], batch)
+    return _read("gc_kv_read", k_pool, v_pool, geo, batch, (), k_out, v_out, stream)
+
+
+def kv_read_fp8(k_pool8, v_pool8, batch: PagedBatch, k_scale, v_scale, k_out=None, v_out=None, stream=None):
+    """kv_read from 8-bit pools: code value * scale, rounded to bf16."""
+    torch = _t()
+    _require(k_pool8, torch.uint8, "k_pool8", batch.device)
+    _require(v_pool8, torch.uint8, "v_pool8", batch.device)
+    geo = _geo_from_pools(k_pool8, v_pool8, k_pool8.shape[1], batch)
+    return _read("gc_kv_read_fp8", k_pool8, v_pool8, geo, batch, (float(k_scale), float(v_scale)), k_out, v_out, stream)
+
+
+def kv_read_fp4(k_pool4, v_pool4, scales4, batch: PagedBatch, k_out=None, v_out=None, stream=None):
+    """kv_read from 4-bit pools: exactly the numbers that the pools hold."""
+    _require_pools4(k_pool4, v_pool4, scales4, batch.device)
+    geo = _geo_from_pools4(k_pool4, v_pool4, k_pool4.shape[1], batch)
+    return _read("gc_kv_read_fp4", k_pool4, v_pool4, geo, batch, (scales4.data_ptr(),), k_out, v_out, stream)
 
 
 # ----------------------------------------------------------------- shared prefixes

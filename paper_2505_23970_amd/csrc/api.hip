@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <mutex>
 
 #include "gc_internal.h"
@@ -463,11 +464,19 @@ int resident_workgroups(const gc_geometry* geo, const Shape& sh, const Plan& pl)
     return pl.items * geo->num_kv_heads >= 2LL * cus ? cus : 0;
 }
 
-// Pools of bf16 elements (fp8 false, scales 1) or of E4M3 codes with one scale each.
+// Pools of bf16 elements (fp8 false, scales 1), of E4M3 codes with one scale each, or of E2M1 codes
+// with scales of their own (scales4 not null).
 struct PoolKind {
     bool fp8 = false;
     float k_scale = 1.f, v_scale = 1.f;
+    const void* scales4 = nullptr;
+    gc::Pool pool() const { return scales4 != nullptr ? gc::Pool::kFp4 : fp8 ? gc::Pool::kFp8 : gc::Pool::kBf16; }
 };
+PoolKind fp4_pools(const void* scales) {
+    PoolKind pk;
+    pk.scales4 = scales;
+    return pk;
+}
 
 gc_status enqueue_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh, const Plan& pl,
                       const void* q, const void* k_pool, const void* v_pool, float scale,
@@ -493,9 +502,15 @@ gc_status enqueue_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh
     a.v_scale = pk.v_scale;
     a.prefer_span = (uint32_t)device_cus();
     a.prefer_odd = pl.heaviest_decides ? 0 : 1;
-    const hipError_t e = sh.small ? gc::launch_attention_small(a, geo->head_dim, pl.items, pk.fp8, stream)
-                                  : gc::launch_attention(a, geo->head_dim, pl.items, sh.wide, pl.three, pk.fp8,
-                                                         resident_workgroups(geo, sh, pl), stream);
+    hipError_t e;
+    if (pk.scales4 != nullptr) {
+        gc::Fp4AttnArgs a4{a, static_cast<const uint8_t*>(pk.scales4)};
+        e = gc::launch_attention_fp4(a4, geo->head_dim, pl.items, sh.small, sh.wide, resident_workgroups(geo, sh, pl), stream);
+    } else if (sh.small) {
+        e = gc::launch_attention_small(a, geo->head_dim, pl.items, pk.fp8, stream);
+    } else {
+        e = gc::launch_attention(a, geo->head_dim, pl.items, sh.wide, pl.three, pk.fp8, resident_workgroups(geo, sh, pl), stream);
+    }
     if (e != hipSuccess) return GC_ERR_HIP;
     if (pl.combines > 0) {
         gc::CombineArgs c{};
@@ -582,6 +597,20 @@ bool overlap(const void* p, int64_t np, const void* q, int64_t nq) {
     return a < b + (uintptr_t)nq && b < a + (uintptr_t)np;
 }
 
+// Bytes of a pool, and of the scales of 4-bit pools.
+int64_t pool_bytes(const gc_geometry* geo, gc::Pool pool) {
+    const int64_t elements = (int64_t)geo->num_blocks * gc::kPage * geo->num_kv_heads * geo->head_dim;
+    return pool == gc::Pool::kFp4 ? elements / 2 : pool == gc::Pool::kFp8 ? elements : elements * 2;
+}
+int64_t scale_bytes(const gc_geometry* geo) { return pool_bytes(geo, gc::Pool::kFp4) / 8; }
+
+// The pointers of 4-bit pools.
+gc_status check_fp4(const void* k_pool, const void* v_pool, const void* scales) {
+    if (k_pool == nullptr || v_pool == nullptr || scales == nullptr) return GC_ERR_NULL_ARG;
+    if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(scales)) return GC_ERR_BAD_SHAPE;
+    return GC_OK;
+}
+
 gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rot, const gc_new_rows* rows,
                         void* q_out, void* k_pool, void* v_pool, const PoolKind& pk, hipStream_t stream) {
     Shape sh;
@@ -596,6 +625,11 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
     if (sh.total_tokens == 0) return GC_OK;
     if (rot->table_dev == nullptr || rows->k == nullptr || rows->v == nullptr || k_pool == nullptr || v_pool == nullptr)
         return GC_ERR_NULL_ARG;
+    const gc::Pool kind = pk.pool();
+    if (kind == gc::Pool::kFp4) {
+        st = check_fp4(k_pool, v_pool, pk.scales4);
+        if (st != GC_OK) return st;
+    }
     if ((rows->q == nullptr) != (q_out == nullptr)) return GC_ERR_NULL_ARG;
     const bool with_q = rows->q != nullptr;
     const int64_t T = sh.total_tokens, D = geo->head_dim;
@@ -612,13 +646,14 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
             (int64_t)batch->prefix_lens_host[r] + batch->new_lens_host[r] > rot->num_positions)
             return GC_ERR_BAD_SHAPE;
     if (with_q) {
-        const int64_t out = T * q_row * 2, pool = (int64_t)geo->num_blocks * gc::kPage * kv_row * (pk.fp8 ? 1 : 2);
+        const int64_t out = T * q_row * 2, pool = pool_bytes(geo, kind);
         const bool in_place = q_out == rows->q && rows->q_stride == q_row;
         if ((!in_place && overlap(q_out, out, rows->q, span_bytes(T, rows->q_stride, q_row))) ||
             overlap(q_out, out, rows->k, span_bytes(T, rows->k_stride, kv_row)) ||
             overlap(q_out, out, rows->v, span_bytes(T, rows->v_stride, kv_row)) ||
             overlap(q_out, out, rot->table_dev, (int64_t)rot->num_positions * rot->rotary_dim * 4) ||
-            overlap(q_out, out, k_pool, pool) || overlap(q_out, out, v_pool, pool))
+            overlap(q_out, out, k_pool, pool) || overlap(q_out, out, v_pool, pool) ||
+            (kind == gc::Pool::kFp4 && overlap(q_out, out, pk.scales4, scale_bytes(geo))))
             return GC_ERR_BAD_SHAPE;
     }
     gc::RotaryArgs ra{};
@@ -635,7 +670,55 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
     ra.num_positions = rot->num_positions;
     ra.rotary_dim = rot->rotary_dim;
     ra.interleaved = rot->pairs == GC_PAIRS_INTERLEAVED;
-    return gc::launch_append_rotary(ra, geo->head_dim, pk.fp8, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+    ra.scales = static_cast<uint8_t*>(const_cast<void*>(pk.scales4));
+    return gc::launch_append_rotary(ra, geo->head_dim, kind, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+}
+
+// The plain append into 4-bit pools: the rotary one's launch without a rotation.
+gc_status append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_new, const void* v_new,
+                     void* k_pool, void* v_pool, void* scales, hipStream_t stream) {
+    Shape sh;
+    gc_status st = check_common(geo, batch, &sh);
+    if (st != GC_OK || sh.total_tokens == 0) return st;
+    if (k_new == nullptr || v_new == nullptr) return GC_ERR_NULL_ARG;
+    st = check_fp4(k_pool, v_pool, scales);
+    if (st != GC_OK) return st;
+    if (!aligned16(k_new) || !aligned16(v_new)) return GC_ERR_BAD_SHAPE;
+    gc::RotaryArgs ra{};
+    ra.a = append_args(geo, batch, sh, k_new, v_new, k_pool, v_pool, PoolKind{});
+    if (gc::rotary_workgroups(ra.a.total_pages, geo->num_q_heads, geo->num_kv_heads, geo->head_dim, false) > gc::kMaxWorkgroups)
+        return GC_ERR_UNSUPPORTED;
+    ra.k_stride = ra.v_stride = (int64_t)geo->num_kv_heads * geo->head_dim;
+    ra.num_q_heads = geo->num_q_heads;
+    ra.num_positions = INT32_MAX;
+    ra.scales = static_cast<uint8_t*>(scales);
+    return gc::launch_append_rotary(ra, geo->head_dim, gc::Pool::kFp4, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+}
+
+gc_status read_rows(const gc_geometry* geo, const gc_batch* batch, const void* k_pool, const void* v_pool,
+                    const PoolKind& pk, void* k_out, void* v_out, hipStream_t stream) {
+    Shape sh;
+    gc_status st = check_common(geo, batch, &sh);
+    if (st != GC_OK || sh.total_tokens == 0) return st;
+    if (k_pool == nullptr || v_pool == nullptr || k_out == nullptr || v_out == nullptr) return GC_ERR_NULL_ARG;
+    if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(pk.scales4) || !aligned16(k_out) || !aligned16(v_out))
+        return GC_ERR_BAD_SHAPE;
+    const gc::Pool kind = pk.pool();
+    const int64_t out = sh.total_tokens * geo->num_kv_heads * geo->head_dim * 2, pool = pool_bytes(geo, kind);
+    if (overlap(k_out, out, v_out, out)) return GC_ERR_BAD_SHAPE;
+    for (const void* p : {k_out, v_out})
+        if (overlap(p, out, k_pool, pool) || overlap(p, out, v_pool, pool) ||
+            (kind == gc::Pool::kFp4 && overlap(p, out, pk.scales4, scale_bytes(geo))))
+            return GC_ERR_BAD_SHAPE;
+    gc::ReadArgs ra{};
+    ra.a = append_args(geo, batch, sh, nullptr, nullptr, const_cast<void*>(k_pool), const_cast<void*>(v_pool), PoolKind{});
+    if (gc::read_workgroups(ra.a.total_pages, geo->num_kv_heads, geo->head_dim) > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
+    ra.k_out = static_cast<uint16_t*>(k_out);
+    ra.v_out = static_cast<uint16_t*>(v_out);
+    ra.scales = static_cast<const uint8_t*>(pk.scales4);
+    ra.k_scale = pk.k_scale;
+    ra.v_scale = pk.v_scale;
+    return gc::launch_read(ra, geo->head_dim, kind, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
 // Append and plan in one launch (the plan reads only the lengths, so the two are
@@ -675,6 +758,13 @@ gc_status run(const gc_geometry* geo, const gc_batch* batch, const gc_plan_optio
     if (pk.fp8) {
         st = check_pool_scales(pk.k_scale, pk.v_scale);
         if (st != GC_OK) return st;
+    }
+    if (pk.scales4 != nullptr) {
+        st = check_fp4(k_pool, v_pool, pk.scales4);
+        if (st != GC_OK) return st;
+        if (!aligned16(q) || !aligned16(out)) return GC_ERR_BAD_SHAPE;
+        if (!aligned16(workspace)) return GC_ERR_WORKSPACE;
+        if (pl.items * geo->num_kv_heads > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
     }
     st = check_workspace(pl, workspace, workspace_bytes);
     if (st != GC_OK) return st;
@@ -1234,6 +1324,61 @@ gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch,
     const gc_status st = check_pool_scales(k_scale, v_scale);
     if (st != GC_OK) return st;
     return append_rotary(geo, batch, rotary, rows, q_out, k_pool, v_pool, PoolKind{true, k_scale, v_scale}, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_new, const void* v_new,
+                           void* k_pool4, void* v_pool4, void* scales4, hipStream_t stream) {
+    return append_fp4(geo, batch, k_new, v_new, k_pool4, v_pool4, scales4, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_append_rotary_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
+                                  const gc_new_rows* rows, void* q_out, void* k_pool4, void* v_pool4, void* scales4,
+                                  hipStream_t stream) {
+    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
+    return append_rotary(geo, batch, rotary, rows, q_out, k_pool4, v_pool4, fp4_pools(scales4), stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_read(const gc_geometry* geo, const gc_batch* batch, const void* k_pool, const void* v_pool, void* k_out,
+                     void* v_out, hipStream_t stream) {
+    return read_rows(geo, batch, k_pool, v_pool, PoolKind{}, k_out, v_out, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_read_fp8(const gc_geometry* geo, const gc_batch* batch, const void* k_pool8, const void* v_pool8,
+                         float k_scale, float v_scale, void* k_out, void* v_out, hipStream_t stream) {
+    const gc_status st = check_pool_scales(k_scale, v_scale);
+    if (st != GC_OK) return st;
+    return read_rows(geo, batch, k_pool8, v_pool8, PoolKind{true, k_scale, v_scale}, k_out, v_out, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_pool4, const void* v_pool4,
+                         const void* scales4, void* k_out, void* v_out, hipStream_t stream) {
+    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
+    return read_rows(geo, batch, k_pool4, v_pool4, fp4_pools(scales4), k_out, v_out, stream);
+}
+
+__attribute__((visibility("default")))
+gc_status gc_prefix_prefill_run_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
+                                    const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
+                                    float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
+    return run(geo, batch, opts, q, k_pool4, v_pool4, scale, out, lse, workspace, workspace_bytes, stream, false,
+               fp4_pools(scales4));
+}
+
+__attribute__((visibility("default")))
+gc_status gc_prefix_prefill_attention_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
+                                          const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
+                                          float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream) {
+    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
+    return run(geo, batch, opts, q, k_pool4, v_pool4, scale, out, lse, workspace, workspace_bytes, stream, true,
+               fp4_pools(scales4));
 }
 
 __attribute__((visibility("default")))

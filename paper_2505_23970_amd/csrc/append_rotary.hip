@@ -32,6 +32,7 @@
 // At 1290 MB it moves 5.7 TB/s (228 us), and 6.1 where the last-level cache holds a part of the inputs; a copy of as
 // many bytes by the framework's tensor library 4.8 to 5.3.
 #include "append_body.h"
+#include "fp4.h"
 
 namespace gc {
 namespace {
@@ -155,6 +156,80 @@ __device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm
     if (head_ok) store_values<D, FP8>(a, sv, page, tid, s0, s1);
 }
 
+// The same into 4-bit pools (fp4.h), whose pages hold whole rows of keys and of values: a token's codes share
+// no byte with another token's. Four lanes hold the 32 elements of a block. Rotated keys are computed in 64
+// bits and rounded to 32 (the products of a bf16 and an fp32 number are exact there, so that the codes are those
+// of the definition, next to a border too): the conversions and products cost nothing that shows beside the memory.
+// rotary_dim 0: keys as they are.
+template <int D>
+__device__ __forceinline__ void rotary_kv_fp4(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int hg) {
+    const AppendArgs& a = ra.a;
+    constexpr int CPR = D / 8;
+    constexpr int kPer = kPage * CPR;
+    constexpr int kBlocks = D / kFp4Block;
+    const int tid = threadIdx.x % kPer;
+    const int h = hg * AppendLds<D>::kHeads + threadIdx.x / kPer;
+    const bool head_ok = h < a.num_kv_heads;
+    const int blk = a.block_tables[(int64_t)at.r * a.max_blocks + lp];
+    const int s = tid / CPR, c = tid % CPR;
+    const int64_t row = (int64_t)at.cu + (int64_t)lp * kPage - at.P + s;
+    const int pos = lp * kPage + s;
+    const bool ok = head_ok && s >= s0 && s < s1 && row >= 0 && row < a.total_tokens && pos < ra.num_positions;
+    const int half = ra.rotary_dim / 16;
+    const bool turned = c < 2 * half;
+    u32x4 key = u32x4{0u, 0u, 0u, 0u}, v = key;
+    float cs[8] = {}, sn[8] = {};
+    if (ok) {
+        key = *reinterpret_cast<const u32x4*>(a.k_new + row * ra.k_stride + h * D + c * 8);
+        v = *reinterpret_cast<const u32x4*>(a.v_new + row * ra.v_stride + h * D + c * 8);
+        if (turned) {
+            const float* table = ra.table + (int64_t)pos * ra.rotary_dim;
+            if (ra.interleaved)
+                load_angles<4>(table + 8 * c, cs, sn);
+            else
+                load_angles<8>(table + 16 * (c < half ? c : c - half), cs, sn);
+        }
+    }
+    float x[8], y[8];
+    widen8(key, x);
+    widen8(v, y);
+    if (ra.interleaved) {
+        if (turned) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const double p = x[2 * j], q = x[2 * j + 1], co = cs[j], si = sn[j];
+                x[2 * j] = (float)fma(p, co, -(q * si));
+                x[2 * j + 1] = (float)fma(q, co, p * si);
+            }
+        }
+    } else if (half > 0) {
+        const int lane = threadIdx.x & 63;
+        const int from = turned ? lane + (c < half ? half : -half) : lane;
+        u32x4 other;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[i] = (uint32_t)__shfl((int)key[i], from);
+        if (turned) {
+            float z[8];
+            widen8(other, z);
+            const double low = c < half ? -1.0 : 1.0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = (float)fma((double)x[j], (double)cs[j], low * ((double)z[j] * (double)sn[j]));
+        }
+    }
+    uint32_t kt = 0, vt = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        kt = max(kt, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+        vt = max(vt, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+    }
+    const uint32_t ks = fp4_scale_code(quad_max(kt)), vs = fp4_scale_code(quad_max(vt));
+    if (!ok || blk < 0 || blk >= a.num_blocks) return;
+    const int64_t slot = ((int64_t)blk * a.num_kv_heads + h) * kPage + s;
+    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.k_pool) + slot * (D / 2) + c * 4) = fp4_quantise8(x, ks);
+    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v_pool) + slot * (D / 2) + c * 4) = fp4_quantise8(y, vs);
+    if (c % 4 == 0) *reinterpret_cast<uint16_t*>(ra.scales + (slot * kBlocks + c / 4) * 2) = (uint16_t)(ks | vs << 8);
+}
+
 // kRotQHeads query heads (group qg) of the tokens of one page.
 template <int D, bool STREAM>
 __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int qg) {
@@ -225,7 +300,7 @@ __device__ __forceinline__ void rotary_q(const RotaryArgs& ra, const PageUnit& a
     }
 }
 
-template <int D, bool FP8, bool STREAM>
+template <int D, Pool KIND, bool STREAM>
 __global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(const RotaryArgs ra) {
     __shared__ AppendLds<D> lds;
     const AppendArgs& a = ra.a;
@@ -240,10 +315,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_rotary_kernel(const Rot
     const int s1 = min(at.P + at.n - lp * kPage, kPage);
     if (lp >= a.max_blocks) return;
     const int kv_jobs = ceil_div(a.num_kv_heads, append_heads(D));
-    if (job < kv_jobs)
-        rotary_kv<D, FP8>(ra, lds, at, lp, s0, s1, job);
-    else
+    if (job >= kv_jobs)
         rotary_q<D, STREAM>(ra, at, lp, s0, s1, job - kv_jobs);
+    else if constexpr (KIND == Pool::kFp4)
+        rotary_kv_fp4<D>(ra, at, lp, s0, s1, job);
+    else
+        rotary_kv<D, KIND == Pool::kFp8>(ra, lds, at, lp, s0, s1, job);
 }
 
 }  // namespace
@@ -252,15 +329,25 @@ int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int 
     return pages * (ceil_div(num_kv_heads, append_heads(head_dim)) + (with_q ? ceil_div(num_q_heads, kRotQHeads) : 0));
 }
 
-template <int D, bool FP8>
+template <int D, Pool KIND>
 static void launch_rotary(const RotaryArgs& ra, bool stream, unsigned grid, hipStream_t s) {
     if (stream)
-        append_rotary_kernel<D, FP8, true><<<grid, kAppendThreads, 0, s>>>(ra);
+        append_rotary_kernel<D, KIND, true><<<grid, kAppendThreads, 0, s>>>(ra);
     else
-        append_rotary_kernel<D, FP8, false><<<grid, kAppendThreads, 0, s>>>(ra);
+        append_rotary_kernel<D, KIND, false><<<grid, kAppendThreads, 0, s>>>(ra);
 }
 
-hipError_t launch_append_rotary(const RotaryArgs& args, int head_dim, bool fp8, hipStream_t s) {
+template <int D>
+static void launch_rotary_kind(const RotaryArgs& ra, Pool kind, bool stream, unsigned grid, hipStream_t s) {
+    if (kind == Pool::kFp4)
+        launch_rotary<D, Pool::kFp4>(ra, stream, grid, s);
+    else if (kind == Pool::kFp8)
+        launch_rotary<D, Pool::kFp8>(ra, stream, grid, s);
+    else
+        launch_rotary<D, Pool::kBf16>(ra, stream, grid, s);
+}
+
+hipError_t launch_append_rotary(const RotaryArgs& args, int head_dim, Pool kind, hipStream_t s) {
     RotaryArgs ra = args;
     if (ra.a.total_pages <= 0) return hipSuccess;
     const bool with_q = ra.q != nullptr;
@@ -269,9 +356,9 @@ hipError_t launch_append_rotary(const RotaryArgs& args, int head_dim, bool fp8, 
     const bool stream = with_q && (int64_t)ra.a.total_tokens * ra.num_q_heads * head_dim * 2 >= (192LL << 20);
     const unsigned grid = ra.jobs * (unsigned)ra.a.total_pages;
     if (head_dim == 128)
-        fp8 ? launch_rotary<128, true>(ra, stream, grid, s) : launch_rotary<128, false>(ra, stream, grid, s);
+        launch_rotary_kind<128>(ra, kind, stream, grid, s);
     else
-        fp8 ? launch_rotary<64, true>(ra, stream, grid, s) : launch_rotary<64, false>(ra, stream, grid, s);
+        launch_rotary_kind<64>(ra, kind, stream, grid, s);
     return hipGetLastError();
 }
 

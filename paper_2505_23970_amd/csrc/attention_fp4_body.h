@@ -1,0 +1,689 @@
+// Attention over 4-bit pools for gfx950 (device code of the small, 128-row and wide tiles): the same causal
+// attention, work lists and merge as over the other pools (attention_small_body.h, attention_kernels.h), with the
+// operands made for pages of E2M1 codes and block scales (fp4.h).
+//
+// Scores. The matrix cores take the key codes and their scales as they lie in the pool: a scaled product of
+// 16 keys by 16 query rows over 128 elements, whose first operand is E2M1 with one scale per row and 32 elements.
+// Its second operand has 8 bits at most, so a query row goes in twice, as two E4M3 numbers per element: with
+// 2^E the row's scale (largest magnitude in [128, 256)),
+//     h = E4M3(q 2^-E),   l = E4M3((q 2^-E - h) 2^5),   q = (h + l 2^-5) 2^E
+// h has 4 significant bits and the rest of a bf16 number has 4, so the sum is q itself for elements from
+// 2^-14 of the row's largest on, and off by at most 2^-22 of the largest below: no more than the fp32 accumulators
+// are. Two such products take the time of the four bf16 ones they replace, and the keys need no conversion:
+// with D = 64 one product takes both, keys twice along k against h and l.
+// Operand layout of the product (lane group G = lane / 16, row or column lane % 16): the codes are elements
+// 32 G .. + 31, with that lane's scale; the 8-bit operand's bytes are elements 16 G .. + 15 and 64 + 16 G .. + 15,
+// with the scale of elements 32 G .. + 31 in lane group G.
+// Values are widened to bf16 (exact) once per workgroup and tile, scales included, into rows of LDS,
+// and read transposed (each 16 lanes a 16 x 4 block) as the V^T operand, with
+//     O^T (D x rows) += V^T . P^T   in 16x16x32 bf16 products, as over the other pools.
+// A value block that held a NaN makes the rows NaN that see its token and no other: in tiles where some row sees
+// some key not, such blocks are zeroed and the rows that see them get the NaN afterwards.
+#pragma once
+#include "attention_kernels.h"
+#include "fp4.h"
+
+namespace gc {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+
+__device__ __forceinline__ f32x4 mfma_fp4_fp8(const u32x4 k, const i32x8 q, const f32x4 c, uint32_t k_scale, uint32_t q_scale) {
+    const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, 0, (int)k_scale, 0, (int)q_scale);
+}
+
+// A query row as operands of those products. D = 128: w[0] the h, w[1] the l; D = 64: both in w[0].
+template <int D>
+struct QueryRow {
+    static constexpr int kParts = D / 64;
+    i32x8 w[kParts];
+    uint32_t scale[kParts];  // of the product's 32 elements of this lane group
+
+    // q: the row (head_dim bf16 values); ok: false gives zeros
+    __device__ __forceinline__ void load(const uint16_t* q, bool ok, int g4) {
+        u32x4 x[2 * kParts];
+#pragma unroll
+        for (int i = 0; i < 2 * kParts; ++i)
+            x[i] = ok ? *reinterpret_cast<const u32x4*>(q + 64 * (i >> 1) + 16 * g4 + 8 * (i & 1)) : u32x4{0u, 0u, 0u, 0u};
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 2 * kParts; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) top = max(top, max(x[i][v] & 0x7FFFu, (x[i][v] >> 16) & 0x7FFFu));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        // largest magnitude 2^7 .. 2^8 in units of the scale; the l's scale is 2^-5 of it
+        const uint32_t e = (uint32_t)max((int)(top >> 7) - 7, 6);
+        const float inv = __uint_as_float((254u - e) << 23);
+        uint32_t hi[4 * kParts], lo[4 * kParts];
+#pragma unroll
+        for (int i = 0; i < 4 * kParts; ++i) {
+            // four elements
+            const uint32_t w0 = x[i >> 1][2 * (i & 1)], w1 = x[i >> 1][2 * (i & 1) + 1];
+            const float f0 = __uint_as_float(w0 << 16) * inv, f1 = __uint_as_float(w0 & 0xFFFF0000u) * inv;
+            const float f2 = __uint_as_float(w1 << 16) * inv, f3 = __uint_as_float(w1 & 0xFFFF0000u) * inv;
+            int h = __builtin_amdgcn_cvt_pk_fp8_f32(f0, f1, 0, false);
+            h = __builtin_amdgcn_cvt_pk_fp8_f32(f2, f3, h, true);
+            const auto b0 = __builtin_amdgcn_cvt_pk_f32_fp8(h, false);
+            const auto b1 = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+            int l = __builtin_amdgcn_cvt_pk_fp8_f32((f0 - b0[0]) * 32.f, (f1 - b0[1]) * 32.f, 0, false);
+            l = __builtin_amdgcn_cvt_pk_fp8_f32((f2 - b1[0]) * 32.f, (f3 - b1[1]) * 32.f, l, true);
+            hi[i] = (uint32_t)h;
+            lo[i] = (uint32_t)l;
+        }
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[0][i] = (int)hi[i];
+                w[kParts - 1][i] = (int)lo[i];
+            }
+            scale[0] = e;
+            scale[kParts - 1] = e - 5;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[0][i] = (int)hi[i];
+                w[0][4 + i] = (int)lo[i];
+            }
+            scale[0] = g4 < 2 ? e : e - 5;
+        }
+    }
+    // scores of 16 keys (codes k and their scales, as this lane's operand)
+    __device__ __forceinline__ f32x4 scores(const u32x4 k, uint32_t k_scale) const {
+        f32x4 s = mfma_fp4_fp8(k, w[0], f32x4{0.f, 0.f, 0.f, 0.f}, k_scale, scale[0]);
+        if constexpr (kParts == 2) s = mfma_fp4_fp8(k, w[1], s, k_scale, scale[1]);
+        return s;
+    }
+};
+
+// Value rows of a tile in LDS: row `key`, D bf16 values; its 32-byte pieces (16 values) are swizzled by the row so that
+// the four rows of a transposed read, and eight rows of two of them, lie in different banks.
+template <int D>
+__device__ __forceinline__ uint32_t value_at(int key, int piece) {
+    const int sw = D == 128 ? key & 7 : (key >> 1) & 3;
+    return (uint32_t)(key * 2 * D + (piece ^ sw) * 32);
+}
+
+// Four elements (keys) of one value column: lane i of 16 gives the address of elements 4 (i % 4) .. + 3 of row i / 4
+// and gets column i of the four rows.
+__device__ __forceinline__ u32x2 read_transposed(const unsigned char* at) {
+    typedef __attribute__((address_space(3))) i16x4* lds_i16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(lds_byte*)at));
+}
+
+// ---------------------------------------------------------------- small tiles
+// Query tiles of 16 rows, key tiles of 32 (two pages), one wavefront a work item, as over the other pools. What
+// bounds it: HBM. A page of codes is 1 KiB (D = 128) that 64 lanes load as they are multiplied: lane (row j, group G) takes
+// block G of key j, 16 bytes, straight into the operand's registers, with its two scales (key, value) beside; kRing
+// tiles are in flight in registers. Values go through 8 KiB of LDS of the wavefront's own for their transposition.
+template <int D>
+constexpr int kFp4SmallLds = kDecN * D * 2;
+
+template <int D>
+__device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkItem it, const int kvh, unsigned char* vbuf) {
+    constexpr int DB = D / 16;
+    constexpr int NB = D / kFp4Block;
+    constexpr int kPageCodes = kPage * D / 2;
+    constexpr int kPageScales = kPage * NB * 2;
+    constexpr int NV = D / 64;  // value loads of a tile: a page each, or half a page of each in one
+    constexpr int kRing = 4;
+    const int lane = threadIdx.x & 63;
+    if (it.r < 0 || it.kt_begin >= it.kt_end) return;
+    const int P = it.P, cu = it.cu, n = it.n;
+    const int L = item_keys(it);
+    const int ntok = min(a.tq, n - it.q0);
+    const int g4 = lane >> 4, j = lane & 15;
+    const int t = (int)((unsigned)j / (unsigned)a.group);
+    const int hl = j - t * a.group;
+    const bool row_ok = t < ntok;
+    const int lim = P + it.q0 + (row_ok ? t : 0);
+    const int64_t qrow = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + hl;
+
+    const scalar_i32p table = (scalar_i32p)(a.block_tables + (int64_t)it.r * a.max_blocks);
+    const int blk = g4 % NB;  // block of the row that this lane holds (keys; values of vpage)
+    const uint32_t code_off = (uint32_t)(j * (D / 2) + blk * 16);
+    const uint32_t scale_off = (uint32_t)((j * NB + blk) * 2);
+    const int vpage = D == 128 ? 0 : g4 >> 1;  // D = 64: the page of this lane's values
+    const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
+    const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
+    const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
+
+    struct Tile {
+        u32x4 k[2], v[NV];
+        uint32_t s[2];
+    };
+    // (pages past the table row or the sequence, or with an id outside the pool, are read from block 0: their
+    // keys are masked, their values zeroed)
+    auto load = [&](int kt, Tile& x) {
+        int64_t b[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int lp = kt * 2 + p;
+            const int id = table[min(lp, a.max_blocks - 1)];
+            const bool ok = (lp < a.max_blocks) & (lp * kPage < L) & (id >= 0) & (id < a.num_blocks);
+            b[p] = (int64_t)(ok ? id : 0) * a.num_kv_heads;
+            x.k[p] = *reinterpret_cast<const u32x4*>(kbase + b[p] * kPageCodes + code_off);
+            x.s[p] = *reinterpret_cast<const uint16_t*>(sbase + b[p] * kPageScales + scale_off);
+            if constexpr (D == 128) x.v[p] = *reinterpret_cast<const u32x4*>(vbase + b[p] * kPageCodes + code_off);
+        }
+        if constexpr (D == 64) x.v[0] = *reinterpret_cast<const u32x4*>(vbase + (vpage ? b[1] : b[0]) * kPageCodes + code_off);
+    };
+
+    Tile ring[kRing];
+#pragma unroll
+    for (int i = 0; i < kRing; ++i)
+        if (it.kt_begin + i < it.kt_end) load(it.kt_begin + i, ring[i]);
+    QueryRow<D> q;
+    q.load(a.q + qrow * D, row_ok, g4);
+
+    // where this lane's values go (row: its key of the tile) and where it reads transposed ones
+    uint32_t v_from[DB];
+    {
+        const int r = 4 * g4 + (j >> 2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) v_from[db] = value_at<D>(r, db) + 8 * (j & 3);
+    }
+
+    f32x4 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+    const float c = a.scale_log2;
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+
+    auto tile = [&](int kt, Tile& x) {
+        const int key0 = kt * kDecN;
+        const bool masked = key0 + kDecN - 1 > P + it.q0;  // some row does not see some key
+        // values: widened, into LDS
+        uint64_t nan[NV] = {};  // lanes whose block is NaN and within the sequence
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int key = (D == 128 ? kPage * i : kPage * vpage) + j;
+            const uint32_t vs = (D == 128 ? x.s[i] : vpage ? x.s[1] : x.s[0]) >> 8;
+            uint32_t keep = 0xFFFFFFFFu;
+            if (masked) {
+                const bool in = key0 + key < L;
+                nan[i] = __ballot(in && vs == kFp4Nan);
+                keep = in && vs != kFp4Nan ? keep : 0u;
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t b[4];
+                fp4_widen8(x.v[i][w], fp4_scale(vs), b);
+                *reinterpret_cast<u32x4*>(vbuf + value_at<D>(key, 2 * blk + (w >> 1)) + 16 * (w & 1)) =
+                    u32x4{b[0] & keep, b[1] & keep, b[2] & keep, b[3] & keep};
+            }
+        }
+        // s[p][v] is the score of tile key 16 p + 4 g4 + v
+        f32x4 s[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) s[p] = q.scores(x.k[p], x.s[p]);
+        if (kt + kRing < it.kt_end) load(kt + kRing, x);
+        const int rel = lim - key0;
+        if (masked) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) s[p][v] = (16 * p + 4 * g4 + v > rel) ? -INFINITY : s[p][v];
+        }
+        const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                               fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        const float m_new = fmaxf(m_run, row_max4(mx) * c);
+        if (__any(m_new > m_run)) {
+            const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        }
+        const float m_use = (m_run == -INFINITY) ? 0.f : m_run;
+        u32x4 pw;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1)], c, -m_use));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[i >> 1][2 * (i & 1) + 1], c, -m_use));
+            const bf16x2 pair = {(__bf16)p0, (__bf16)p1};
+            l_run = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, l_run, false);
+            pw[i] = __builtin_bit_cast(uint32_t, pair);
+        }
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+        wave_lds_sync();
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            const u32x2 lo = read_transposed(vbuf + v_from[db]);
+            const u32x2 hi = read_transposed(vbuf + v_from[db] + kPage * 2 * D);
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[db], 0, 0, 0);
+        }
+        wave_lds_sync();
+        if (masked) {
+            // value blocks that held a NaN: bit 16 g + j of `nan` is (key j of page i, block g), or for D = 64
+            // (key j of page g / 2, block g % 2)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (nan[i] == 0) continue;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const uint32_t keys = (uint32_t)(nan[i] >> (16 * g)) & 0xFFFFu;
+                    const int seen = rel - kPage * (D == 128 ? i : g >> 1);  // keys 0 .. seen of the page
+                    const uint32_t sees = seen < 0 ? 0u : 0xFFFFu >> (15 - min(seen, 15));
+                    const float add = (keys & sees) != 0 ? __builtin_nanf("") : 0.f;
+                    const int b = D == 128 ? g : g & 1;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        o[2 * b][v] += add;
+                        o[2 * b + 1][v] += add;
+                    }
+                }
+            }
+        }
+    };
+
+    for (int kt = it.kt_begin; kt < it.kt_end; kt += kRing) {
+#pragma unroll
+        for (int i = 0; i < kRing; ++i)
+            if (kt + i < it.kt_end) tile(kt + i, ring[i]);
+    }
+
+    const float l_tot = row_sum4(l_run);
+    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    // (a split item passes a NaN sum on to the merge)
+    const float lse_v = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : (it.part >= 0 && l_tot != l_tot ? l_tot : -INFINITY);
+    // o[db][v] is element d = 16 db + 4 g4 + v of row j
+    if (!row_ok) return;
+    if (it.part < 0) {
+        uint16_t* op = a.out + qrow * D + 4 * g4;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            u32x2 w;
+            w[0] = pack_pair(o[db][0] * inv, o[db][1] * inv);
+            w[1] = pack_pair(o[db][2] * inv, o[db][3] * inv);
+            *reinterpret_cast<u32x2*>(op + 16 * db) = w;
+        }
+        if (a.lse != nullptr && g4 == 0) a.lse[qrow] = lse_v;
+    } else {
+        const int64_t prow = ((int64_t)it.part * a.num_kv_heads + kvh) * kDecM + j;
+        float* po = a.part_o + prow * D + 4 * g4;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = o[db] * inv;
+        if (g4 == 0) a.part_lse[prow] = lse_v;
+    }
+}
+
+// ---------------------------------------------------------------- 128-row and wide tiles
+// Query tiles of 32 rows a wavefront, key tiles of 64 (four pages), double buffered. Pages of key codes and of scales are
+// copied straight into LDS and multiplied as they are; the values' codes go through registers and are widened into LDS
+// after the tile's products. What bounds it: the matrix cores and the softmax's vector instructions, as over
+// the other pools; against 8-bit pools a tile has no keys to widen and half the value codes.
+template <int D, int WAVES>
+struct Fp4Lds {
+    static constexpr int kValueBytes = kBlockN * D * 2;
+    static constexpr int kCodeBytes = kBlockN * D / 2;
+    static constexpr int kScaleBytes = kBlockN * (D / kFp4Block) * 2;
+    __align__(16) unsigned char v[2][kValueBytes];
+    __align__(16) unsigned char k[2][kCodeBytes];
+    __align__(16) unsigned char s[2][kScaleBytes];
+};
+
+// Direct global->LDS copies with an address of their own per lane: lane i's 16 (4) bytes land at lds + 16 i (4 i).
+// As dma16 (attention_kernels.h): the compiler does not track them, every wait is explicit.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const unsigned char* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const unsigned char* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int D, int WAVES>
+__device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const unsigned bid, Fp4Lds<D, WAVES>& lds) {
+    constexpr int ROWS = kRowsPerWave;
+    constexpr int RB = ROWS / 16;
+    constexpr int KB = kBlockN / 16;   // key blocks (pages) of a tile
+    constexpr int DB = D / 16;
+    constexpr int NB = D / kFp4Block;
+    constexpr int kPageCodes = kPage * D / 2;
+    constexpr int kPageScales = kPage * NB * 2;
+    constexpr int kTileLog2Thresh = 8;
+
+    int tid_opaque = (int)threadIdx.x;  // (lane constants per work item, not held across a resident launch's items)
+    asm volatile("" : "+v"(tid_opaque));
+    const int tid = tid_opaque, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g4 = lane >> 4, j16 = lane & 15;
+    const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
+    const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
+    asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P), "s"(it.cu), "s"(it.n));
+    if (it.r < 0 || it.kt_begin >= it.kt_end) return;
+    const int P = it.P, cu = it.cu, n = it.n;
+    const int L = item_keys(it);
+    const int ntok = min(a.tq, n - it.q0);
+
+    bool row_ok[RB];
+    int lim[RB];  // last key the row may see
+    int64_t qrow[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int m = wave * ROWS + 16 * rb + j16;
+        const int t = (int)((unsigned)m / (unsigned)a.group);
+        row_ok[rb] = t < ntok;
+        lim[rb] = P + it.q0 + (row_ok[rb] ? t : 0);
+        qrow[rb] = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group);
+    }
+
+    // Block ids of a tile's pages: entry p in lanes with lane % 4 == p (clamped into the row). A page past the table
+    // row or the sequence, or with an id outside the pool, is taken from block 0: its keys are masked, its values zeroed.
+    const int32_t* const table = a.block_tables + (int64_t)it.r * a.max_blocks;
+    auto fetch_ids = [&](int kt) -> int { return table[(uint32_t)min(kt * 4 + (lane & 3), a.max_blocks - 1)]; };
+    auto checked = [&](int kt, int ids) -> int {
+        const int lp = kt * 4 + (lane & 3);
+        return lp < a.max_blocks && lp * kPage < L && ids >= 0 && ids < a.num_blocks ? ids : 0;
+    };
+    int ids = fetch_ids(it.kt_begin);
+
+    QueryRow<D> q[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) q[rb].load(a.q + qrow[rb] * D, row_ok[rb], g4);
+
+    // Key codes: 1 KiB copies, a page (D = 128) or two (D = 64) each, by the first wavefronts. Lane i brings 16-byte
+    // block i % NB (swizzled at D = 128, so that the reads of eight neighbouring rows lie in different banks) of row i / NB.
+    constexpr int kKeyCopies = KB * kPageCodes / 1024;
+    constexpr int kPagesPerCopy = KB / kKeyCopies;
+    const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
+    const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
+    const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
+    const uint32_t k_lds = lds_address(lds.k[0]), s_lds = lds_address(lds.s[0]);
+    auto key_swizzle = [](int row) { return D == 128 ? (row >> 2) & 3 : 0; };
+    const int copy_row = lane / NB % kPage;
+    const uint32_t key_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ key_swizzle(copy_row)) * 16);
+    // Scales: 256-byte copies of two (four) pages
+    constexpr int kScaleCopies = KB * kPageScales / 256;
+    constexpr int kScalePages = KB / kScaleCopies;
+    static_assert(kKeyCopies <= WAVES && kScaleCopies <= WAVES, "copies");
+    constexpr int kScaleWave = WAVES >= kKeyCopies + kScaleCopies ? kKeyCopies : 0;
+    auto copy_tile = [&](int buf, int okids) {
+        if (wave < kKeyCopies) {
+            const int64_t b = __shfl(okids, wave * kPagesPerCopy + lane / (64 / kPagesPerCopy));
+            copy16(kbase + b * a.num_kv_heads * kPageCodes + key_from,
+                   k_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kCodeBytes) + (uint32_t)wave * 1024u);
+        }
+        if (wave >= kScaleWave && wave < kScaleWave + kScaleCopies) {
+            const int w = wave - kScaleWave;
+            const int64_t b = __shfl(okids, w * kScalePages + lane / (64 / kScalePages));
+            copy4(sbase + b * a.num_kv_heads * kPageScales + lane % (64 / kScalePages) * 4,
+                  s_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kScaleBytes) + (uint32_t)w * 256u);
+        }
+    };
+    // Values: thread t takes elements kPer t .. of the tile's [64][D], which lie in one row and one block.
+    constexpr int kPer = kBlockN * D / (WAVES * 64);  // 32, 16 or 8
+    constexpr int kWords = kPer / 8;
+    const int v_key = tid * kPer / D, v_el = tid * kPer % D;
+    const int v_page = wave * 64 * kPer / (kPage * D);
+    uint32_t vc[kWords], vs = 0;
+    auto load_values = [&](int okids) {
+        const int64_t b = (int64_t)__builtin_amdgcn_readlane(okids, v_page) * a.num_kv_heads;
+        const unsigned char* const from = vbase + b * kPageCodes + (v_key % kPage) * (D / 2) + v_el / 2;
+        if constexpr (kWords == 4) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vc[i] = w[i];
+        } else if constexpr (kWords == 2) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(from);
+            vc[0] = w[0];
+            vc[1] = w[1];
+        } else {
+            vc[0] = *reinterpret_cast<const uint32_t*>(from);
+        }
+        vs = (sbase + b * kPageScales)[((v_key % kPage) * NB + v_el / kFp4Block) * 2 + 1];
+    };
+    const int first_masked = P + it.q0;  // tiles that reach past this key hide some key from some row
+    auto store_values = [&](int buf, int kt) {
+        uint32_t keep = 0xFFFFFFFFu;
+        if (kt * kBlockN + kBlockN - 1 > first_masked) keep = kt * kBlockN + v_key < L && vs != kFp4Nan ? keep : 0u;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+            uint32_t b[4];
+            fp4_widen8(vc[w], fp4_scale(vs), b);
+            const int e = v_el / 8 + w;  // 16 bytes of the row
+            *reinterpret_cast<u32x4*>(lds.v[buf] + value_at<D>(v_key, e >> 1) + 16 * (e & 1)) =
+                u32x4{b[0] & keep, b[1] & keep, b[2] & keep, b[3] & keep};
+        }
+    };
+
+    f32x4 o[RB][DB];
+    float m_run[RB], neg_off[RB], l_run[RB];
+    bool need_max, exact = false;  // (the exponent offset, as in attention_kernels.h)
+    const float c = a.scale_log2;
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+
+    const uint32_t k_at = (uint32_t)(j16 * (D / 2) + ((g4 % NB) ^ key_swizzle(j16)) * 16);
+    const uint32_t s_at = (uint32_t)((j16 * NB + g4 % NB) * 2);
+    uint32_t v_from[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) v_from[db] = value_at<D>(4 * g4 + (j16 >> 2), db) + 8 * (j16 & 3);
+
+    auto compute_tile = [&](int buf, int kt) {
+        const unsigned char* const kb = lds.k[buf];
+        const unsigned char* const sb = lds.s[buf];
+        const unsigned char* const vb = lds.v[buf];
+        u32x4 kf[KB];
+        uint32_t ks[KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            kf[b] = *reinterpret_cast<const u32x4*>(kb + b * kPageCodes + k_at);
+            ks[b] = *reinterpret_cast<const uint16_t*>(sb + b * kPageScales + s_at);
+        }
+        // s[rb][b][v] is the score of row 16 rb + j16 and tile key 16 b + 4 g4 + v
+        f32x4 s[RB][KB];
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) s[rb][b] = q[rb].scores(kf[b], ks[b]);
+
+        const int key0 = kt * kBlockN;
+        const bool masked = key0 + kBlockN - 1 > first_masked;
+        if (masked) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int rel = lim[rb] - key0 - 4 * g4;
+#pragma unroll
+                for (int b = 0; b < KB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) s[rb][b][v] = (16 * b + v > rel) ? -INFINITY : s[rb][b][v];
+            }
+        }
+        if (need_max) {
+            need_max = exact;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                float mx = s[rb][0][0];
+#pragma unroll
+                for (int e = 1; e < 4 * KB; ++e) mx = __builtin_elementwise_maximum(mx, s[rb][e >> 2][e & 3]);
+                {
+                    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                    mx = __builtin_elementwise_maximum(__uint_as_float(x[0]), __uint_as_float(x[1]));
+                    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                    mx = __builtin_elementwise_maximum(__uint_as_float(y[0]), __uint_as_float(y[1]));
+                }
+                const float m_tile = mx * c;
+                if (__any(m_tile > m_run[rb] + kTileLog2Thresh)) {
+                    const float m_new = fmaxf(m_run[rb], m_tile);
+                    const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[rb] - m_new);
+                    m_run[rb] = m_new;
+                    l_run[rb] *= alpha;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) o[rb][db] *= alpha;
+                }
+                need_max |= __any(m_run[rb] == -INFINITY);
+                neg_off[rb] = m_run[rb] == -INFINITY ? 0.f : -m_run[rb];
+            }
+        }
+        bf16x8 pf[RB][2];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int qq = 0; qq < 4; ++qq)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const f32x4 x = s[rb][2 * hb + (qq >> 1)];
+                    const bf16x2 pq = {(__bf16)__builtin_amdgcn_exp2f(fmaf(x[2 * (qq & 1)], c, neg_off[rb])),
+                                       (__bf16)__builtin_amdgcn_exp2f(fmaf(x[2 * (qq & 1) + 1], c, neg_off[rb]))};
+                    pf[rb][hb][2 * qq] = pq[0];
+                    pf[rb][hb][2 * qq + 1] = pq[1];
+                    l_run[rb] = __builtin_amdgcn_fdot2_f32_bf16(pq, ones, l_run[rb], false);
+                }
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const u32x2 lo = read_transposed(vb + v_from[db] + (2 * hb) * kPage * 2 * D);
+                const u32x2 hi = read_transposed(vb + v_from[db] + (2 * hb + 1) * kPage * 2 * D);
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][hb], o[rb][db], 0, 0, 0);
+            }
+        if (masked) {
+            // value blocks that held a NaN (lane = key of the tile)
+            uint64_t nan[NB];
+            uint64_t any = 0;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                nan[b] = __ballot(key0 + lane < L && sb[(lane * NB + b) * 2 + 1] == kFp4Nan);
+                any |= nan[b];
+            }
+            if (any != 0) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const int seen = lim[rb] - key0;  // keys 0 .. seen of the tile
+                    const uint64_t sees = seen < 0 ? 0ull : ~0ull >> (63 - min(seen, 63));
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        const float add = (nan[db / 2] & sees) != 0 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) o[rb][db][v] += add;
+                    }
+                }
+            }
+        }
+    };
+
+    int kt = it.kt_begin;
+    auto step = [&](const int cur) {
+        const bool more = kt + 1 < it.kt_end;
+        if (more) {
+            const int okids = checked(kt + 1, ids);
+            copy_tile(1 - cur, okids);
+            load_values(okids);
+            if (kt + 2 < it.kt_end) ids = fetch_ids(kt + 2);
+        }
+        compute_tile(cur, kt);
+        if (more) store_values(1 - cur, kt + 1);
+        wait_vmem<0>();
+        __syncthreads();
+    };
+    for (;;) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+            m_run[rb] = -INFINITY;
+            neg_off[rb] = 0.f;
+            l_run[rb] = 0.f;
+        }
+        need_max = true;
+        kt = it.kt_begin;
+        if (exact) ids = fetch_ids(kt);
+        {
+            const int okids = checked(kt, ids);
+            copy_tile(0, okids);
+            load_values(okids);
+            if (kt + 1 < it.kt_end) ids = fetch_ids(kt + 1);
+            store_values(0, kt);
+        }
+        wait_vmem<0>();
+        __syncthreads();
+        while (true) {
+            step(0);
+            if (++kt >= it.kt_end) break;
+            step(1);
+            if (++kt >= it.kt_end) break;
+        }
+        if (exact || !__syncthreads_or(!(l_run[0] <= 0x1p100f) || !(l_run[RB - 1] <= 0x1p100f))) break;
+        exact = true;
+    }
+
+    float inv[RB], lse_v[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const float l = row_sum4(l_run[rb]);
+        inv[rb] = l > 0.f ? 1.f / l : 0.f;
+        lse_v[rb] = l > 0.f ? (m_run[rb] + log2f(l)) * kLn2 : (it.part >= 0 && l != l ? l : -INFINITY);
+    }
+    // o[rb][db][v] is element d = 16 db + 4 g4 + v of row 16 rb + j16. Rows go through LDS (the values' buffers, no longer
+    // read), so that a store covers whole rows: each wavefront a part of its own, as many of its rows at a time as fit.
+    constexpr int kStage = 2 * Fp4Lds<D, WAVES>::kValueBytes / WAVES;
+    unsigned char* const stage = lds.v[0] + wave * kStage;
+    auto through_stage = [&](auto out_bytes, auto&& put, auto&& get) {
+        constexpr int kOutRow = decltype(out_bytes)::value;
+        constexpr int CH = kOutRow / 16;
+        constexpr int kRows = kStage / kOutRow < ROWS ? kStage / kOutRow : ROWS;
+        constexpr int kSw = (CH < 16 ? CH : 16) - 1;  // chunk swizzle
+        static_assert(ROWS % kRows == 0 && kRows * CH % 64 == 0, "stage");
+#pragma unroll
+        for (int r0 = 0; r0 < ROWS; r0 += kRows) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int sr = 16 * rb + j16 - r0;
+                if (sr < 0 || sr >= kRows) continue;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+                    put(rb, db, [&](int ch) { return stage + sr * kOutRow + (ch ^ (sr & kSw)) * 16; });
+            }
+            wave_lds_sync();
+#pragma unroll
+            for (int i = 0; i < kRows * CH / 64; ++i) {
+                const int x = i * 64 + lane, sr = x / CH, ch = x % CH;
+                get(r0 + sr, ch, *reinterpret_cast<const u32x4*>(stage + sr * kOutRow + (ch ^ (sr & kSw)) * 16));
+            }
+            wave_lds_sync();
+        }
+    };
+    if (it.part < 0) {
+        through_stage(std::integral_constant<int, 2 * D>{},
+            [&](int rb, int db, auto&& at) {
+                u32x2 w;
+                w[0] = pack_bf16x2(o[rb][db][0] * inv[rb], o[rb][db][1] * inv[rb]);
+                w[1] = pack_bf16x2(o[rb][db][2] * inv[rb], o[rb][db][3] * inv[rb]);
+                *reinterpret_cast<u32x2*>(at(2 * db + (g4 >> 1)) + 8 * (g4 & 1)) = w;
+            },
+            [&](int row, int ch, const u32x4 w) {
+                const int m = wave * ROWS + row;
+                const int t = (int)((unsigned)m / (unsigned)a.group);
+                if (t < ntok)
+                    *reinterpret_cast<u32x4*>(a.out + ((int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group)) * D + ch * 8) = w;
+            });
+        if (a.lse != nullptr && g4 == 0) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                if (row_ok[rb]) a.lse[qrow[rb]] = lse_v[rb];
+        }
+    } else {
+        const int64_t prow0 = ((int64_t)it.part * a.num_kv_heads + kvh) * (WAVES * ROWS) + wave * ROWS;
+        through_stage(std::integral_constant<int, 4 * D>{},
+            [&](int rb, int db, auto&& at) { *reinterpret_cast<f32x4*>(at(4 * db + g4)) = o[rb][db] * inv[rb]; },
+            [&](int row, int ch, const u32x4 w) { *reinterpret_cast<u32x4*>(a.part_o + (prow0 + row) * D + ch * 4) = w; });
+        if (g4 == 0) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) a.part_lse[prow0 + 16 * rb + j16] = lse_v[rb];
+        }
+    }
+}
+
+}  // namespace
+}  // namespace gc

@@ -242,6 +242,9 @@ inline WorkspaceLayout workspace_layout(int batch, int64_t items, int64_t combin
 }
 
 // ---------------------------------------------------------------- kernel launch arguments
+// What a pool holds: bf16 elements, E4M3 codes with one scale, E2M1 codes with scales of their own (fp4.h).
+enum class Pool { kBf16, kFp8, kFp4 };
+
 struct AppendArgs {
     const uint16_t* k_new;
     const uint16_t* v_new;
@@ -264,6 +267,16 @@ struct RotaryArgs {
     int64_t q_stride, k_stride, v_stride;
     int32_t num_q_heads, num_positions, rotary_dim, interleaved;
     uint32_t jobs, by_page;  // workgroups of a page; launched page by page (else head by head)
+    uint8_t* scales;         // 4-bit pools: [blocks][Hkv][16][D / 32][key, value]
+};
+
+// Rows out of a pool: keys and values at the positions that an append of the batch writes.
+struct ReadArgs {
+    AppendArgs a;      // (k_new, v_new, k_inv and v_inv unread)
+    uint16_t *k_out, *v_out;  // [T][Hkv][D]
+    const uint8_t* scales;    // 4-bit pools
+    float k_scale, v_scale;   // 8-bit pools
+    uint32_t jobs;            // workgroups of a page
 };
 
 struct PlanArgs {
@@ -307,6 +320,11 @@ struct AttnArgs {
     int32_t* queues;     // resident launch: [kQueues] ticket counters, then the exit counter
     float scale_log2;    // softmax scale * log2(e) (times the key scale for 8-bit pools)
     float v_scale;       // value scale of 8-bit pools, 1 for bf16 pools
+};
+
+// Attention over 4-bit pools.
+struct Fp4AttnArgs : AttnArgs {
+    const uint8_t* scales;  // [blocks][Hkv][16][D / 32][key, value]
 };
 
 // One launch of both kinds of items: workgroups of 128-row items first (rounded up to whole rounds of
@@ -370,7 +388,9 @@ struct CombineArgs {
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool fp8, hipStream_t s);
 hipError_t launch_plan(const PlanArgs& a, hipStream_t s);
-hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, bool fp8, hipStream_t s);
+hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, Pool kind, hipStream_t s);
+hipError_t launch_read(const ReadArgs& ra, int head_dim, Pool kind, hipStream_t s);
+int64_t read_workgroups(int64_t pages, int num_kv_heads, int head_dim);  // of that launch
 // workgroups of that launch
 int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int head_dim, bool with_q);
 // append (AppendArgs) and plan (PlanArgs) in one launch
@@ -385,6 +405,9 @@ hipError_t launch_attention_fp8(const AttnArgs& a, int head_dim, int64_t num_ite
                                 int resident, hipStream_t s);
 hipError_t launch_attention_small(const AttnArgs& a, int head_dim, int64_t num_items, bool fp8,
                                   hipStream_t s);
+// the same over 4-bit pools: small, 128-row or wide tiles
+hipError_t launch_attention_fp4(const Fp4AttnArgs& a, int head_dim, int64_t num_items, bool small, bool wide,
+                                int resident, hipStream_t s);
 hipError_t launch_read_probe(const void* buf, size_t bytes, uint32_t* sink, hipStream_t s);
 hipError_t launch_mfma_probe(int iterations, float* sink, hipStream_t s);
 hipError_t launch_shared_plan(const SharedPlanArgs& a, hipStream_t s);
