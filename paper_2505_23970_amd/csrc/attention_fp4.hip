@@ -5,10 +5,10 @@ namespace gc {
 namespace {
 
 template <int D>
-__global__ __launch_bounds__(64, 1) void attention_fp4_small_kernel(const Fp4AttnArgs a) {
-    __shared__ __align__(16) unsigned char values[kFp4SmallLds<D>];
+__global__ __launch_bounds__(kFp4SmallWaves * 64, 4) void attention_fp4_small_kernel(const Fp4AttnArgs a) {
+    __shared__ Fp4SmallLds<D> lds;
     const int kvh = (int)(blockIdx.x % (unsigned)a.num_kv_heads);
-    fp4_small_body<D>(a, a.items[blockIdx.x / (unsigned)a.num_kv_heads], kvh, values);
+    fp4_small_body<D>(a, a.items[blockIdx.x / (unsigned)a.num_kv_heads], kvh, lds);
 }
 
 template <int D, int WAVES>
@@ -57,7 +57,7 @@ void launch_fp4(const Fp4AttnArgs& a, int64_t num_items, bool small, bool wide, 
     const int64_t total = num_items * a.num_kv_heads;
     const dim3 grid((unsigned)total);
     if (small)
-        attention_fp4_small_kernel<D><<<grid, 64, 0, s>>>(a);
+        attention_fp4_small_kernel<D><<<grid, kFp4SmallWaves * 64, 0, s>>>(a);
     else if (wide && resident > 0)
         attention_fp4_resident_kernel<D><<<dim3((unsigned)resident), kWideWaves * 64, 0, s>>>(a, (int)total);
     else if (wide)

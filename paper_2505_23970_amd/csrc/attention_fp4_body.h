@@ -99,12 +99,18 @@ struct QueryRow {
     }
 };
 
-// Value rows of a tile in LDS: row `key`, D bf16 values; its 32-byte pieces (16 values) are swizzled by the row so that
-// the four rows of a transposed read, and eight rows of two of them, lie in different banks.
+// Value rows of a tile in LDS: row `key`, D bf16 values, whose 16-byte chunk `chunk` lies at this offset. Pieces of 32 bytes
+// are swizzled by the row, so that the eight rows that 32 lanes read transposed lie in different banks, and their halves,
+// so that eight lanes that write a chunk of eight rows (at D = 64: all even, or odd, ones of two) fall on different parts of
+// 128 bytes (else a write takes twice as long).
 template <int D>
-__device__ __forceinline__ uint32_t value_at(int key, int piece) {
-    const int sw = D == 128 ? key & 7 : (key >> 1) & 3;
-    return (uint32_t)(key * 2 * D + (piece ^ sw) * 32);
+__device__ __forceinline__ uint32_t value_at(int key, int chunk) {
+    return (uint32_t)(key * 2 * D + (chunk ^ (D == 128 ? 2 * (key & 7) + (key >> 2 & 1) : key & 7)) * 16);
+}
+// Where a lane reads four elements of element block db (transposed, see below) of rows 4 (lane / 16) .. + 3.
+template <int D>
+__device__ __forceinline__ uint32_t value_from(int lane, int db) {
+    return value_at<D>(4 * (lane >> 4) + ((lane & 15) >> 2), 2 * db + ((lane & 3) >> 1)) + 8 * (lane & 1);
 }
 
 // Four elements (keys) of one value column: lane i of 16 gives the address of elements 4 (i % 4) .. + 3 of row i / 4
@@ -114,22 +120,56 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* at) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(lds_byte*)at));
 }
 
-// ---------------------------------------------------------------- small tiles
-// Query tiles of 16 rows, key tiles of 32 (two pages), one wavefront a work item, as over the other pools. What
-// bounds it: HBM. A page of codes is 1 KiB (D = 128) that 64 lanes load as they are multiplied: lane (row j, group G) takes
-// block G of key j, 16 bytes, straight into the operand's registers, with its two scales (key, value) beside; kRing
-// tiles are in flight in registers. Values go through 8 KiB of LDS of the wavefront's own for their transposition.
+// Direct global->LDS copies with an address of their own per lane: lane i's 16 (4) bytes land at lds + 16 i (4 i).
+// As dma16 (attention_kernels.h): the compiler does not track them, every wait is explicit.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const unsigned char* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const unsigned char* from, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Codes of a page in LDS (D = 128): 16-byte block `block` of row `row` lies at block ^ code_swizzle(row) of it, so that
+// the sixteen lanes of a 16-byte read (see value_at) lie in different banks, and the 32 of an 8-byte one (at D = 64
+// they do without): 0, 2, 3, 1 for the rows 4 i .. 4 i + 3.
 template <int D>
-constexpr int kFp4SmallLds = kDecN * D * 2;
+__device__ __forceinline__ int code_swizzle(int row) {
+    const int q = row >> 2 & 3;
+    return D == 128 ? q >> 1 | ((q ^ q >> 1) & 1) << 1 : 0;
+}
+
+// ---------------------------------------------------------------- small tiles
+// Query tiles of 16 rows, key tiles of 32 (two pages), as over the other pools, but kFp4SmallWaves wavefronts a work item,
+// which take its key tiles in turn and join their rows in LDS at the end: a tile is a chain of some thousand
+// cycles (copies, widening, products, weights, transposition, products) for 4.3 KB, and one wavefront a SIMD waits through it.
+// What bounds it: HBM. A wavefront's next tile (pages of codes, 1 KiB at D = 128, and their scales) is copied into LDS
+// while it works on the present one in registers: of the keys lane (row j, group G) holds block G of key j, 16 bytes and
+// their scale, as the products take them; of the values 16 elements of key j for every 64 elements of a row, which
+// go through 4 KiB of LDS for their transposition, 64 elements of the rows at a time.
+constexpr int kFp4SmallWaves = 4;
+template <int D>
+struct Fp4SmallLds {
+    static constexpr int kCodeBytes = kDecN * D / 2;  // of a tile's keys, or values
+    static constexpr int kScaleBytes = 256;
+    static constexpr int kTileBytes = 2 * kCodeBytes + kScaleBytes;
+    static constexpr int kValueBytes = kDecN * 64 * 2;
+    static_assert(kTileBytes + kValueBytes >= kDecM * D * 4, "the sums of 16 rows, at the end");
+    __align__(16) unsigned char wave[kFp4SmallWaves][kTileBytes + kValueBytes];
+    float m[kFp4SmallWaves][kDecM], l[kFp4SmallWaves][kDecM];
+};
 
 template <int D>
-__device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkItem it, const int kvh, unsigned char* vbuf) {
+__device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkItem it, const int kvh, Fp4SmallLds<D>& lds) {
     constexpr int DB = D / 16;
     constexpr int NB = D / kFp4Block;
     constexpr int kPageCodes = kPage * D / 2;
     constexpr int kPageScales = kPage * NB * 2;
-    constexpr int NV = D / 64;  // value loads of a tile: a page each, or half a page of each in one
-    constexpr int kRing = 4;
+    constexpr int kCodeBytes = Fp4SmallLds<D>::kCodeBytes;
+    constexpr int W = kFp4SmallWaves;
+    constexpr int NH = D / 64;  // halves of a row, 64 elements each
     const int lane = threadIdx.x & 63;
     if (it.r < 0 || it.kt_begin >= it.kt_end) return;
     const int P = it.P, cu = it.cu, n = it.n;
@@ -141,51 +181,72 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
     const bool row_ok = t < ntok;
     const int lim = P + it.q0 + (row_ok ? t : 0);
     const int64_t qrow = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + hl;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    unsigned char* const tile = lds.wave[wave];
+    unsigned char* const vbuf = tile + Fp4SmallLds<D>::kTileBytes;
+    const int kt_begin = it.kt_begin + wave, kt_end = it.kt_end;  // this wavefront's tiles: kt_begin, + W, ..
 
     const scalar_i32p table = (scalar_i32p)(a.block_tables + (int64_t)it.r * a.max_blocks);
-    const int blk = g4 % NB;  // block of the row that this lane holds (keys; values of vpage)
-    const uint32_t code_off = (uint32_t)(j * (D / 2) + blk * 16);
-    const uint32_t scale_off = (uint32_t)((j * NB + blk) * 2);
-    const int vpage = D == 128 ? 0 : g4 >> 1;  // D = 64: the page of this lane's values
+    const uint32_t code_at = (uint32_t)(j * (D / 2) + ((g4 % NB) ^ code_swizzle<D>(j)) * 16);
+    const uint32_t scale_at = (uint32_t)((j * NB + g4 % NB) * 2);
+    uint32_t vcode_at[NH];  // elements 64 h + 16 g4 .. + 15
+#pragma unroll
+    for (int h = 0; h < NH; ++h) vcode_at[h] = (uint32_t)(j * (D / 2) + ((2 * h + (g4 >> 1)) ^ code_swizzle<D>(j)) * 16 + 8 * (g4 & 1));
+    const uint32_t vscale_at = (uint32_t)((j * NB + (g4 >> 1)) * 2 + 1);  // + 4 h
     const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
+    // where each lane of a copy reads
+    const int copy_row = lane / NB % kPage;
+    const uint32_t code_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ code_swizzle<D>(copy_row)) * 16);
+    const uint32_t scale_from = (uint32_t)(lane % (kPageScales / 4) * 4);
+    const uint32_t tile_at = __builtin_amdgcn_readfirstlane(lds_address(tile));
 
-    struct Tile {
-        u32x4 k[2], v[NV];
-        uint32_t s[2];
+    // Block ids of a tile's two pages (scalar loads, fetched a tile ahead of their use). A page behind the last one (which
+    // the table row holds: the plan has seen to that) stands for it, one with an id outside the pool is copied from
+    // block 0: the keys behind the end are masked, their values zeroed.
+    struct Ids {
+        int b0, b1;
     };
-    // (pages past the table row or the sequence, or with an id outside the pool, are read from block 0: their
-    // keys are masked, their values zeroed)
-    auto load = [&](int kt, Tile& x) {
-        int64_t b[2];
+    const int last_page = min((L - 1) / kPage, a.max_blocks - 1);
+    auto fetch_ids = [&](int kt) -> Ids { return Ids{table[min(kt * 2, last_page)], table[min(kt * 2 + 1, last_page)]}; };
+    const int64_t block_codes = (int64_t)a.num_kv_heads * kPageCodes;
+    auto copy_tile = [&](const Ids& ids) {
+        int64_t b[2];  // byte offsets of the pages' codes; of their scales an eighth
+        static_assert(kPageScales * 8 == kPageCodes, "scales");
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            const int lp = kt * 2 + p;
-            const int id = table[min(lp, a.max_blocks - 1)];
-            const bool ok = (lp < a.max_blocks) & (lp * kPage < L) & (id >= 0) & (id < a.num_blocks);
-            b[p] = (int64_t)(ok ? id : 0) * a.num_kv_heads;
-            x.k[p] = *reinterpret_cast<const u32x4*>(kbase + b[p] * kPageCodes + code_off);
-            x.s[p] = *reinterpret_cast<const uint16_t*>(sbase + b[p] * kPageScales + scale_off);
-            if constexpr (D == 128) x.v[p] = *reinterpret_cast<const u32x4*>(vbase + b[p] * kPageCodes + code_off);
+            const uint32_t id = (uint32_t)(p ? ids.b1 : ids.b0);
+            b[p] = (int64_t)(id < (uint32_t)a.num_blocks ? id : 0u) * block_codes;
         }
-        if constexpr (D == 64) x.v[0] = *reinterpret_cast<const u32x4*>(vbase + (vpage ? b[1] : b[0]) * kPageCodes + code_off);
+        const uint32_t at = tile_at;
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                dma16(kbase + b[p], code_from, at + p * kPageCodes);
+                dma16(vbase + b[p], code_from, at + kCodeBytes + p * kPageCodes);
+            }
+            copy4(sbase + (lane < 32 ? b[0] / 8 : b[1] / 8) + scale_from, at + 2 * kCodeBytes);
+        } else {
+            const int64_t mine = lane < 32 ? b[0] : b[1];
+            copy16(kbase + mine + code_from, at);
+            copy16(vbase + mine + code_from, at + kCodeBytes);
+            copy4(sbase + (lane & 16 ? b[1] / 8 : b[0] / 8) + scale_from, at + 2 * kCodeBytes);  // (twice over)
+        }
     };
 
-    Tile ring[kRing];
-#pragma unroll
-    for (int i = 0; i < kRing; ++i)
-        if (it.kt_begin + i < it.kt_end) load(it.kt_begin + i, ring[i]);
+    Ids next = fetch_ids(kt_begin);
+    if (kt_begin < kt_end) copy_tile(next);
+    next = fetch_ids(kt_begin + W);
     QueryRow<D> q;
     q.load(a.q + qrow * D, row_ok, g4);
 
-    // where this lane's values go (row: its key of the tile) and where it reads transposed ones
-    uint32_t v_from[DB];
-    {
-        const int r = 4 * g4 + (j >> 2);
+    // where this lane puts 8 elements and reads transposed ones, of 64
+    uint32_t v_to[2], v_from[4];
 #pragma unroll
-        for (int db = 0; db < DB; ++db) v_from[db] = value_at<D>(r, db) + 8 * (j & 3);
-    }
+    for (int w = 0; w < 2; ++w) v_to[w] = value_at<64>(j, 2 * g4 + w);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) v_from[db] = value_from<64>(lane, db);
 
     f32x4 o[DB];
 #pragma unroll
@@ -194,34 +255,60 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
     const float c = a.scale_log2;
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
-    auto tile = [&](int kt, Tile& x) {
+    for (int kt = kt_begin; kt < kt_end; kt += W) {
+        wait_copies<0>();
+        u32x4 xk[2];
+        u32x2 xv[NH][2];
+        uint32_t xs[2], vs[NH][2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            xk[p] = *reinterpret_cast<const u32x4*>(tile + p * kPageCodes + code_at);
+            xs[p] = *reinterpret_cast<const uint16_t*>(tile + 2 * kCodeBytes + p * kPageScales + scale_at);
+        }
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                xv[h][p] = *reinterpret_cast<const u32x2*>(tile + kCodeBytes + p * kPageCodes + vcode_at[h]);
+                vs[h][p] = (tile + 2 * kCodeBytes + p * kPageScales)[vscale_at + 4 * h];
+            }
+        wait_lds_reads();
+        if (kt + W < kt_end) {
+            copy_tile(next);
+            next = fetch_ids(kt + 2 * W);
+        }
+
         const int key0 = kt * kDecN;
         const bool masked = key0 + kDecN - 1 > P + it.q0;  // some row does not see some key
-        // values: widened, into LDS
-        uint64_t nan[NV] = {};  // lanes whose block is NaN and within the sequence
+        uint64_t nan[NH][2] = {};                          // lanes whose value block is NaN and within the sequence
+        if (masked) {                                      // (values behind the end, and NaN, as zeros)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int key = (D == 128 ? kPage * i : kPage * vpage) + j;
-            const uint32_t vs = (D == 128 ? x.s[i] : vpage ? x.s[1] : x.s[0]) >> 8;
-            uint32_t keep = 0xFFFFFFFFu;
-            if (masked) {
-                const bool in = key0 + key < L;
-                nan[i] = __ballot(in && vs == kFp4Nan);
-                keep = in && vs != kFp4Nan ? keep : 0u;
-            }
+            for (int h = 0; h < NH; ++h)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t b[4];
-                fp4_widen8(x.v[i][w], fp4_scale(vs), b);
-                *reinterpret_cast<u32x4*>(vbuf + value_at<D>(key, 2 * blk + (w >> 1)) + 16 * (w & 1)) =
-                    u32x4{b[0] & keep, b[1] & keep, b[2] & keep, b[3] & keep};
-            }
+                for (int p = 0; p < 2; ++p) {
+                    const bool in = key0 + kPage * p + j < L;
+                    nan[h][p] = __ballot(in && vs[h][p] == kFp4Nan);
+                    if (!in || vs[h][p] == kFp4Nan) {
+                        xv[h][p] = u32x2{0u, 0u};
+                        vs[h][p] = 127;
+                    }
+                }
         }
         // s[p][v] is the score of tile key 16 p + 4 g4 + v
         f32x4 s[2];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) s[p] = q.scores(x.k[p], x.s[p]);
-        if (kt + kRing < it.kt_end) load(kt + kRing, x);
+        for (int p = 0; p < 2; ++p) s[p] = q.scores(xk[p], xs[p]);
+        auto put_values = [&](int h) {  // widened, into LDS
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    uint32_t b[4];
+                    fp4_widen8(xv[h][p][w], fp4_scale(vs[h][p]), b);
+                    *reinterpret_cast<u32x4*>(vbuf + v_to[w] + p * kPage * 128) = u32x4{b[0], b[1], b[2], b[3]};
+                }
+        };
+        put_values(0);
         const int rel = lim - key0;
         if (masked) {
 #pragma unroll
@@ -229,9 +316,17 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 #pragma unroll
                 for (int v = 0; v < 4; ++v) s[p][v] = (16 * p + 4 * g4 + v > rel) ? -INFINITY : s[p][v];
         }
-        const float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                               fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        const float m_new = fmaxf(m_run, row_max4(mx) * c);
+        // (maxima that pass a NaN on, as it is the row's anyway, take three operands an instruction)
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) mx = __builtin_elementwise_maximum(mx, s[e >> 2][e & 3]);
+        {
+            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = __builtin_elementwise_maximum(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = __builtin_elementwise_maximum(__uint_as_float(y[0]), __uint_as_float(y[1]));
+        }
+        const float m_new = __builtin_elementwise_maximum(m_run, mx * c);
         if (__any(m_new > m_run)) {
             const float alpha = m_new == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
@@ -250,66 +345,96 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
             pw[i] = __builtin_bit_cast(uint32_t, pair);
         }
         const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
-        wave_lds_sync();
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const u32x2 lo = read_transposed(vbuf + v_from[db]);
-            const u32x2 hi = read_transposed(vbuf + v_from[db] + kPage * 2 * D);
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[db], 0, 0, 0);
+        for (int h = 0; h < NH; ++h) {
+            if (h > 0) put_values(h);
+            wave_lds_sync();
+#pragma unroll
+            for (int db = 0; db < 4; ++db) {
+                const u32x2 lo = read_transposed(vbuf + v_from[db]);
+                const u32x2 hi = read_transposed(vbuf + v_from[db] + kPage * 128);
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+                o[4 * h + db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[4 * h + db], 0, 0, 0);
+            }
+            wave_lds_sync();
         }
-        wave_lds_sync();
         if (masked) {
-            // value blocks that held a NaN: bit 16 g + j of `nan` is (key j of page i, block g), or for D = 64
-            // (key j of page g / 2, block g % 2)
+            // value blocks that held a NaN: bit 16 g + j of nan[h][p] is key 16 p + j, block 2 h + g / 2
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (nan[i] == 0) continue;
+            for (int h = 0; h < NH; ++h)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const uint32_t keys = (uint32_t)(nan[i] >> (16 * g)) & 0xFFFFu;
-                    const int seen = rel - kPage * (D == 128 ? i : g >> 1);  // keys 0 .. seen of the page
+                for (int p = 0; p < 2; ++p) {
+                    if (nan[h][p] == 0) continue;
+                    const int seen = rel - kPage * p;  // keys 0 .. seen of the page
                     const uint32_t sees = seen < 0 ? 0u : 0xFFFFu >> (15 - min(seen, 15));
-                    const float add = (keys & sees) != 0 ? __builtin_nanf("") : 0.f;
-                    const int b = D == 128 ? g : g & 1;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        o[2 * b][v] += add;
-                        o[2 * b + 1][v] += add;
+                    for (int b = 0; b < 2; ++b) {
+                        const float add = ((uint32_t)(nan[h][p] >> (32 * b)) & sees) != 0 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            o[4 * h + 2 * b][v] += add;
+                            o[4 * h + 2 * b + 1][v] += add;
+                        }
                     }
                 }
-            }
         }
-    };
-
-    for (int kt = it.kt_begin; kt < it.kt_end; kt += kRing) {
-#pragma unroll
-        for (int i = 0; i < kRing; ++i)
-            if (kt + i < it.kt_end) tile(kt + i, ring[i]);
     }
 
-    const float l_tot = row_sum4(l_run);
+    float l_tot = row_sum4(l_run);
+    constexpr int kOwn = DB / W;  // element blocks whose sums this wavefront joins and writes: from kOwn wave on
+    f32x4 mine[kOwn];
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) mine[db] = o[db];
+    } else {
+        // rows in units of 2^m of their own: joined in wavefront order
+        f32x4* const at = reinterpret_cast<f32x4*>(tile);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) at[db * 64 + lane] = o[db];
+        if (g4 == 0) {
+            lds.m[wave][j] = m_run;
+            lds.l[wave][j] = l_tot;
+        }
+        __syncthreads();
+        float m = lds.m[0][j];
+#pragma unroll
+        for (int w = 1; w < W; ++w) m = fmaxf(m, lds.m[w][j]);
+        m_run = m;
+        l_tot = 0.f;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) mine[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(lds.m[w][j] - m);
+            l_tot = fmaf(lds.l[w][j], alpha, l_tot);
+            const f32x4* const from = reinterpret_cast<const f32x4*>(lds.wave[w]) + kOwn * wave * 64 + lane;
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) mine[i] += from[i * 64] * alpha;
+        }
+    }
     const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
     // (a split item passes a NaN sum on to the merge)
     const float lse_v = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : (it.part >= 0 && l_tot != l_tot ? l_tot : -INFINITY);
-    // o[db][v] is element d = 16 db + 4 g4 + v of row j
+    // mine[i][v] is element d = 16 (kOwn wave + i) + 4 g4 + v of row j
     if (!row_ok) return;
+    const int d0 = 16 * kOwn * wave + 4 * g4;
+    const bool first = wave == 0 && g4 == 0;
     if (it.part < 0) {
-        uint16_t* op = a.out + qrow * D + 4 * g4;
+        uint16_t* op = a.out + qrow * D + d0;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
+        for (int i = 0; i < kOwn; ++i) {
             u32x2 w;
-            w[0] = pack_pair(o[db][0] * inv, o[db][1] * inv);
-            w[1] = pack_pair(o[db][2] * inv, o[db][3] * inv);
-            *reinterpret_cast<u32x2*>(op + 16 * db) = w;
+            w[0] = pack_pair(mine[i][0] * inv, mine[i][1] * inv);
+            w[1] = pack_pair(mine[i][2] * inv, mine[i][3] * inv);
+            *reinterpret_cast<u32x2*>(op + 16 * i) = w;
         }
-        if (a.lse != nullptr && g4 == 0) a.lse[qrow] = lse_v;
+        if (a.lse != nullptr && first) a.lse[qrow] = lse_v;
     } else {
         const int64_t prow = ((int64_t)it.part * a.num_kv_heads + kvh) * kDecM + j;
-        float* po = a.part_o + prow * D + 4 * g4;
+        float* po = a.part_o + prow * D + d0;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(po + 16 * db) = o[db] * inv;
-        if (g4 == 0) a.part_lse[prow] = lse_v;
+        for (int i = 0; i < kOwn; ++i) *reinterpret_cast<f32x4*>(po + 16 * i) = mine[i] * inv;
+        if (first) a.part_lse[prow] = lse_v;
     }
 }
 
@@ -328,18 +453,6 @@ struct Fp4Lds {
     __align__(16) unsigned char s[2][kScaleBytes];
 };
 
-// Direct global->LDS copies with an address of their own per lane: lane i's 16 (4) bytes land at lds + 16 i (4 i).
-// As dma16 (attention_kernels.h): the compiler does not track them, every wait is explicit.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy16(const unsigned char* from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
-}
-__device__ __forceinline__ void copy4(const unsigned char* from, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 template <int D, int WAVES>
 __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const unsigned bid, Fp4Lds<D, WAVES>& lds) {
     constexpr int ROWS = kRowsPerWave;
@@ -350,12 +463,15 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     constexpr int kPageCodes = kPage * D / 2;
     constexpr int kPageScales = kPage * NB * 2;
     constexpr int kTileLog2Thresh = 8;
+    constexpr int kAhead = 4;  // value fragments read ahead of their products
 
     int tid_opaque = (int)threadIdx.x;  // (lane constants per work item, not held across a resident launch's items)
     asm volatile("" : "+v"(tid_opaque));
     const int tid = tid_opaque, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, j16 = lane & 15;
+    // (one of a SIMD's two wavefronts is preferred: attention_kernels.h)
+    if (WAVES == kWideWaves ? wave < WAVES / 2 : D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd) __builtin_amdgcn_s_setprio(2);
     const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
     const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
     asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P), "s"(it.cu), "s"(it.n));
@@ -391,16 +507,15 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     for (int rb = 0; rb < RB; ++rb) q[rb].load(a.q + qrow[rb] * D, row_ok[rb], g4);
 
     // Key codes: 1 KiB copies, a page (D = 128) or two (D = 64) each, by the first wavefronts. Lane i brings 16-byte
-    // block i % NB (swizzled at D = 128, so that the reads of eight neighbouring rows lie in different banks) of row i / NB.
+    // block i % NB (swizzled) of row i / NB.
     constexpr int kKeyCopies = KB * kPageCodes / 1024;
     constexpr int kPagesPerCopy = KB / kKeyCopies;
     const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
     const uint32_t k_lds = lds_address(lds.k[0]), s_lds = lds_address(lds.s[0]);
-    auto key_swizzle = [](int row) { return D == 128 ? (row >> 2) & 3 : 0; };
     const int copy_row = lane / NB % kPage;
-    const uint32_t key_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ key_swizzle(copy_row)) * 16);
+    const uint32_t key_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ code_swizzle<D>(copy_row)) * 16);
     // Scales: 256-byte copies of two (four) pages
     constexpr int kScaleCopies = KB * kPageScales / 256;
     constexpr int kScalePages = KB / kScaleCopies;
@@ -419,10 +534,12 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
                   s_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kScaleBytes) + (uint32_t)w * 256u);
         }
     };
-    // Values: thread t takes elements kPer t .. of the tile's [64][D], which lie in one row and one block.
+    // Values: a thread takes kPer elements of one row and block; at D = 128 neighbouring lanes take neighbouring rows (value_at).
     constexpr int kPer = kBlockN * D / (WAVES * 64);  // 32, 16 or 8
     constexpr int kWords = kPer / 8;
-    const int v_key = tid * kPer / D, v_el = tid * kPer % D;
+    constexpr int kRowsOfWave = 64 * kPer / D;
+    const int v_key = D == 128 ? wave * kRowsOfWave + lane % kRowsOfWave : tid * kPer / D;
+    const int v_el = D == 128 ? lane / kRowsOfWave * kPer : tid * kPer % D;
     const int v_page = wave * 64 * kPer / (kPage * D);
     uint32_t vc[kWords], vs = 0;
     auto load_values = [&](int okids) {
@@ -443,15 +560,16 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     };
     const int first_masked = P + it.q0;  // tiles that reach past this key hide some key from some row
     auto store_values = [&](int buf, int kt) {
-        uint32_t keep = 0xFFFFFFFFu;
-        if (kt * kBlockN + kBlockN - 1 > first_masked) keep = kt * kBlockN + v_key < L && vs != kFp4Nan ? keep : 0u;
+        if (kt * kBlockN + kBlockN - 1 > first_masked && (kt * kBlockN + v_key >= L || vs == kFp4Nan)) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) vc[w] = 0;  // (values behind the end, and NaN, as zeros)
+            vs = 127;
+        }
 #pragma unroll
         for (int w = 0; w < kWords; ++w) {
             uint32_t b[4];
             fp4_widen8(vc[w], fp4_scale(vs), b);
-            const int e = v_el / 8 + w;  // 16 bytes of the row
-            *reinterpret_cast<u32x4*>(lds.v[buf] + value_at<D>(v_key, e >> 1) + 16 * (e & 1)) =
-                u32x4{b[0] & keep, b[1] & keep, b[2] & keep, b[3] & keep};
+            *reinterpret_cast<u32x4*>(lds.v[buf] + value_at<D>(v_key, v_el / 8 + w)) = u32x4{b[0], b[1], b[2], b[3]};
         }
     };
 
@@ -461,11 +579,11 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     const float c = a.scale_log2;
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
-    const uint32_t k_at = (uint32_t)(j16 * (D / 2) + ((g4 % NB) ^ key_swizzle(j16)) * 16);
+    const uint32_t k_at = (uint32_t)(j16 * (D / 2) + ((g4 % NB) ^ code_swizzle<D>(j16)) * 16);
     const uint32_t s_at = (uint32_t)((j16 * NB + g4 % NB) * 2);
     uint32_t v_from[DB];
 #pragma unroll
-    for (int db = 0; db < DB; ++db) v_from[db] = value_at<D>(4 * g4 + (j16 >> 2), db) + 8 * (j16 & 3);
+    for (int db = 0; db < DB; ++db) v_from[db] = value_from<D>(lane, db);
 
     auto compute_tile = [&](int buf, int kt) {
         const unsigned char* const kb = lds.k[buf];
@@ -478,12 +596,31 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
             kf[b] = *reinterpret_cast<const u32x4*>(kb + b * kPageCodes + k_at);
             ks[b] = *reinterpret_cast<const uint16_t*>(sb + b * kPageScales + s_at);
         }
+        bf16x8 vf[2 * DB];  // value fragment i: keys 32 (i / DB) .. + 31, elements 16 (i % DB) .. + 15
+        auto vread = [&](int i) {
+            const unsigned char* const at = vb + v_from[i % DB] + (i / DB) * 2 * kPage * 2 * D;
+            const u32x2 lo = read_transposed(at), hi = read_transposed(at + kPage * 2 * D);
+            vf[i] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+        };
+        __builtin_amdgcn_sched_barrier(0);
         // s[rb][b][v] is the score of row 16 rb + j16 and tile key 16 b + 4 g4 + v
         f32x4 s[RB][KB];
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int part = 0; part < QueryRow<D>::kParts; ++part) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) s[rb][b] = q[rb].scores(kf[b], ks[b]);
+            for (int b = 0; b < KB; ++b) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    s[rb][b] = mfma_fp4_fp8(kf[b], q[rb].w[part], part == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][b], ks[b], q[rb].scale[part]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // the first value fragments go out before the last products; they land during those and the softmax
+            if (part == 0) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) vread(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
 
         const int key0 = kt * kBlockN;
         const bool masked = key0 + kBlockN - 1 > first_masked;
@@ -523,31 +660,41 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
                 neg_off[rb] = m_run[rb] == -INFINITY ? 0.f : -m_run[rb];
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 pf[RB][2];
+        // pair x of a half's eight weights of a row, as bf16, and its part of the row sum
+        auto w_pair = [&](int rb, int hb, int x) {
+            const f32x4 y = s[rb][2 * hb + (x >> 1)];
+            const bf16x2 pq = {(__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1)], c, neg_off[rb])),
+                               (__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1) + 1], c, neg_off[rb]))};
+            pf[rb][hb][2 * x] = pq[0];
+            pf[rb][hb][2 * x + 1] = pq[1];
+            l_run[rb] = __builtin_amdgcn_fdot2_f32_bf16(pq, ones, l_run[rb], false);
+            asm volatile("" : "+v"(l_run[rb]));
+        };
+        // (weights in blocks: attention_kernels.h)
+        constexpr bool kAllFirst = WAVES == kWideWaves;
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int hb = 0; hb < (kAllFirst ? 2 : 1); ++hb)
 #pragma unroll
-            for (int qq = 0; qq < 4; ++qq)
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const f32x4 x = s[rb][2 * hb + (qq >> 1)];
-                    const bf16x2 pq = {(__bf16)__builtin_amdgcn_exp2f(fmaf(x[2 * (qq & 1)], c, neg_off[rb])),
-                                       (__bf16)__builtin_amdgcn_exp2f(fmaf(x[2 * (qq & 1) + 1], c, neg_off[rb]))};
-                    pf[rb][hb][2 * qq] = pq[0];
-                    pf[rb][hb][2 * qq + 1] = pq[1];
-                    l_run[rb] = __builtin_amdgcn_fdot2_f32_bf16(pq, ones, l_run[rb], false);
-                }
+                for (int rb = 0; rb < RB; ++rb) w_pair(rb, hb, x);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb)
+        for (int i = 0; i < 2 * DB; ++i) {
+            const int hb = i / DB, db = i % DB;
+            if (i + kAhead < 2 * DB) vread(i + kAhead);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const u32x2 lo = read_transposed(vb + v_from[db] + (2 * hb) * kPage * 2 * D);
-                const u32x2 hi = read_transposed(vb + v_from[db] + (2 * hb + 1) * kPage * 2 * D);
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+            for (int rb = 0; rb < RB; ++rb)
+                o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[rb][hb], o[rb][db], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (!kAllFirst && hb == 0 && db % (DB / 4) == DB / 4 - 1) {
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb][hb], o[rb][db], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) w_pair(rb, 1, db / (DB / 4));
+                __builtin_amdgcn_sched_barrier(0);
             }
+        }
         if (masked) {
             // value blocks that held a NaN (lane = key of the tile)
             uint64_t nan[NB];
