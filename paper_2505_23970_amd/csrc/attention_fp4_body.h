@@ -127,6 +127,9 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* at) {
 __device__ __forceinline__ void copy16(const unsigned char* from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
 }
+__device__ __forceinline__ void dma4(const unsigned char* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
 __device__ __forceinline__ void copy4(const unsigned char* from, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(lds) : "memory", "m0");
 }
@@ -492,13 +495,17 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         qrow[rb] = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group);
     }
 
-    // Block ids of a tile's pages: entry p in lanes with lane % 4 == p (clamped into the row). A page past the table
-    // row or the sequence, or with an id outside the pool, is taken from block 0: its keys are masked, its values zeroed.
+    // Block ids of a tile's pages: entry p in lanes with lane % 4 == p. A page behind the last one (which the table row
+    // holds: the plan has seen to that) stands for it, one with an id outside the pool is taken from block 0: the keys
+    // behind the end are masked, their values zeroed.
     const int32_t* const table = a.block_tables + (int64_t)it.r * a.max_blocks;
-    auto fetch_ids = [&](int kt) -> int { return table[(uint32_t)min(kt * 4 + (lane & 3), a.max_blocks - 1)]; };
-    auto checked = [&](int kt, int ids) -> int {
-        const int lp = kt * 4 + (lane & 3);
-        return lp < a.max_blocks && lp * kPage < L && ids >= 0 && ids < a.num_blocks ? ids : 0;
+    const int last_page = min((L - 1) / kPage, a.max_blocks - 1);
+    auto fetch_ids = [&](int kt) -> int { return table[(uint32_t)min(kt * 4 + (lane & 3), last_page)]; };
+    const int64_t block_codes = (int64_t)a.num_kv_heads * kPageCodes;
+    auto page_at = [&](int ids, int p) -> int64_t {  // byte offset of page p's codes; of its scales an eighth
+        static_assert(kPageScales * 8 == kPageCodes, "scales");
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, p);
+        return (int64_t)(id < (uint32_t)a.num_blocks ? id : 0u) * block_codes;
     };
     int ids = fetch_ids(it.kt_begin);
 
@@ -506,33 +513,18 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) q[rb].load(a.q + qrow[rb] * D, row_ok[rb], g4);
 
-    // Key codes: 1 KiB copies, a page (D = 128) or two (D = 64) each, by the first wavefronts. Lane i brings 16-byte
-    // block i % NB (swizzled) of row i / NB.
-    constexpr int kKeyCopies = KB * kPageCodes / 1024;
-    constexpr int kPagesPerCopy = KB / kKeyCopies;
+    // Copies straight into LDS: wavefront w brings the key codes of page w % 4, its lane i the 16-byte block i % NB
+    // (swizzled) of row i / NB, and the page's scales; of 8 wavefronts the first four do the one, the others the other.
     const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
-    const uint32_t k_lds = lds_address(lds.k[0]), s_lds = lds_address(lds.s[0]);
+    const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.k[0]) + (wave & 3) * kPageCodes);
+    const uint32_t s_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.s[0]) + (wave & 3) * kPageScales);
     const int copy_row = lane / NB % kPage;
     const uint32_t key_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ code_swizzle<D>(copy_row)) * 16);
-    // Scales: 256-byte copies of two (four) pages
-    constexpr int kScaleCopies = KB * kPageScales / 256;
-    constexpr int kScalePages = KB / kScaleCopies;
-    static_assert(kKeyCopies <= WAVES && kScaleCopies <= WAVES, "copies");
-    constexpr int kScaleWave = WAVES >= kKeyCopies + kScaleCopies ? kKeyCopies : 0;
-    auto copy_tile = [&](int buf, int okids) {
-        if (wave < kKeyCopies) {
-            const int64_t b = __shfl(okids, wave * kPagesPerCopy + lane / (64 / kPagesPerCopy));
-            copy16(kbase + b * a.num_kv_heads * kPageCodes + key_from,
-                   k_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kCodeBytes) + (uint32_t)wave * 1024u);
-        }
-        if (wave >= kScaleWave && wave < kScaleWave + kScaleCopies) {
-            const int w = wave - kScaleWave;
-            const int64_t b = __shfl(okids, w * kScalePages + lane / (64 / kScalePages));
-            copy4(sbase + b * a.num_kv_heads * kPageScales + lane % (64 / kScalePages) * 4,
-                  s_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kScaleBytes) + (uint32_t)w * 256u);
-        }
+    auto copy_tile = [&](int buf, int64_t at) {  // at: page_at(ids, wave & 3)
+        if (wave < 4 && lane < kPageCodes / 16) dma16(kbase + at, key_from, k_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kCodeBytes));
+        if (wave >= WAVES - 4 && lane < kPageScales / 4) dma4(sbase + at / 8, 4u * lane, s_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kScaleBytes));
     };
     // Values: a thread takes kPer elements of one row and block; at D = 128 neighbouring lanes take neighbouring rows (value_at).
     constexpr int kPer = kBlockN * D / (WAVES * 64);  // 32, 16 or 8
@@ -541,10 +533,10 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     const int v_key = D == 128 ? wave * kRowsOfWave + lane % kRowsOfWave : tid * kPer / D;
     const int v_el = D == 128 ? lane / kRowsOfWave * kPer : tid * kPer % D;
     const int v_page = wave * 64 * kPer / (kPage * D);
+    const uint32_t v_at = (uint32_t)((v_key % kPage) * (D / 2) + v_el / 2), vs_at = (uint32_t)(((v_key % kPage) * NB + v_el / kFp4Block) * 2 + 1);
     uint32_t vc[kWords], vs = 0;
-    auto load_values = [&](int okids) {
-        const int64_t b = (int64_t)__builtin_amdgcn_readlane(okids, v_page) * a.num_kv_heads;
-        const unsigned char* const from = vbase + b * kPageCodes + (v_key % kPage) * (D / 2) + v_el / 2;
+    auto load_values = [&](int64_t at) {  // at: page_at(ids, v_page)
+        const unsigned char* const from = vbase + at + v_at;
         if constexpr (kWords == 4) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
@@ -556,7 +548,7 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         } else {
             vc[0] = *reinterpret_cast<const uint32_t*>(from);
         }
-        vs = (sbase + b * kPageScales)[((v_key % kPage) * NB + v_el / kFp4Block) * 2 + 1];
+        vs = (sbase + at / 8)[vs_at];
     };
     const int first_masked = P + it.q0;  // tiles that reach past this key hide some key from some row
     auto store_values = [&](int buf, int kt) {
@@ -724,9 +716,8 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     auto step = [&](const int cur) {
         const bool more = kt + 1 < it.kt_end;
         if (more) {
-            const int okids = checked(kt + 1, ids);
-            copy_tile(1 - cur, okids);
-            load_values(okids);
+            copy_tile(1 - cur, page_at(ids, wave & 3));
+            load_values(page_at(ids, v_page));
             if (kt + 2 < it.kt_end) ids = fetch_ids(kt + 2);
         }
         compute_tile(cur, kt);
@@ -747,9 +738,8 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         kt = it.kt_begin;
         if (exact) ids = fetch_ids(kt);
         {
-            const int okids = checked(kt, ids);
-            copy_tile(0, okids);
-            load_values(okids);
+            copy_tile(0, page_at(ids, wave & 3));
+            load_values(page_at(ids, v_page));
             if (kt + 1 < it.kt_end) ids = fetch_ids(kt + 1);
             store_values(0, kt);
         }
