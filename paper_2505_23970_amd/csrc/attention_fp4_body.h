@@ -442,18 +442,19 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 }
 
 // ---------------------------------------------------------------- 128-row and wide tiles
-// Query tiles of 32 rows a wavefront, key tiles of 64 (four pages), double buffered. Pages of key codes and of scales are
-// copied straight into LDS and multiplied as they are; the values' codes go through registers and are widened into LDS
-// after the tile's products. What bounds it: the matrix cores and the softmax's vector instructions, as over
-// the other pools; against 8-bit pools a tile has no keys to widen and half the value codes.
+// Query tiles of 32 rows a wavefront, key tiles of 64 (four pages). Pages of codes and of scales are copied straight into
+// LDS, two tiles ahead; keys are multiplied as they are, values are widened from there into rows of bf16, a tile ahead.
+// What bounds it: the matrix cores and, beside them, the softmax's vector instructions.
 template <int D, int WAVES>
 struct Fp4Lds {
+    static constexpr int kSlots = 4;  // tiles t to t + 2 are in use, and the scales of t - 1
+    static constexpr int kValueBuffers = WAVES == kWideWaves ? 3 : 2;
     static constexpr int kValueBytes = kBlockN * D * 2;
     static constexpr int kCodeBytes = kBlockN * D / 2;
     static constexpr int kScaleBytes = kBlockN * (D / kFp4Block) * 2;
-    __align__(16) unsigned char v[2][kValueBytes];
-    __align__(16) unsigned char k[2][kCodeBytes];
-    __align__(16) unsigned char s[2][kScaleBytes];
+    __align__(16) unsigned char v[kValueBuffers][kValueBytes];
+    __align__(16) unsigned char kc[kSlots][kCodeBytes], vc[kSlots][kCodeBytes];  // codes of keys and of values
+    __align__(16) unsigned char s[kSlots][kScaleBytes];
 };
 
 template <int D, int WAVES>
@@ -473,8 +474,8 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     const int tid = tid_opaque, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, j16 = lane & 15;
-    // (one of a SIMD's two wavefronts is preferred: attention_kernels.h)
-    if (WAVES == kWideWaves ? wave < WAVES / 2 : D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd) __builtin_amdgcn_s_setprio(2);
+    // (4 wavefronts: one of the two workgroups on a compute unit is preferred, attention_kernels.h)
+    if (WAVES != kWideWaves && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd) __builtin_amdgcn_s_setprio(2);
     const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
     const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
     asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P), "s"(it.cu), "s"(it.n));
@@ -495,48 +496,60 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         qrow[rb] = (int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group);
     }
 
-    // Block ids of a tile's pages: entry p in lanes with lane % 4 == p. A page behind the last one (which the table row
-    // holds: the plan has seen to that) stands for it, one with an id outside the pool is taken from block 0: the keys
-    // behind the end are masked, their values zeroed.
+    // Block ids: lane l of `ids` holds that of page 64 i + l of the item (from its first tile on), of `ids_next` the next 64.
+    // A page behind the last one (which the table row holds: the plan has seen to that) stands for it, one with an id
+    // outside the pool is taken from block 0: the keys behind the end are masked, their values zeroed.
     const int32_t* const table = a.block_tables + (int64_t)it.r * a.max_blocks;
     const int last_page = min((L - 1) / kPage, a.max_blocks - 1);
-    auto fetch_ids = [&](int kt) -> int { return table[(uint32_t)min(kt * 4 + (lane & 3), last_page)]; };
+    auto fetch_ids = [&](int i) -> int { return table[(uint32_t)min(it.kt_begin * 4 + 64 * i + lane, last_page)]; };
     const int64_t block_codes = (int64_t)a.num_kv_heads * kPageCodes;
-    auto page_at = [&](int ids, int p) -> int64_t {  // byte offset of page p's codes; of its scales an eighth
-        static_assert(kPageScales * 8 == kPageCodes, "scales");
-        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, p);
-        return (int64_t)(id < (uint32_t)a.num_blocks ? id : 0u) * block_codes;
-    };
-    int ids = fetch_ids(it.kt_begin);
+    int ids = fetch_ids(0), ids_next = ids;
 
     QueryRow<D> q[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) q[rb].load(a.q + qrow[rb] * D, row_ok[rb], g4);
 
-    // Copies straight into LDS: wavefront w brings the key codes of page w % 4, its lane i the 16-byte block i % NB
-    // (swizzled) of row i / NB, and the page's scales; of 8 wavefronts the first four do the one, the others the other.
+    // Copies of a tile (its number counts from the item's first): a wavefront brings parts of page w % 4: codes, lane i the
+    // 16-byte block i % NB (swizzled) of row i / NB, of its keys and of its values, and its scales. Of 8 wavefronts the first four,
+    // which are half a tile ahead (see turns), bring what is needed first, values and scales, the others the keys.
     const unsigned char* const kbase = reinterpret_cast<const unsigned char*>(a.k_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const vbase = reinterpret_cast<const unsigned char*>(a.v_pool) + (int64_t)kvh * kPageCodes;
     const unsigned char* const sbase = a.scales + (int64_t)kvh * kPageScales;
-    const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.k[0]) + (wave & 3) * kPageCodes);
+    using Lds = Fp4Lds<D, WAVES>;
+    const uint32_t kc_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.kc[0]) + (wave & 3) * kPageCodes);
+    const uint32_t vc_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.vc[0]) + (wave & 3) * kPageCodes);
     const uint32_t s_lds = __builtin_amdgcn_readfirstlane(lds_address(lds.s[0]) + (wave & 3) * kPageScales);
     const int copy_row = lane / NB % kPage;
-    const uint32_t key_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ code_swizzle<D>(copy_row)) * 16);
-    auto copy_tile = [&](int buf, int64_t at) {  // at: page_at(ids, wave & 3)
-        if (wave < 4 && lane < kPageCodes / 16) dma16(kbase + at, key_from, k_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kCodeBytes));
-        if (wave >= WAVES - 4 && lane < kPageScales / 4) dma4(sbase + at / 8, 4u * lane, s_lds + (uint32_t)(buf * Fp4Lds<D, WAVES>::kScaleBytes));
+    const uint32_t code_from = (uint32_t)(copy_row * (D / 2) + ((lane % NB) ^ code_swizzle<D>(copy_row)) * 16);
+    auto copy_tile = [&](int tile) {
+        const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(ids, tile * 4 % 64 + (wave & 3));
+        const int64_t at = (int64_t)(id < (uint32_t)a.num_blocks ? id : 0u) * block_codes;
+        const uint32_t to = (uint32_t)(tile % Lds::kSlots);
+        static_assert(kPageScales * 8 == kPageCodes, "offsets of scales");
+        if (lane < kPageCodes / 16) {
+            if (WAVES == 4 || wave < 4) dma16(vbase + at, code_from, vc_lds + to * Lds::kCodeBytes);
+            if (WAVES == 4 || wave >= 4) dma16(kbase + at, code_from, kc_lds + to * Lds::kCodeBytes);
+        }
+        if ((WAVES == 4 || wave < 4) && lane < kPageScales / 4) dma4(sbase + at / 8, 4u * lane, s_lds + to * Lds::kScaleBytes);
+        if (tile % 16 == 15) {
+            ids = ids_next;
+            ids_next = fetch_ids(tile / 16 + 2);
+        }
     };
-    // Values: a thread takes kPer elements of one row and block; at D = 128 neighbouring lanes take neighbouring rows (value_at).
+    // Values: a thread widens kPer elements of one row and block; at D = 128 neighbouring lanes take neighbouring rows (value_at).
     constexpr int kPer = kBlockN * D / (WAVES * 64);  // 32, 16 or 8
     constexpr int kWords = kPer / 8;
     constexpr int kRowsOfWave = 64 * kPer / D;
     const int v_key = D == 128 ? wave * kRowsOfWave + lane % kRowsOfWave : tid * kPer / D;
     const int v_el = D == 128 ? lane / kRowsOfWave * kPer : tid * kPer % D;
-    const int v_page = wave * 64 * kPer / (kPage * D);
-    const uint32_t v_at = (uint32_t)((v_key % kPage) * (D / 2) + v_el / 2), vs_at = (uint32_t)(((v_key % kPage) * NB + v_el / kFp4Block) * 2 + 1);
+    const uint32_t vc_at = (uint32_t)(v_key * (D / 2) + ((v_el / 32) ^ code_swizzle<D>(v_key)) * 16 + v_el % 32 / 2);
+    const uint32_t vs_at = (uint32_t)((v_key * NB + v_el / kFp4Block) * 2 + 1);
+    uint32_t v_to[kWords];
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) v_to[w] = value_at<D>(v_key, v_el / 8 + w);
     uint32_t vc[kWords], vs = 0;
-    auto load_values = [&](int64_t at) {  // at: page_at(ids, v_page)
-        const unsigned char* const from = vbase + at + v_at;
+    auto read_codes = [&](int tile) {
+        const unsigned char* const from = lds.vc[0] + tile % Lds::kSlots * Lds::kCodeBytes + vc_at;
         if constexpr (kWords == 4) {
             const u32x4 w = *reinterpret_cast<const u32x4*>(from);
 #pragma unroll
@@ -548,11 +561,12 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         } else {
             vc[0] = *reinterpret_cast<const uint32_t*>(from);
         }
-        vs = (sbase + at / 8)[vs_at];
+        vs = (lds.s[0] + tile % Lds::kSlots * Lds::kScaleBytes)[vs_at];
     };
     const int first_masked = P + it.q0;  // tiles that reach past this key hide some key from some row
-    auto store_values = [&](int buf, int kt) {
-        if (kt * kBlockN + kBlockN - 1 > first_masked && (kt * kBlockN + v_key >= L || vs == kFp4Nan)) {
+    auto put_values = [&](int buf, int tile) {
+        const int key0 = (it.kt_begin + tile) * kBlockN;
+        if (key0 + kBlockN - 1 > first_masked && (key0 + v_key >= L || vs == kFp4Nan)) {
 #pragma unroll
             for (int w = 0; w < kWords; ++w) vc[w] = 0;  // (values behind the end, and NaN, as zeros)
             vs = 127;
@@ -561,15 +575,18 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
         for (int w = 0; w < kWords; ++w) {
             uint32_t b[4];
             fp4_widen8(vc[w], fp4_scale(vs), b);
-            *reinterpret_cast<u32x4*>(lds.v[buf] + value_at<D>(v_key, v_el / 8 + w)) = u32x4{b[0], b[1], b[2], b[3]};
+            *reinterpret_cast<u32x4*>(lds.v[0] + buf * Lds::kValueBytes + v_to[w]) = u32x4{b[0], b[1], b[2], b[3]};
         }
     };
 
     f32x4 o[RB][DB];
-    float m_run[RB], neg_off[RB], l_run[RB];
+    float m_run[RB], neg_off[RB];
     bool need_max, exact = false;  // (the exponent offset, as in attention_kernels.h)
     const float c = a.scale_log2;
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    // Row sums of the (rounded) weights by products with ones: every element of l_run[rb] is its column's sum. Dot products
+    // of the vector unit share the matrix cores: one took 54 to 86 cycles beside another wavefront's products.
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+    f32x4 l_run[RB];
 
     const uint32_t k_at = (uint32_t)(j16 * (D / 2) + ((g4 % NB) ^ code_swizzle<D>(j16)) * 16);
     const uint32_t s_at = (uint32_t)((j16 * NB + g4 % NB) * 2);
@@ -577,28 +594,23 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
 #pragma unroll
     for (int db = 0; db < DB; ++db) v_from[db] = value_from<D>(lane, db);
 
-    auto compute_tile = [&](int buf, int kt) {
-        const unsigned char* const kb = lds.k[buf];
-        const unsigned char* const sb = lds.s[buf];
-        const unsigned char* const vb = lds.v[buf];
-        u32x4 kf[KB];
-        uint32_t ks[KB];
+    f32x4 s[RB][KB];     // s[rb][b][v] is the score of row 16 rb + j16 and tile key 16 b + 4 g4 + v
+    bf16x8 pf[RB][2];    // the weights, as operands of the products with the values
+    bf16x8 vf[2 * DB];   // value fragment i: keys 32 (i / DB) .. + 31, elements 16 (i % DB) .. + 15
+    u32x4 kf[KB];        // key fragments and their scales
+    uint32_t ks[KB];
+    auto kread = [&](int tile) {
+        const uint32_t in = (uint32_t)(tile % Lds::kSlots);
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
-            kf[b] = *reinterpret_cast<const u32x4*>(kb + b * kPageCodes + k_at);
-            ks[b] = *reinterpret_cast<const uint16_t*>(sb + b * kPageScales + s_at);
+            kf[b] = *reinterpret_cast<const u32x4*>(lds.kc[0] + in * Lds::kCodeBytes + b * kPageCodes + k_at);
+            ks[b] = *reinterpret_cast<const uint16_t*>(lds.s[0] + in * Lds::kScaleBytes + b * kPageScales + s_at);
         }
-        bf16x8 vf[2 * DB];  // value fragment i: keys 32 (i / DB) .. + 31, elements 16 (i % DB) .. + 15
-        auto vread = [&](int i) {
-            const unsigned char* const at = vb + v_from[i % DB] + (i / DB) * 2 * kPage * 2 * D;
-            const u32x2 lo = read_transposed(at), hi = read_transposed(at + kPage * 2 * D);
-            vf[i] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-        };
         __builtin_amdgcn_sched_barrier(0);
-        // s[rb][b][v] is the score of row 16 rb + j16 and tile key 16 b + 4 g4 + v
-        f32x4 s[RB][KB];
+    };
+    auto scores = [&]() {
 #pragma unroll
-        for (int part = 0; part < QueryRow<D>::kParts; ++part) {
+        for (int part = 0; part < QueryRow<D>::kParts; ++part)
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
 #pragma unroll
@@ -606,17 +618,16 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
                     s[rb][b] = mfma_fp4_fp8(kf[b], q[rb].w[part], part == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb][b], ks[b], q[rb].scale[part]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            // the first value fragments go out before the last products; they land during those and the softmax
-            if (part == 0) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) vread(i);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
-
-        const int key0 = kt * kBlockN;
-        const bool masked = key0 + kBlockN - 1 > first_masked;
-        if (masked) {
+    };
+    auto vread = [&](int buf, int i) {
+        const unsigned char* const at = lds.v[0] + buf * Lds::kValueBytes + v_from[i % DB] + (i / DB) * 2 * kPage * 2 * D;
+        const u32x2 lo = read_transposed(at), hi = read_transposed(at + kPage * 2 * D);
+        vf[i] = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+    };
+    // masks the tile's scores and, where a row has no exponent offset yet (or in the exact pass), takes it
+    auto offsets = [&](int tile) {
+        const int key0 = (it.kt_begin + tile) * kBlockN;
+        if (key0 + kBlockN - 1 > first_masked) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const int rel = lim[rb] - key0 - 4 * g4;
@@ -653,77 +664,142 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pf[RB][2];
-        // pair x of a half's eight weights of a row, as bf16, and its part of the row sum
-        auto w_pair = [&](int rb, int hb, int x) {
-            const f32x4 y = s[rb][2 * hb + (x >> 1)];
-            const bf16x2 pq = {(__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1)], c, neg_off[rb])),
-                               (__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1) + 1], c, neg_off[rb]))};
-            pf[rb][hb][2 * x] = pq[0];
-            pf[rb][hb][2 * x + 1] = pq[1];
-            l_run[rb] = __builtin_amdgcn_fdot2_f32_bf16(pq, ones, l_run[rb], false);
-            asm volatile("" : "+v"(l_run[rb]));
-        };
-        // (weights in blocks: attention_kernels.h)
-        constexpr bool kAllFirst = WAVES == kWideWaves;
+    };
+    // pair x of a half's eight weights of a row, as bf16
+    auto w_pair = [&](int rb, int hb, int x) {
+        const f32x4 y = s[rb][2 * hb + (x >> 1)];
+        const bf16x2 pq = {(__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1)], c, neg_off[rb])),
+                           (__bf16)__builtin_amdgcn_exp2f(fmaf(y[2 * (x & 1) + 1], c, neg_off[rb]))};
+        pf[rb][hb][2 * x] = pq[0];
+        pf[rb][hb][2 * x + 1] = pq[1];
+    };
+    auto weights = [&](int hb) {
 #pragma unroll
-        for (int hb = 0; hb < (kAllFirst ? 2 : 1); ++hb)
+        for (int x = 0; x < 8; ++x) w_pair(x & 1, hb, x >> 1);
+    };
+    auto value_products = [&](int buf, int i) {
+        if (i + kAhead < 2 * DB) vread(buf, i + kAhead);
+        if (i % DB == 0) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) w_pair(rb, hb, x);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 2 * DB; ++i) {
-            const int hb = i / DB, db = i % DB;
-            if (i + kAhead < 2 * DB) vread(i + kAhead);
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-                o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[rb][hb], o[rb][db], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (!kAllFirst && hb == 0 && db % (DB / 4) == DB / 4 - 1) {
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) w_pair(rb, 1, db / (DB / 4));
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int rb = 0; rb < RB; ++rb) l_run[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[rb][i / DB], l_run[rb], 0, 0, 0);
         }
-        if (masked) {
-            // value blocks that held a NaN (lane = key of the tile)
-            uint64_t nan[NB];
-            uint64_t any = 0;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                nan[b] = __ballot(key0 + lane < L && sb[(lane * NB + b) * 2 + 1] == kFp4Nan);
-                any |= nan[b];
-            }
-            if (any != 0) {
+        for (int rb = 0; rb < RB; ++rb)
+            o[rb][i % DB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[rb][i / DB], o[rb][i % DB], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // value blocks that held a NaN, in a tile where some row sees some key not (lane = key of the tile)
+    auto nan_values = [&](int tile) {
+        const int key0 = (it.kt_begin + tile) * kBlockN;
+        if (key0 + kBlockN - 1 <= first_masked) return;
+        const unsigned char* const sb = lds.s[0] + tile % Lds::kSlots * Lds::kScaleBytes;
+        uint64_t nan[NB];
+        uint64_t any = 0;
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const int seen = lim[rb] - key0;  // keys 0 .. seen of the tile
-                    const uint64_t sees = seen < 0 ? 0ull : ~0ull >> (63 - min(seen, 63));
+        for (int b = 0; b < NB; ++b) {
+            nan[b] = __ballot(key0 + lane < L && sb[(lane * NB + b) * 2 + 1] == kFp4Nan);
+            any |= nan[b];
+        }
+        if (any != 0) {
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        const float add = (nan[db / 2] & sees) != 0 ? __builtin_nanf("") : 0.f;
+            for (int rb = 0; rb < RB; ++rb) {
+                const int seen = lim[rb] - key0;  // keys 0 .. seen of the tile
+                const uint64_t sees = seen < 0 ? 0ull : ~0ull >> (63 - min(seen, 63));
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) o[rb][db][v] += add;
-                    }
+                for (int db = 0; db < DB; ++db) {
+                    const float add = (nan[db / 2] & sees) != 0 ? __builtin_nanf("") : 0.f;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o[rb][db][v] += add;
                 }
             }
         }
     };
 
-    int kt = it.kt_begin;
+    const int tiles = it.kt_end - it.kt_begin;
+    int tile = 0;
+    // 4 wavefronts: tile after tile, another workgroup's wavefronts beside them. The first half's weights as a block, a
+    // quarter of the second half's after every quarter of the products with the first (attention_kernels.h).
     auto step = [&](const int cur) {
-        const bool more = kt + 1 < it.kt_end;
-        if (more) {
-            copy_tile(1 - cur, page_at(ids, wave & 3));
-            load_values(page_at(ids, v_page));
-            if (kt + 2 < it.kt_end) ids = fetch_ids(kt + 2);
+        kread(tile);
+        if (tile + 1 < tiles) read_codes(tile + 1);
+        if (tile + 2 < tiles) copy_tile(tile + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        scores();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) vread(cur, i);
+        __builtin_amdgcn_sched_barrier(0);
+        if (tile + 1 < tiles) put_values(1 - cur, tile + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        offsets(tile);
+        weights(0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            value_products(cur, i);
+            if (i < DB && i % (DB / 4) == DB / 4 - 1) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) w_pair(rb, 1, i / (DB / 4));
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        compute_tile(cur, kt);
-        if (more) store_values(1 - cur, kt + 1);
+        nan_values(tile);
         wait_vmem<0>();
         __syncthreads();
+    };
+    // 8 wavefronts: in turns. The two wavefronts of a SIMD are half a tile apart: while one multiplies (the values of
+    // tile t, then the keys of tile t + 1), the other computes weights and widens the values of the next tile, and at a barrier
+    // they change. In the turns 0, 1, .. the wavefronts ahead multiply in 2 t + 2 and weigh tile t in 2 t + 1, those behind a
+    // turn later. So
+    //   - values of t + 1 are written in turns 2 t + 1 and 2 t + 2, and read in 2 t + 4 and 2 t + 5: three buffers;
+    //   - codes of tile t + 2 are asked for in turn 2 t + 1 (values, scales) and 2 t + 2 (keys), waited for at the end of the
+    //     turn after, and needed from turn 2 t + 3 (values, scales) and 2 t + 4 (keys) on; what lay there was tile t - 2's,
+    //     whose scales were read last in turn 2 t - 1.
+    auto change = [&]() {  // (this wavefront's writes to LDS are over; the reads of the first value fragments may go on)
+        static_assert(2 * kAhead == 8, "the wait");
+        asm volatile("s_waitcnt lgkmcnt(8)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto turns = [&]() {
+        int buf = 0;
+        if (wave >= WAVES / 2) change();
+        __builtin_amdgcn_s_setprio(2);
+        kread(0);
+        scores();
+        wait_vmem<0>();
+        change();
+        while (true) {
+            __builtin_amdgcn_s_setprio(0);
+            const int next = buf == 2 ? 0 : buf + 1;
+            const bool more = tile + 1 < tiles;
+            if (more) read_codes(tile + 1);
+            if (tile + 2 < tiles) copy_tile(tile + 2);
+            offsets(tile);
+            if (more) put_values(next, tile + 1);
+            weights(0);
+            weights(1);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) asm volatile("" : "+v"(pf[rb][0]), "+v"(pf[rb][1]));  // (in this turn)
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) vread(buf, i);
+            change();
+            __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) {
+                value_products(buf, i);
+                if (i == 2 * DB - kAhead && more) kread(tile + 1);
+            }
+            nan_values(tile);
+            buf = next;
+            ++tile;
+            if (!more) break;
+            scores();
+            wait_vmem<0>();
+            change();
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (wave < WAVES / 2) change();
     };
     for (;;) {
 #pragma unroll
@@ -732,39 +808,44 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
             for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
             m_run[rb] = -INFINITY;
             neg_off[rb] = 0.f;
-            l_run[rb] = 0.f;
+            l_run[rb] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         need_max = true;
-        kt = it.kt_begin;
-        if (exact) ids = fetch_ids(kt);
-        {
-            copy_tile(0, page_at(ids, wave & 3));
-            load_values(page_at(ids, v_page));
-            if (kt + 1 < it.kt_end) ids = fetch_ids(kt + 1);
-            store_values(0, kt);
-        }
+        tile = 0;
+        if (exact) ids = fetch_ids(0);
+        ids_next = fetch_ids(1);
+        copy_tile(0);
         wait_vmem<0>();
         __syncthreads();
-        while (true) {
-            step(0);
-            if (++kt >= it.kt_end) break;
-            step(1);
-            if (++kt >= it.kt_end) break;
+        read_codes(0);
+        if (tiles > 1) copy_tile(1);
+        put_values(0, 0);
+        wait_vmem<0>();
+        __syncthreads();
+        if constexpr (WAVES == kWideWaves) {
+            turns();
+        } else {
+            while (true) {
+                step(0);
+                if (++tile >= tiles) break;
+                step(1);
+                if (++tile >= tiles) break;
+            }
         }
-        if (exact || !__syncthreads_or(!(l_run[0] <= 0x1p100f) || !(l_run[RB - 1] <= 0x1p100f))) break;
+        if (exact || !__syncthreads_or(!(l_run[0][0] <= 0x1p100f) || !(l_run[RB - 1][0] <= 0x1p100f))) break;
         exact = true;
     }
 
     float inv[RB], lse_v[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const float l = row_sum4(l_run[rb]);
+        const float l = l_run[rb][0];
         inv[rb] = l > 0.f ? 1.f / l : 0.f;
         lse_v[rb] = l > 0.f ? (m_run[rb] + log2f(l)) * kLn2 : (it.part >= 0 && l != l ? l : -INFINITY);
     }
     // o[rb][db][v] is element d = 16 db + 4 g4 + v of row 16 rb + j16. Rows go through LDS (the values' buffers, no longer
     // read), so that a store covers whole rows: each wavefront a part of its own, as many of its rows at a time as fit.
-    constexpr int kStage = 2 * Fp4Lds<D, WAVES>::kValueBytes / WAVES;
+    constexpr int kStage = 2 * Fp4Lds<D, WAVES>::kValueBytes / WAVES;  // (two of the buffers)
     unsigned char* const stage = lds.v[0] + wave * kStage;
     auto through_stage = [&](auto out_bytes, auto&& put, auto&& get) {
         constexpr int kOutRow = decltype(out_bytes)::value;
