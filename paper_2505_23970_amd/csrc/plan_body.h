@@ -212,36 +212,63 @@ __device__ __forceinline__ void plan_body(const PlanArgs& a, PlanLds& sm) {
         return;
     }
 
-    // 3. items at their sorted positions
-    for (int g = tid; g < total_tiles; g += kPlanThreads) {
-        const Tile t = tile_at(a, lens, g);
-        int part0 = -1;
-        if (t.ns > 1) {
-            part0 = atomicAdd(&s_part, t.ns);
-            const int ci = atomicAdd(&s_comb, 1);
-            if (part0 + t.ns > a.expect_partials || ci >= a.expect_combines) {
-                s_bad = 1;  // cannot happen when the item totals matched; never write out of range
-                part0 = -2;
-            } else {
-                a.combines[ci] = CombineItem{t.r, t.q0, part0, t.ns};
+    // 3. items at their sorted positions. A thread hands out its query tile's chunks one by one; where they are many, its
+    // wavefront does together (one request of 120000 tokens in 128 chunks: 27.6 -> 6.6 us).
+    constexpr int kAlone = 32;
+    for (int g0 = 0; g0 < total_tiles; g0 += kPlanThreads) {
+        const int g = g0 + tid;
+        Tile t{0, 0, 0, 0, 0};
+        int part0 = -1, pos_lo = 0, pos_hi = 0, lo = 0, n_hi = 0;
+        if (g < total_tiles) {
+            t = tile_at(a, lens, g);
+            if (t.ns > 1) {
+                part0 = atomicAdd(&s_part, t.ns);
+                const int ci = atomicAdd(&s_comb, 1);
+                if (part0 + t.ns > a.expect_partials || ci >= a.expect_combines) {
+                    s_bad = 1;  // cannot happen when the item totals matched; never write out of range
+                    part0 = -2;
+                } else {
+                    a.combines[ci] = CombineItem{t.r, t.q0, part0, t.ns};
+                }
             }
+            // reserve the tile's positions in both cost buckets at once, then hand them out
+            lo = t.kt / t.ns;
+            n_hi = t.kt - lo * t.ns;
+            const int n_lo = t.ns - n_hi;
+            pos_lo = n_lo > 0 ? atomicAdd(&s_hist[bucket_of(a, lo, t.req_tiles)], n_lo) : 0;
+            pos_hi = n_hi > 0 ? atomicAdd(&s_hist[bucket_of(a, lo + 1, t.req_tiles)], n_hi) : 0;
         }
-        // reserve the tile's positions in both cost buckets at once, then hand them out
-        const int lo = t.kt / t.ns, n_hi = t.kt - lo * t.ns, n_lo = t.ns - n_hi;
-        int pos_lo = n_lo > 0 ? atomicAdd(&s_hist[bucket_of(a, lo, t.req_tiles)], n_lo) : 0;
-        int pos_hi = n_hi > 0 ? atomicAdd(&s_hist[bucket_of(a, lo + 1, t.req_tiles)], n_hi) : 0;
+        auto item = [&](const Tile& x, int part, int s, int b0, int b1) {
+            return part == -2 ? WorkItem{-1, 0, 0, 0, -1, 0, 0, 0}
+                              : WorkItem{x.r, x.q0, b0, b1, part < 0 ? -1 : part + s, lens.prefix[x.r], lens.cu[x.r],
+                                         lens.cu[x.r + 1] - lens.cu[x.r]};
+        };
         // chunk s covers [floor(s kt / ns), floor((s + 1) kt / ns)): lo or lo + 1 tiles, one
         // more whenever the remainders add up to ns (with a 64-bit division per chunk, and all
         // 2048 buckets, the plan of 32 decode requests took 13.2 us, now 11.0)
-        int b0 = 0, b1 = 0, rest = 0;
-        for (int s = 0; s < t.ns; ++s, b0 = b1) {
-            rest += n_hi;
-            b1 = b0 + lo + (rest >= t.ns ? 1 : 0);
-            if (rest >= t.ns) rest -= t.ns;
-            const int pos = b1 - b0 == lo ? pos_lo++ : pos_hi++;
-            a.items[pos] = part0 == -2 ? WorkItem{-1, 0, 0, 0, -1, 0, 0, 0}
-                                       : WorkItem{t.r, t.q0, b0, b1, part0 < 0 ? -1 : part0 + s, lens.prefix[t.r],
-                                                  lens.cu[t.r], lens.cu[t.r + 1] - lens.cu[t.r]};
+        if (t.ns <= kAlone) {
+            int b0 = 0, b1 = 0, rest = 0, p_lo = pos_lo, p_hi = pos_hi;
+            for (int s = 0; s < t.ns; ++s, b0 = b1) {
+                rest += n_hi;
+                b1 = b0 + lo + (rest >= t.ns ? 1 : 0);
+                if (rest >= t.ns) rest -= t.ns;
+                const int pos = b1 - b0 == lo ? p_lo++ : p_hi++;
+                a.items[pos] = item(t, part0, s, b0, b1);
+            }
+        }
+        for (uint64_t many = __ballot(t.ns > kAlone); many != 0; many &= many - 1) {
+            const int src = (int)__builtin_ctzll(many);
+            const Tile x{__shfl(t.r, src), __shfl(t.q0, src), 0, __shfl(t.ns, src), 0};
+            const int part = __shfl(part0, src), at_lo = __shfl(pos_lo, src), at_hi = __shfl(pos_hi, src);
+            const int len = __shfl(lo, src), longer = __shfl(n_hi, src);
+            for (int s = (int)threadIdx.x & 63; s < x.ns; s += 64) {
+                // longer ones before chunk s, and before the next (one division: they differ by one at most)
+                const int64_t all = (int64_t)s * longer;
+                const int before = (int)(all / x.ns);
+                const int with = before + (all - (int64_t)before * x.ns + longer >= x.ns ? 1 : 0);
+                const int b0 = s * len + before, b1 = b0 + len + (with - before);
+                a.items[with > before ? at_hi + before : at_lo + s - before] = item(x, part, s, b0, b1);
+            }
         }
     }
     __syncthreads();
