@@ -674,7 +674,6 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
     return gc::launch_append_rotary(ra, geo->head_dim, kind, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
-// The plain append into 4-bit pools: the rotary one's launch without a rotation.
 gc_status append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_new, const void* v_new,
                      void* k_pool, void* v_pool, void* scales, hipStream_t stream) {
     Shape sh;
@@ -684,15 +683,9 @@ gc_status append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* 
     st = check_fp4(k_pool, v_pool, scales);
     if (st != GC_OK) return st;
     if (!aligned16(k_new) || !aligned16(v_new)) return GC_ERR_BAD_SHAPE;
-    gc::RotaryArgs ra{};
-    ra.a = append_args(geo, batch, sh, k_new, v_new, k_pool, v_pool, PoolKind{});
-    if (gc::rotary_workgroups(ra.a.total_pages, geo->num_q_heads, geo->num_kv_heads, geo->head_dim, false) > gc::kMaxWorkgroups)
-        return GC_ERR_UNSUPPORTED;
-    ra.k_stride = ra.v_stride = (int64_t)geo->num_kv_heads * geo->head_dim;
-    ra.num_q_heads = geo->num_q_heads;
-    ra.num_positions = INT32_MAX;
-    ra.scales = static_cast<uint8_t*>(scales);
-    return gc::launch_append_rotary(ra, geo->head_dim, gc::Pool::kFp4, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
+    const gc::AppendArgs a = append_args(geo, batch, sh, k_new, v_new, k_pool, v_pool, PoolKind{});
+    if (gc::head_page_workgroups(a.total_pages, geo->num_kv_heads, geo->head_dim) > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
+    return gc::launch_append_fp4(a, static_cast<uint8_t*>(scales), geo->head_dim, stream) == hipSuccess ? GC_OK : GC_ERR_HIP;
 }
 
 gc_status read_rows(const gc_geometry* geo, const gc_batch* batch, const void* k_pool, const void* v_pool,
@@ -712,7 +705,7 @@ gc_status read_rows(const gc_geometry* geo, const gc_batch* batch, const void* k
             return GC_ERR_BAD_SHAPE;
     gc::ReadArgs ra{};
     ra.a = append_args(geo, batch, sh, nullptr, nullptr, const_cast<void*>(k_pool), const_cast<void*>(v_pool), PoolKind{});
-    if (gc::read_workgroups(ra.a.total_pages, geo->num_kv_heads, geo->head_dim) > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
+    if (gc::head_page_workgroups(ra.a.total_pages, geo->num_kv_heads, geo->head_dim) > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
     ra.k_out = static_cast<uint16_t*>(k_out);
     ra.v_out = static_cast<uint16_t*>(v_out);
     ra.scales = static_cast<const uint8_t*>(pk.scales4);

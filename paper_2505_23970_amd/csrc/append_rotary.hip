@@ -160,13 +160,11 @@ __device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm
 // no byte with another token's. Four lanes hold the 32 elements of a block. Rotated keys are computed in 64
 // bits and rounded to 32 (the products of a bf16 and an fp32 number are exact there, so that the codes are those
 // of the definition, next to a border too): the conversions and products cost nothing that shows beside the memory.
-// rotary_dim 0: keys as they are.
 template <int D>
 __device__ __forceinline__ void rotary_kv_fp4(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int hg) {
     const AppendArgs& a = ra.a;
     constexpr int CPR = D / 8;
     constexpr int kPer = kPage * CPR;
-    constexpr int kBlocks = D / kFp4Block;
     const int tid = threadIdx.x % kPer;
     const int h = hg * AppendLds<D>::kHeads + threadIdx.x / kPer;
     const bool head_ok = h < a.num_kv_heads;
@@ -202,7 +200,7 @@ __device__ __forceinline__ void rotary_kv_fp4(const RotaryArgs& ra, const PageUn
                 x[2 * j + 1] = (float)fma(q, co, p * si);
             }
         }
-    } else if (half > 0) {
+    } else {
         const int lane = threadIdx.x & 63;
         const int from = turned ? lane + (c < half ? half : -half) : lane;
         u32x4 other;
@@ -216,18 +214,9 @@ __device__ __forceinline__ void rotary_kv_fp4(const RotaryArgs& ra, const PageUn
             for (int j = 0; j < 8; ++j) x[j] = (float)fma((double)x[j], (double)cs[j], low * ((double)z[j] * (double)sn[j]));
         }
     }
-    uint32_t kt = 0, vt = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        kt = max(kt, __float_as_uint(x[j]) & 0x7FFFFFFFu);
-        vt = max(vt, __float_as_uint(y[j]) & 0x7FFFFFFFu);
-    }
-    const uint32_t ks = fp4_scale_code(quad_max(kt)), vs = fp4_scale_code(quad_max(vt));
-    if (!ok || blk < 0 || blk >= a.num_blocks) return;
     const int64_t slot = ((int64_t)blk * a.num_kv_heads + h) * kPage + s;
-    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.k_pool) + slot * (D / 2) + c * 4) = fp4_quantise8(x, ks);
-    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.v_pool) + slot * (D / 2) + c * 4) = fp4_quantise8(y, vs);
-    if (c % 4 == 0) *reinterpret_cast<uint16_t*>(ra.scales + (slot * kBlocks + c / 4) * 2) = (uint16_t)(ks | vs << 8);
+    fp4_store<D>(static_cast<uint8_t*>(a.k_pool), static_cast<uint8_t*>(a.v_pool), ra.scales, slot, c, x, y,
+                 ok && blk >= 0 && blk < a.num_blocks);
 }
 
 // kRotQHeads query heads (group qg) of the tokens of one page.

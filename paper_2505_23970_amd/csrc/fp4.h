@@ -55,5 +55,23 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
 }
 
+// Eight elements of a token's key and of its value, chunk c of the row (four lanes hold a block), into its slot: codes, and by
+// the first of the four lanes the block's scales. All lanes of a wavefront call it, those that store nothing with ok false.
+template <int D>
+__device__ __forceinline__ void fp4_store(uint8_t* k_pool, uint8_t* v_pool, uint8_t* scales, int64_t slot, int c,
+                                          const float (&k)[8], const float (&v)[8], bool ok) {
+    uint32_t kt = 0, vt = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        kt = max(kt, __float_as_uint(k[j]) & 0x7FFFFFFFu);
+        vt = max(vt, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+    }
+    const uint32_t ks = fp4_scale_code(quad_max(kt)), vs = fp4_scale_code(quad_max(vt));
+    if (!ok) return;
+    *reinterpret_cast<uint32_t*>(k_pool + slot * (D / 2) + c * 4) = fp4_quantise8(k, ks);
+    *reinterpret_cast<uint32_t*>(v_pool + slot * (D / 2) + c * 4) = fp4_quantise8(v, vs);
+    if (c % 4 == 0) *reinterpret_cast<uint16_t*>(scales + (slot * (D / kFp4Block) + c / 4) * 2) = (uint16_t)(ks | vs << 8);
+}
+
 }  // namespace
 }  // namespace gc

@@ -389,8 +389,10 @@ struct CombineArgs {
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool fp8, hipStream_t s);
 hipError_t launch_plan(const PlanArgs& a, hipStream_t s);
 hipError_t launch_append_rotary(const RotaryArgs& ra, int head_dim, Pool kind, hipStream_t s);
+hipError_t launch_append_fp4(const AppendArgs& a, uint8_t* scales, int head_dim, hipStream_t s);
 hipError_t launch_read(const ReadArgs& ra, int head_dim, Pool kind, hipStream_t s);
-int64_t read_workgroups(int64_t pages, int num_kv_heads, int head_dim);  // of that launch
+// the most workgroups of either launch
+int64_t head_page_workgroups(int64_t pages, int num_kv_heads, int head_dim);
 // workgroups of that launch
 int64_t rotary_workgroups(int64_t pages, int num_q_heads, int num_kv_heads, int head_dim, bool with_q);
 // append (AppendArgs) and plan (PlanArgs) in one launch

@@ -16,6 +16,8 @@
 namespace gc {
 namespace {
 
+constexpr int64_t kManyWorkgroups = 4096;  // (workgroups of one head each)
+
 // Eight E4M3 codes times scale as eight bf16 values.
 __device__ __forceinline__ u32x4 widen_fp8x8(const u32x2 w, float scale) {
     u32x4 r;
@@ -31,15 +33,21 @@ __device__ __forceinline__ u32x4 widen_fp8x8(const u32x2 w, float scale) {
     return r;
 }
 
-template <int D, Pool KIND>
+template <int D, Pool KIND, int HEADS>
 __global__ __launch_bounds__(kAppendThreads) void read_kernel(const ReadArgs ra) {
-    __shared__ AppendLds<D> lds;
     const AppendArgs& a = ra.a;
     constexpr int CPR = D / 8;
     constexpr int kPer = kPage * CPR;  // threads per head
+    constexpr int kBeside = AppendLds<D>::kHeads;
+    constexpr int kStride = AppendLds<D>::kStride;
+    constexpr bool kRows = KIND == Pool::kFp4;  // values lie as rows
+    __shared__ union {
+        AppendLds<D> search;
+        uint16_t v[kRows ? 1 : HEADS][kRows ? 1 : kBeside][kRows ? 1 : kPage * kStride];
+    } lds;
     const unsigned u = blockIdx.x / ra.jobs, hg = blockIdx.x - u * ra.jobs;
     PageUnit at;
-    if (!locate_page<D>(a, lds, (int)u, (int)gridDim.x, at)) return;
+    if (!locate_page<D>(a, lds.search, (int)u, (int)gridDim.x, at)) return;
     const int lp = at.P / kPage + at.k;
     const int s0 = max(at.P - lp * kPage, 0);
     const int s1 = min(at.P + at.n - lp * kPage, kPage);
@@ -47,78 +55,97 @@ __global__ __launch_bounds__(kAppendThreads) void read_kernel(const ReadArgs ra)
     const int blk = a.block_tables[(int64_t)at.r * a.max_blocks + lp];
     if (blk < 0 || blk >= a.num_blocks) return;
     const int tid = threadIdx.x % kPer, sub = threadIdx.x / kPer;
-    const int h = (int)hg * AppendLds<D>::kHeads + sub;
-    const bool head_ok = h < a.num_kv_heads;
     const int s = tid / CPR, c = tid % CPR;
     const int64_t row = (int64_t)at.cu + (int64_t)lp * kPage - at.P + s;
-    const bool ok = head_ok && s >= s0 && s < s1 && row >= 0 && row < a.total_tokens;
-    const int64_t page = (int64_t)blk * a.num_kv_heads + h;
-    const int64_t slot = page * kPage + s;
-    u32x4 k = u32x4{0u, 0u, 0u, 0u}, v = k;
-    if constexpr (KIND == Pool::kFp4) {
+    const int h0 = (int)hg * (HEADS * kBeside) + sub;
+    const bool ok = s >= s0 && s < s1 && row >= 0 && row < a.total_tokens;
+    const int64_t page0 = (int64_t)blk * a.num_kv_heads;
+    u32x4 k[HEADS], v[HEADS];
+    if constexpr (kRows) {
+        uint32_t kw[HEADS], vw[HEADS], sc[HEADS];
         if (!ok) return;
-        const uint32_t kw = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.k_pool) + slot * (D / 2) + c * 4);
-        const uint32_t vw = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v_pool) + slot * (D / 2) + c * 4);
-        const uint32_t sc = *reinterpret_cast<const uint16_t*>(ra.scales + (slot * (D / kFp4Block) + c / 4) * 2);
-        uint32_t w[4];
-        fp4_widen8(kw, fp4_scale(sc & 255), w);
-        k = u32x4{w[0], w[1], w[2], w[3]};
-        fp4_widen8(vw, fp4_scale(sc >> 8), w);
-        v = u32x4{w[0], w[1], w[2], w[3]};
-    } else {
-        if (ok) {
-            if constexpr (KIND == Pool::kFp8)
-                k = widen_fp8x8(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.k_pool) + slot * D + c * 8), ra.k_scale);
-            else
-                k = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.k_pool) + slot * D + c * 8);
-        }
-        constexpr int kStride = AppendLds<D>::kStride;
-        uint16_t* const sv = lds.v[sub];
-        if (head_ok) {
-            const int d = tid >> 1, x0 = 8 * (tid & 1);
-            const int64_t src = (page * D + d) * kPage + x0;
-            u32x4 w;
-            if constexpr (KIND == Pool::kFp8)
-                w = widen_fp8x8(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.v_pool) + src), ra.v_scale);
-            else
-                w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.v_pool) + src);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) sv[(x0 + x) * kStride + d] = (uint16_t)(w[x / 2] >> (16 * (x % 2)));
+        for (int i = 0; i < HEADS; ++i) {
+            const int h = min(h0 + i * kBeside, a.num_kv_heads - 1);  // (a head twice rather than none)
+            const int64_t slot = (page0 + h) * kPage + s;
+            kw[i] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.k_pool) + slot * (D / 2) + c * 4);
+            vw[i] = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.v_pool) + slot * (D / 2) + c * 4);
+            sc[i] = *reinterpret_cast<const uint16_t*>(ra.scales + (slot * (D / kFp4Block) + c / 4) * 2);
         }
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            uint32_t w[4];
+            fp4_widen8(kw[i], fp4_scale(sc[i] & 255), w);
+            k[i] = u32x4{w[0], w[1], w[2], w[3]};
+            fp4_widen8(vw[i], fp4_scale(sc[i] >> 8), w);
+            v[i] = u32x4{w[0], w[1], w[2], w[3]};
+        }
+    } else {
+        // Value pages are transposed: thread (value row d, half of the slots) brings eight slots, through LDS.
+        const int d = tid >> 1, x0 = 8 * (tid & 1);
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) {
+            const int h = min(h0 + i * kBeside, a.num_kv_heads - 1);
+            const int64_t from = ((page0 + h) * kPage + s) * D + c * 8, v_from = ((page0 + h) * D + d) * kPage + x0;
+            if constexpr (KIND == Pool::kFp8) {
+                k[i] = widen_fp8x8(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.k_pool) + from), ra.k_scale);
+                v[i] = widen_fp8x8(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(a.v_pool) + v_from), ra.v_scale);
+            } else {
+                k[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.k_pool) + from);
+                v[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.v_pool) + v_from);
+            }
+        }
+        __syncthreads();  // (the search is over)
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) lds.v[i][sub][(x0 + x) * kStride + d] = (uint16_t)(v[i][x / 2] >> (16 * (x % 2)));
         __syncthreads();
         if (!ok) return;
-        v = *reinterpret_cast<const u32x4*>(&sv[s * kStride + c * 8]);
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) v[i] = *reinterpret_cast<const u32x4*>(&lds.v[i][sub][s * kStride + c * 8]);
     }
-    const int64_t dst = (row * a.num_kv_heads + h) * D + c * 8;
-    *reinterpret_cast<u32x4*>(ra.k_out + dst) = k;
-    *reinterpret_cast<u32x4*>(ra.v_out + dst) = v;
+#pragma unroll
+    for (int i = 0; i < HEADS; ++i) {
+        const int h = h0 + i * kBeside;
+        if (h >= a.num_kv_heads) return;
+        const int64_t dst = (row * a.num_kv_heads + h) * D + c * 8;
+        *reinterpret_cast<u32x4*>(ra.k_out + dst) = k[i];
+        *reinterpret_cast<u32x4*>(ra.v_out + dst) = v[i];
+    }
+}
+
+template <int D, Pool KIND, int MOST>
+void launch_kind(ReadArgs ra, hipStream_t s) {
+    const int64_t one = head_page_workgroups(ra.a.total_pages, ra.a.num_kv_heads, D);
+    const int groups = ceil_div(ra.a.num_kv_heads, append_heads(D));
+    if (one >= kManyWorkgroups) {
+        ra.jobs = (uint32_t)ceil_div(groups, MOST);
+        read_kernel<D, KIND, MOST><<<ra.jobs * (unsigned)ra.a.total_pages, kAppendThreads, 0, s>>>(ra);
+    } else {
+        ra.jobs = (uint32_t)groups;
+        read_kernel<D, KIND, 1><<<(unsigned)one, kAppendThreads, 0, s>>>(ra);
+    }
 }
 
 template <int D>
-void launch_kind(const ReadArgs& ra, Pool kind, unsigned grid, hipStream_t s) {
+void launch(const ReadArgs& ra, Pool kind, hipStream_t s) {
     if (kind == Pool::kFp4)
-        read_kernel<D, Pool::kFp4><<<grid, kAppendThreads, 0, s>>>(ra);
+        launch_kind<D, Pool::kFp4, 8>(ra, s);
     else if (kind == Pool::kFp8)
-        read_kernel<D, Pool::kFp8><<<grid, kAppendThreads, 0, s>>>(ra);
+        launch_kind<D, Pool::kFp8, 4>(ra, s);
     else
-        read_kernel<D, Pool::kBf16><<<grid, kAppendThreads, 0, s>>>(ra);
+        launch_kind<D, Pool::kBf16, 4>(ra, s);
 }
 
 }  // namespace
 
-int64_t read_workgroups(int64_t pages, int num_kv_heads, int head_dim) {
-    return pages * ceil_div(num_kv_heads, append_heads(head_dim));
-}
-
-hipError_t launch_read(const ReadArgs& args, int head_dim, Pool kind, hipStream_t s) {
-    ReadArgs ra = args;
+hipError_t launch_read(const ReadArgs& ra, int head_dim, Pool kind, hipStream_t s) {
     if (ra.a.total_pages <= 0) return hipSuccess;
-    ra.jobs = (uint32_t)read_workgroups(1, ra.a.num_kv_heads, head_dim);
-    const unsigned grid = ra.jobs * (unsigned)ra.a.total_pages;
     if (head_dim == 128)
-        launch_kind<128>(ra, kind, grid, s);
+        launch<128>(ra, kind, s);
     else
-        launch_kind<64>(ra, kind, grid, s);
+        launch<64>(ra, kind, s);
     return hipGetLastError();
 }
 
