@@ -3,8 +3,9 @@
 // of kHeads KV heads or groups of heads; thread (slot s, chunk c) takes eight elements of a key row and of a value row of each,
 // four neighbouring lanes a block.
 // What bounds it: memory, and for a few tokens the chain lengths -> block id, rows -> codes. A workgroup of one head has 8 KB in
-// flight and starts too often: from kManyWorkgroups of them on, a workgroup takes four (32000 tokens of 8 heads, d = 64:
-// 29.8 -> 24.3 us).
+// flight and starts too often: from kManyWorkgroups of them on, a workgroup takes four (32000 tokens of 8 heads, d = 64, 96 MB:
+// 29.8 -> 19.6 us; two 20.9, eight 22.1). Rows of more than the last-level cache keeps, 192 MB, are read past it (66000 tokens,
+// d = 128, 340 MB: 59.8 us, else 68.4; but 96 MB 20.1 / 19.6).
 #include "append_body.h"
 #include "fp4.h"
 
@@ -13,7 +14,7 @@ namespace {
 
 constexpr int64_t kManyWorkgroups = 4096;
 
-template <int D, int HEADS>
+template <int D, int HEADS, bool STREAM>
 __global__ __launch_bounds__(kAppendThreads) void append_fp4_kernel(const AppendArgs a, uint8_t* scales, uint32_t jobs) {
     __shared__ AppendLds<D> lds;
     constexpr int CPR = D / 8;
@@ -39,8 +40,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_fp4_kernel(const Append
         k[i] = v[i] = u32x4{0u, 0u, 0u, 0u};
         if (ok && h < a.num_kv_heads) {  // (before the block id is looked at, so that the loads run beside its own)
             const int64_t src = (row * a.num_kv_heads + h) * D + c * 8;
-            k[i] = *reinterpret_cast<const u32x4*>(a.k_new + src);
-            v[i] = *reinterpret_cast<const u32x4*>(a.v_new + src);
+            const u32x4* const kp = reinterpret_cast<const u32x4*>(a.k_new + src);
+            const u32x4* const vp = reinterpret_cast<const u32x4*>(a.v_new + src);
+            k[i] = STREAM ? __builtin_nontemporal_load(kp) : *kp;
+            v[i] = STREAM ? __builtin_nontemporal_load(vp) : *vp;
         }
     }
     if (blk < 0 || blk >= a.num_blocks) return;
@@ -65,10 +68,14 @@ void launch(const AppendArgs& a, uint8_t* scales, hipStream_t s) {
     const int64_t one = head_page_workgroups(a.total_pages, a.num_kv_heads, D);
     const int groups = ceil_div(a.num_kv_heads, append_heads(D));
     if (one >= kManyWorkgroups) {
-        const int jobs = ceil_div(groups, 4);
-        append_fp4_kernel<D, 4><<<(unsigned)jobs * (unsigned)a.total_pages, kAppendThreads, 0, s>>>(a, scales, (uint32_t)jobs);
+        const uint32_t jobs = (uint32_t)ceil_div(groups, 4);
+        const unsigned grid = jobs * (unsigned)a.total_pages;
+        if ((int64_t)a.total_tokens * a.num_kv_heads * D * 4 >= (192LL << 20))
+            append_fp4_kernel<D, 4, true><<<grid, kAppendThreads, 0, s>>>(a, scales, jobs);
+        else
+            append_fp4_kernel<D, 4, false><<<grid, kAppendThreads, 0, s>>>(a, scales, jobs);
     } else {
-        append_fp4_kernel<D, 1><<<(unsigned)one, kAppendThreads, 0, s>>>(a, scales, (uint32_t)groups);
+        append_fp4_kernel<D, 1, false><<<(unsigned)one, kAppendThreads, 0, s>>>(a, scales, (uint32_t)groups);
     }
 }
 
