@@ -6,7 +6,6 @@ import pytest
 
 import fp4_reference as R
 import gpu_helpers as H
-import oracle
 import rotary_reference as RR
 from paper_2505_23970_amd import workloads as W
 
