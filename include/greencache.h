@@ -460,7 +460,7 @@ gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch,
  *   bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), a scale an OCP E8M0 number: exponent code c stands for
  *   2^(c - 127), 255 for NaN. An element is code value * scale, a bf16 number exactly for the codes
  *   that the append writes (c in 3 .. 252); a block of scale 255 is NaN throughout.
- *   All three are 16-byte aligned (else GC_ERR_BAD_SHAPE).
+ *   All three are 16-byte aligned, and where they are written apart from each other (else GC_ERR_BAD_SHAPE).
  */
 
 /*
@@ -506,8 +506,9 @@ gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const vo
  * every key and value element as the number it stands for. Plans, workspaces, tilings and options are
  * those of the other pools (gc_prefix_prefill_plan and gc_prefix_prefill_workspace_size serve all). A value
  * block that is NaN makes those rows NaN that see its token, in its elements. Errors as those calls, and
- * GC_ERR_BAD_SHAPE for q or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_UNSUPPORTED for a batch of more work
- * than one launch holds. Shared prefixes (gc_shared_prefix_*) are over bf16 and 8-bit pools only.
+ * GC_ERR_BAD_SHAPE for q or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_UNSUPPORTED
+ * for a batch of more work than one launch holds. Shared prefixes (gc_shared_prefix_*) are over bf16 and 8-bit
+ * pools only.
  */
 gc_status gc_prefix_prefill_run_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_plan_options* opts,
                                     const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,

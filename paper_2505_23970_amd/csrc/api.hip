@@ -610,6 +610,14 @@ gc_status check_fp4(const void* k_pool, const void* v_pool, const void* scales) 
     if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(scales)) return GC_ERR_BAD_SHAPE;
     return GC_OK;
 }
+// Of pools that are written: apart from each other, too.
+gc_status check_fp4_written(const gc_geometry* geo, const void* k_pool, const void* v_pool, const void* scales) {
+    const gc_status st = check_fp4(k_pool, v_pool, scales);
+    if (st != GC_OK) return st;
+    const int64_t pool = pool_bytes(geo, gc::Pool::kFp4), sc = scale_bytes(geo);
+    return overlap(k_pool, pool, v_pool, pool) || overlap(k_pool, pool, scales, sc) || overlap(v_pool, pool, scales, sc)
+               ? GC_ERR_BAD_SHAPE : GC_OK;
+}
 
 gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rot, const gc_new_rows* rows,
                         void* q_out, void* k_pool, void* v_pool, const PoolKind& pk, hipStream_t stream) {
@@ -627,7 +635,7 @@ gc_status append_rotary(const gc_geometry* geo, const gc_batch* batch, const gc_
         return GC_ERR_NULL_ARG;
     const gc::Pool kind = pk.pool();
     if (kind == gc::Pool::kFp4) {
-        st = check_fp4(k_pool, v_pool, pk.scales4);
+        st = check_fp4_written(geo, k_pool, v_pool, pk.scales4);
         if (st != GC_OK) return st;
     }
     if ((rows->q == nullptr) != (q_out == nullptr)) return GC_ERR_NULL_ARG;
@@ -680,7 +688,7 @@ gc_status append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* 
     gc_status st = check_common(geo, batch, &sh);
     if (st != GC_OK || sh.total_tokens == 0) return st;
     if (k_new == nullptr || v_new == nullptr) return GC_ERR_NULL_ARG;
-    st = check_fp4(k_pool, v_pool, scales);
+    st = check_fp4_written(geo, k_pool, v_pool, scales);
     if (st != GC_OK) return st;
     if (!aligned16(k_new) || !aligned16(v_new)) return GC_ERR_BAD_SHAPE;
     const gc::AppendArgs a = append_args(geo, batch, sh, k_new, v_new, k_pool, v_pool, PoolKind{});

@@ -52,7 +52,7 @@ def test_scales_and_idempotence():
 STATUS_CALLS = ("append", "rotary", "read", "read_fp8", "read_fp4", "run")
 
 
-def call(lib, name, g, b, k=0x200000, v=0x200000, s=0x200000, k_new=0x10000, v_new=0x20000, scales=(0.5, 0.5),
+def call(lib, name, g, b, k=0x200000, v=0xA00000, s=0xC00000, k_new=0x10000, v_new=0x20000, scales=(0.5, 0.5),
          scale=0.1, ws=0x400000, ws_bytes=1 << 30, q=0x500000, out=0x600000):
     g, d = ctypes.byref(g), ctypes.byref(b.desc)
     if name == "append":
@@ -119,6 +119,15 @@ def test_outputs_over_inputs_are_refused(lib, name):
     assert call(lib, name, g, b, k_new=0x200000 + int(pool) - 16) == -2
     if name == "read_fp4":
         assert call(lib, name, g, b, s=0x10000) == -2
+
+
+@pytest.mark.parametrize("name", ["append", "rotary"])
+def test_written_pools_over_each_other_are_refused(lib, name):
+    g, b = geo(), HostBatch([4], [3])
+    pool, scales = 64 * 2 * 16 * 64, 64 * 2 * 16 * 8
+    for over in (dict(v=0x200000), dict(v=0x200000 + pool - 16), dict(s=0x200000 + pool - 16), dict(s=0x200000 - scales + 16),
+                 dict(s=0xA00000 + pool - 16), dict(s=0xA00000 - scales + 16)):
+        assert call(lib, name, g, b, **over) == -2, over
 
 
 @pytest.mark.parametrize("name", ["append", "rotary", "read", "read_fp8", "read_fp4"])

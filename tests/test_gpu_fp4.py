@@ -307,6 +307,24 @@ def test_nan_reaches_the_rows_that_see_it(tiling, D):
             assert np.array_equal(got[~nan], want[~nan])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tiling", [1, 2, 3], ids=["prefill", "small", "wide"])
+def test_queries_that_are_not_numbers(tiling, D):
+    """NaN or an infinity in a head's query: that head's row is NaN, every other row what it was."""
+    w = W.build([90, 20], [30, 6], 4, 2, D, seed=2850 + D, values="peaked", name="fp4_wild_queries")
+    clean, _ = appended(w)
+    base = numbers(clean.attention(tiling=tiling)[0])
+    nan = np.zeros(base.shape, bool)
+    for (token, head, el), bits in (((3, 1, 7), 0x7FC0), ((17, 2, D - 1), 0x7F80), ((33, 0, 0), 0xFF80)):
+        w.q[token, head, el] = bits
+        nan[token, head] = True
+    run, _ = appended(w)
+    got = numbers(run.attention(tiling=tiling)[0])
+    assert np.array_equal(np.isnan(got), nan), np.argwhere(np.isnan(got) != nan)[:4]
+    # (a NaN sum sends a whole tile through the second pass, whose offsets follow every tile: the other rows may round anew)
+    assert np.allclose(got[~nan], base[~nan], rtol=0, atol=2.0 ** -6 * np.abs(base).max())
+
+
 def test_pages_outside_the_pool_and_stale_blocks():
     """Ids outside the pool behind the last position are never followed; rows past a request's end keep their contents."""
     import torch
