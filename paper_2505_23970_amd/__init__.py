@@ -690,15 +690,16 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
         pool_dtype = torch.uint8 if scales else torch.bfloat16
         _require(k_pool, pool_dtype, "k_pool", device)
         _require(v_pool, pool_dtype, "v_pool", device)
+        _, Hkv, _, D = k_pool.shape
+        pools = (k_pool.data_ptr(), v_pool.data_ptr())
     else:
-        _require_pools4(k_pool, v_pool, scales4, device)
+        geo = _require_pools4(k_pool, v_pool, scales4, None, batch)
+        Hkv, D = geo.num_kv_heads, geo.head_dim
+        pools = (k_pool.data_ptr(), v_pool.data_ptr(), scales4.data_ptr())
     _require(table, torch.float32, "table", device)
     if table.dim() != 3 or table.shape[2] != 2:
         raise ValueError("table must be [positions][rotary_dim / 2][2]")
     T = int(batch.cu_new_lens[-1])
-    _, Hkv, _, D = k_pool.shape
-    if scales4 is not None:
-        D *= 2
     kv_shape = (T, Hkv, D)
     k_stride = _require_rows(k_new, "k_new", kv_shape, device)
     v_stride = _require_rows(v_new, "v_new", kv_shape, device)
@@ -716,11 +717,13 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
     elif q_out is not None:
         raise ValueError("q_out without q")
     rows = NewRows(q_at, k_new.data_ptr(), v_new.data_ptr(), q_stride, k_stride, v_stride)
-    geo = (_geo_from_pools if scales4 is None else _geo_from_pools4)(k_pool, v_pool, Hq, batch)
+    if scales4 is None:
+        geo = _geo_from_pools(k_pool, v_pool, Hq, batch)
+    else:
+        geo.num_q_heads = Hq
     rot = Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1],
                  PAIRS_INTERLEAVED if interleaved else PAIRS_HALVES)
     byref = ctypes.byref
-    pools = (k_pool.data_ptr(), v_pool.data_ptr()) + (() if scales4 is None else (scales4.data_ptr(),))
     st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), byref(rot), byref(rows), out_at, *scales, *pools)
     _check(fn, st, lib)
     return q_out
@@ -760,16 +763,27 @@ def alloc_pools_fp4(num_blocks, num_kv_heads, head_dim, device="cuda"):
     return (*codes, torch.full((*shape, head_dim // 32, 2), 127, dtype=torch.uint8, device=device))
 
 
-def _require_pools4(k_pool4, v_pool4, scales4, device):
+def _require_pools4(k_pool4, v_pool4, scales4, q_heads, batch):
+    """The geometry of 4-bit pools (q_heads None: as many query heads as KV heads)."""
     torch = _t()
-    _require(k_pool4, torch.uint8, "k_pool4", device)
-    _require(v_pool4, torch.uint8, "v_pool4", device)
-    _require(scales4, torch.uint8, "scales4", device)
-    if k_pool4.dim() != 4:
+    device, u8, tensor = batch.device, torch.uint8, torch.Tensor
+    # one test for what every valid call passes, the tests one by one for the others
+    if not (isinstance(k_pool4, tensor) and isinstance(v_pool4, tensor) and isinstance(scales4, tensor) and k_pool4.is_cuda and
+            k_pool4.dtype is u8 and v_pool4.dtype is u8 and scales4.dtype is u8 and k_pool4.device == device and
+            v_pool4.device == device and scales4.device == device and k_pool4.is_contiguous() and v_pool4.is_contiguous() and
+            scales4.is_contiguous()):
+        _require(k_pool4, u8, "k_pool4", device)
+        _require(v_pool4, u8, "v_pool4", device)
+        _require(scales4, u8, "scales4", device)
+    shape = k_pool4.shape
+    if len(shape) != 4:
         raise ValueError("k_pool4 must be [NB][Hkv][16][D / 2]")
-    NB, Hkv, S, half = k_pool4.shape
+    NB, Hkv, S, half = shape
+    if v_pool4.shape != shape:
+        raise ValueError(f"v_pool4 must have k_pool4's shape [NB][Hkv][S][D / 2] = {tuple(shape)}, got {tuple(v_pool4.shape)}")
     if scales4.shape != (NB, Hkv, S, half // 16, 2):
         raise ValueError(f"scales4 must be [NB][Hkv][S][D / 32][2] = {(NB, Hkv, S, half // 16, 2)}, got {tuple(scales4.shape)}")
+    return Geometry(Hkv if q_heads is None else q_heads, Hkv, 2 * half, S, NB, batch.max_blocks_per_seq)
 
 
 def kv_append_fp4(k_new, v_new, k_pool4, v_pool4, scales4, batch: PagedBatch, stream=None):
@@ -778,8 +792,7 @@ def kv_append_fp4(k_new, v_new, k_pool4, v_pool4, scales4, batch: PagedBatch, st
     torch = _t()
     lib = load_library()
     device = batch.device
-    _require_pools4(k_pool4, v_pool4, scales4, device)
-    geo = _geo_from_pools4(k_pool4, v_pool4, k_pool4.shape[1], batch)
+    geo = _require_pools4(k_pool4, v_pool4, scales4, None, batch)
     shape = (int(batch.cu_new_lens[-1]), geo.num_kv_heads, geo.head_dim)
     _require_host_or_device_rows(k_new, "k_new", shape, device)
     _require_host_or_device_rows(v_new, "v_new", shape, device)
@@ -814,10 +827,9 @@ def _attention_fp4(fn, q, k_pool4, v_pool4, scales4, batch, scale, workspace, ou
     torch = _t()
     lib = load_library()
     device = batch.device
-    _require_pools4(k_pool4, v_pool4, scales4, device)
     _require(q, torch.bfloat16, "q", device)
     T, Hq, D = q.shape
-    geo = _geo_from_pools4(k_pool4, v_pool4, Hq, batch)
+    geo = _require_pools4(k_pool4, v_pool4, scales4, Hq, batch)
     if T != int(batch.cu_new_lens[-1]) or D != geo.head_dim:
         raise ValueError("q must be [T][Hq][D] matching the batch and pools")
     if workspace is None:
@@ -904,8 +916,7 @@ def kv_read_fp8(k_pool8, v_pool8, batch: PagedBatch, k_scale, v_scale, k_out=Non
 
 def kv_read_fp4(k_pool4, v_pool4, scales4, batch: PagedBatch, k_out=None, v_out=None, stream=None):
     """kv_read from 4-bit pools: exactly the numbers that the pools hold."""
-    _require_pools4(k_pool4, v_pool4, scales4, batch.device)
-    geo = _geo_from_pools4(k_pool4, v_pool4, k_pool4.shape[1], batch)
+    geo = _require_pools4(k_pool4, v_pool4, scales4, None, batch)
     return _read("gc_kv_read_fp4", k_pool4, v_pool4, geo, batch, (scales4.data_ptr(),), k_out, v_out, stream)
 
 
