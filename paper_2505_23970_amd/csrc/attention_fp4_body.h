@@ -457,10 +457,11 @@ struct Fp4Lds {
     __align__(16) unsigned char s[kSlots][kScaleBytes];
 };
 
-template <int D, int WAVES>
-__device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const unsigned bid, Fp4Lds<D, WAVES>& lds) {
-    constexpr int ROWS = kRowsPerWave;
-    constexpr int RB = ROWS / 16;
+// Work item `it` by this wavefront, which has RB 16-row blocks of the tile. Wavefronts with one block and with two meet at the same
+// barriers.
+template <int D, int WAVES, int RB>
+__device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const WorkItem it, const int kvh, Fp4Lds<D, WAVES>& lds) {
+    constexpr int ROWS = 16 * RB;
     constexpr int KB = kBlockN / 16;   // key blocks (pages) of a tile
     constexpr int DB = D / 16;
     constexpr int NB = D / kFp4Block;
@@ -474,22 +475,18 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     const int tid = tid_opaque, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, j16 = lane & 15;
-    // (4 wavefronts: one of the two workgroups on a compute unit is preferred, attention_kernels.h)
-    if (WAVES != kWideWaves && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd) __builtin_amdgcn_s_setprio(2);
-    const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
-    const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
-    asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P), "s"(it.cu), "s"(it.n));
-    if (it.r < 0 || it.kt_begin >= it.kt_end) return;
     const int P = it.P, cu = it.cu, n = it.n;
     const int L = item_keys(it);
     const int ntok = min(a.tq, n - it.q0);
 
+    // row of the tile of this wavefront's row
+    auto row_of = [&](int row) { return WAVES == kWideWaves ? wave * ROWS + row : 16 * (wave + (row >> 4) * WAVES) + (row & 15); };
     bool row_ok[RB];
     int lim[RB];  // last key the row may see
     int64_t qrow[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int m = wave * ROWS + 16 * rb + j16;
+        const int m = row_of(16 * rb + j16);
         const int t = (int)((unsigned)m / (unsigned)a.group);
         row_ok[rb] = t < ntok;
         lim[rb] = P + it.q0 + (row_ok[rb] ? t : 0);
@@ -675,7 +672,7 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
     };
     auto weights = [&](int hb) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) w_pair(x & 1, hb, x >> 1);
+        for (int x = 0; x < 4 * RB; ++x) w_pair(x % RB, hb, x / RB);
     };
     auto value_products = [&](int buf, int i) {
         if (i + kAhead < 2 * DB) vread(buf, i + kAhead);
@@ -881,7 +878,7 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
                 *reinterpret_cast<u32x2*>(at(2 * db + (g4 >> 1)) + 8 * (g4 & 1)) = w;
             },
             [&](int row, int ch, const u32x4 w) {
-                const int m = wave * ROWS + row;
+                const int m = row_of(row);
                 const int t = (int)((unsigned)m / (unsigned)a.group);
                 if (t < ntok)
                     *reinterpret_cast<u32x4*>(a.out + ((int64_t)(cu + it.q0 + t) * a.num_q_heads + kvh * a.group + (m - t * a.group)) * D + ch * 8) = w;
@@ -892,14 +889,39 @@ __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const u
                 if (row_ok[rb]) a.lse[qrow[rb]] = lse_v[rb];
         }
     } else {
-        const int64_t prow0 = ((int64_t)it.part * a.num_kv_heads + kvh) * (WAVES * ROWS) + wave * ROWS;
+        const int64_t prow0 = ((int64_t)it.part * a.num_kv_heads + kvh) * (WAVES * kRowsPerWave);
         through_stage(std::integral_constant<int, 4 * D>{},
             [&](int rb, int db, auto&& at) { *reinterpret_cast<f32x4*>(at(4 * db + g4)) = o[rb][db] * inv[rb]; },
-            [&](int row, int ch, const u32x4 w) { *reinterpret_cast<u32x4*>(a.part_o + (prow0 + row) * D + ch * 4) = w; });
+            [&](int row, int ch, const u32x4 w) {
+                const int m = row_of(row);
+                if (m < ntok * a.group) *reinterpret_cast<u32x4*>(a.part_o + (prow0 + m) * D + ch * 4) = w;
+            });
         if (g4 == 0) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) a.part_lse[prow0 + 16 * rb + j16] = lse_v[rb];
+            for (int rb = 0; rb < RB; ++rb) a.part_lse[prow0 + row_of(16 * rb + j16)] = lse_v[rb];
         }
+    }
+}
+
+// Rows of a tile: 8 wavefronts take 32 in a row each. Of 4, wavefront w takes the 16-row blocks w and w + 4, and only the first where
+// the second is empty: a tile of up to 64 rows costs half (24 requests of 10 tokens, 32 heads on 8, d = 64: 33.5 -> 23.8 us; of 20
+// tokens 38 -> 36; 8 requests of 288, d = 128, whose tiles are full, 101 -> 102).
+template <int D, int WAVES>
+__device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const unsigned bid, Fp4Lds<D, WAVES>& lds) {
+    constexpr int RB = kRowsPerWave / 16;
+    // (4 wavefronts: one of the two workgroups on a compute unit is preferred, attention_kernels.h)
+    if (WAVES != kWideWaves && D == 128 && (bid / a.prefer_span & 1) == a.prefer_odd) __builtin_amdgcn_s_setprio(2);
+    const int kvh = (int)(bid % (unsigned)a.num_kv_heads);
+    const WorkItem it = a.items[bid / (unsigned)a.num_kv_heads];
+    asm volatile("" ::"s"(it.r), "s"(it.q0), "s"(it.kt_begin), "s"(it.kt_end), "s"(it.part), "s"(it.P), "s"(it.cu), "s"(it.n));
+    if (it.r < 0 || it.kt_begin >= it.kt_end) return;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if constexpr (WAVES == kWideWaves) {
+        fp4_attention_rows<D, WAVES, RB>(a, it, kvh, lds);
+    } else {
+        static_assert(RB == 2, "row blocks");
+        if (__builtin_expect(16 * (wave + WAVES) < min(a.tq, it.n - it.q0) * a.group, 1)) fp4_attention_rows<D, WAVES, 2>(a, it, kvh, lds);
+        else fp4_attention_rows<D, WAVES, 1>(a, it, kvh, lds);
     }
 }
 

@@ -505,3 +505,15 @@ def test_refusals():
                  lambda: gc.kv_read(k, v, b)):
         with pytest.raises((TypeError, ValueError)):
             call()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 32, 8), (128, 8, 1), (128, 12, 4)])
+@pytest.mark.parametrize("split", [None, -1, 2])
+def test_tiles_that_are_not_full(D, Hq, Hkv, split):
+    """128-row tiles of 1 to 128 rows: every number of 16-row blocks a wavefront, at its borders."""
+    g = Hq // Hkv
+    n = sorted({max(1, min(128 // g, (16 * b + d) // g)) for b in (0, 1, 3, 4, 5, 7, 8) for d in (-1, 0, 1, g)})
+    P = np.arange(len(n)) * 37 % 200
+    w = W.build(P, n, Hq, Hkv, D, seed=2580 + Hq + D, values="peaked", name=f"fp4_partial_{Hq}_{Hkv}_d{D}")
+    run, ref = appended(w)
+    check(w, *run.attention(split=split, tiling=1), ref)
