@@ -159,7 +159,8 @@ __device__ __forceinline__ void rotary_kv(const RotaryArgs& ra, AppendLds<D>& sm
 // The same into 4-bit pools (fp4.h), whose pages hold whole rows of keys and of values: a token's codes share
 // no byte with another token's. Four lanes hold the 32 elements of a block. Rotated keys are computed in 64
 // bits and rounded to 32 (the products of a bf16 and an fp32 number are exact there, so that the codes are those
-// of the definition, next to a border too): the conversions and products cost nothing that shows beside the memory.
+// of the definition, next to a border too): the conversions and products cost nothing that shows beside the memory (16 prompts
+// of 1900 tokens, 64 heads on 8, d = 128, 1200 MB: 209 us, 5.7 TB/s; 96 single tokens 5.3 us, one 3.7).
 template <int D>
 __device__ __forceinline__ void rotary_kv_fp4(const RotaryArgs& ra, const PageUnit& at, int lp, int s0, int s1, int hg) {
     const AppendArgs& a = ra.a;
