@@ -447,7 +447,7 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 // Query tiles of 32 rows a wavefront, key tiles of 64 (four pages). Pages of codes and of scales are copied straight into
 // LDS, two tiles ahead; keys are multiplied as they are, values are widened from there into rows of bf16, a tile ahead.
 // What bounds it: the matrix cores and, beside them, the softmax's vector instructions. 6 prompts of 800 tokens on 9000, 64 heads
-// on 8, d = 128 (wide tiles, 1.09 TFLOP): 815-837 us, 1300-1340 TFLOP/s, matrix cores busy 62 % of the time; over bf16 pools 928.
+// on 8, d = 128 (wide tiles, 1.09 TFLOP): 815-837 us, 1300-1340 TFLOP/s, matrix cores busy 62 % of the time (839 beside 881 over bf16 pools).
 // 8 requests of 288 on 2560, 32 heads on 8 (128-row tiles): 102 us, of which the slot that ends last has 60 key tiles on a mean
 // of 46. At d = 64 (24 requests of 20 on 3000) 36 us: vector instructions 52 % of the cycles, matrix cores 35 %, little of
 // it at once with two wavefronts a SIMD; copies three tiles ahead, or three workgroups a compute unit, change nothing.
