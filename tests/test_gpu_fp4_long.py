@@ -168,3 +168,36 @@ def test_batches_without_work():
         check(w, out, lse, ref)
         got = gc.kv_read_fp4(*run.dev, run.batch)[1]
         assert torch.equal(out, got.repeat_interleave(4, dim=1))
+
+
+def test_calls_side_by_side_and_appends_in_a_graph():
+    """Attention of three batches on three streams at once, each with its own workspace; an append captured and replayed."""
+    import torch
+    import paper_2505_23970_amd as gc
+    cases = [W.build(P, n, 16, 2, 128, seed=4500 + i, values="peaked", name=f"fp4_beside_{i}")
+             for i, (P, n) in enumerate((([3000, 500], [1, 1]), ([700, 0], [60, 90]), ([64] * 20, [130] * 20)))]
+    runs = [appended(w)[0] for w in cases]
+    want = [[t.clone() for t in r.attention()] for r in runs]
+    streams = [torch.cuda.Stream() for _ in cases]
+    plans = [gc.alloc_workspace(16, r.k, r.v, r.batch) for r in runs]
+    outs = [torch.empty_like(r.q) for r in runs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o in outs:
+            o.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for r, s, ws, o in zip(runs, streams, plans, outs):
+            gc.prefix_prefill_attention_fp4(r.q, *r.dev, r.batch, r.w.scale, ws, out=o, stream=s)
+        torch.cuda.synchronize()
+        for o, (x, _) in zip(outs, want):
+            assert torch.equal(o.view(torch.int16), x.view(torch.int16))
+    r = runs[1]
+    images = r.images()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r.append()
+    for _ in range(3):
+        for t, image in zip(r.dev, (r.k4, r.v4, r.s4)):
+            t.copy_(H.to_dev_u8(image))
+        graph.replay()
+        same_pools(r.images(), images)
