@@ -210,9 +210,9 @@ def _stream_handle(stream=None):
 
 def _require(t, dtype, name, device=None):
     torch = _t()
-    # one test for what every valid call passes, the tests one by one for the others
-    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous() and
-            (device is None or t.device == device)):
+    # one test for what every valid call passes (get_device: -1 for tensors elsewhere), the tests one by one for the others
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and
+            (t.is_cuda if device is None else t.get_device() == device.index)):
         return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
@@ -633,7 +633,7 @@ def _require_rows(t, name, shape, device):
     torch = _t()
     T, heads, D = shape
     # one test for what every valid call passes, the tests one by one for the others
-    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.device == device:
+    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device.index:
         between, heads_apart, step = t.stride()
         if step == 1 and heads_apart == D:
             if T == 1:
@@ -665,9 +665,9 @@ def _here(device, stream, call, *args):
     torch = _t()
     if stream is not None and stream.device != device:
         raise ValueError(f"stream is on {stream.device}, the batch on {device}")
-    index = device.index
-    if torch.cuda.current_device() == index:
-        return call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    index, c = device.index, torch._C
+    if c._cuda_getDevice() == index:  # (the batch's tensors live there: the runtime is up)
+        return call(*args, c._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
     with torch.cuda.device(device):
         return call(*args, _stream_handle(stream))
 
@@ -697,7 +697,8 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
         Hkv, D = geo.num_kv_heads, geo.head_dim
         pools = (k_pool.data_ptr(), v_pool.data_ptr(), scales4.data_ptr())
     _require(table, torch.float32, "table", device)
-    if table.dim() != 3 or table.shape[2] != 2:
+    angles = table.shape
+    if len(angles) != 3 or angles[2] != 2:
         raise ValueError("table must be [positions][rotary_dim / 2][2]")
     T = int(batch.cu_new_lens[-1])
     kv_shape = (T, Hkv, D)
@@ -721,7 +722,7 @@ def _append_rotary(fn, q, k_new, v_new, k_pool, v_pool, batch, table, q_out, int
         geo = _geo_from_pools(k_pool, v_pool, Hq, batch)
     else:
         geo.num_q_heads = Hq
-    rot = Rotary(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+    rot = Rotary(table.data_ptr(), angles[0], 2 * angles[1],
                  PAIRS_INTERLEAVED if interleaved else PAIRS_HALVES)
     byref = ctypes.byref
     st = _here(device, stream, getattr(lib, fn), byref(geo), byref(batch._desc), byref(rot), byref(rows), out_at, *scales, *pools)
@@ -767,11 +768,12 @@ def _require_pools4(k_pool4, v_pool4, scales4, q_heads, batch):
     """The geometry of 4-bit pools (q_heads None: as many query heads as KV heads)."""
     torch = _t()
     device, u8, tensor = batch.device, torch.uint8, torch.Tensor
-    # one test for what every valid call passes, the tests one by one for the others
-    if not (isinstance(k_pool4, tensor) and isinstance(v_pool4, tensor) and isinstance(scales4, tensor) and k_pool4.is_cuda and
-            k_pool4.dtype is u8 and v_pool4.dtype is u8 and scales4.dtype is u8 and k_pool4.device == device and
-            v_pool4.device == device and scales4.device == device and k_pool4.is_contiguous() and v_pool4.is_contiguous() and
-            scales4.is_contiguous()):
+    index = device.index
+    # one test for what every valid call passes (get_device: -1 for tensors elsewhere), the tests one by one for the others
+    if not (isinstance(k_pool4, tensor) and isinstance(v_pool4, tensor) and isinstance(scales4, tensor) and
+            k_pool4.dtype is u8 and v_pool4.dtype is u8 and scales4.dtype is u8 and k_pool4.get_device() == index and
+            v_pool4.get_device() == index and scales4.get_device() == index and k_pool4.is_contiguous() and
+            v_pool4.is_contiguous() and scales4.is_contiguous()):
         _require(k_pool4, u8, "k_pool4", device)
         _require(v_pool4, u8, "v_pool4", device)
         _require(scales4, u8, "scales4", device)
@@ -858,7 +860,7 @@ def _attention_fp4(fn, q, k_pool4, v_pool4, scales4, batch, scale, workspace, ou
 def _require_host_or_device_rows(t, name, shape, device):
     """Contiguous bf16 rows [T][heads][D] on the batch's device or in pinned host memory."""
     torch = _t()
-    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.is_contiguous() and t.device == device:
+    if isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.shape == shape and t.is_contiguous() and t.get_device() == device.index:
         return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
