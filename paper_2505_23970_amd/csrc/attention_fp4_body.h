@@ -447,7 +447,7 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 // Query tiles of 32 rows a wavefront, key tiles of 64 (four pages). Pages of codes and of scales are copied straight into
 // LDS, two tiles ahead; keys are multiplied as they are, values are widened from there into rows of bf16, a tile ahead.
 // What bounds it: the matrix cores and, beside them, the softmax's vector instructions. 6 prompts of 800 tokens on 9000, 64 heads
-// on 8, d = 128 (wide tiles, 1.09 TFLOP): 815-837 us, 1300-1340 TFLOP/s, matrix cores busy 62 % of the time (839 beside 881 over bf16 pools).
+// on 8, d = 128 (wide tiles, 1.09 TFLOP): 805-830 us, 1320-1360 TFLOP/s, matrix cores busy 62 % of the time (830 where bf16 pools take 881).
 // 8 requests of 288 on 2560, 32 heads on 8 (128-row tiles): 102 us, of which the slot that ends last has 60 key tiles on a mean
 // of 46. At d = 64 (24 requests of 20 on 3000) 36 us: vector instructions 52 % of the cycles, matrix cores 35 %, little of
 // it at once with two wavefronts a SIMD; copies three tiles ahead, or three workgroups a compute unit, change nothing.
@@ -474,7 +474,9 @@ __device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const W
     constexpr int kPageCodes = kPage * D / 2;
     constexpr int kPageScales = kPage * NB * 2;
     constexpr int kTileLog2Thresh = 8;
-    constexpr int kAhead = 4;  // value fragments read ahead of their products
+    // Value fragments read ahead of their products (wide tiles: 2 and 3 take 830 us on the prompts above, 4 844, 5 860, 1 835;
+    // 128-row tiles: 2 to 4 the same).
+    constexpr int kAhead = 3;
 
     int tid_opaque = (int)threadIdx.x;  // (lane constants per work item, not held across a resident launch's items)
     asm volatile("" : "+v"(tid_opaque));
@@ -758,8 +760,8 @@ __device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const W
     //     turn after, and needed from turn 2 t + 3 (values, scales) and 2 t + 4 (keys) on; what lay there was tile t - 2's,
     //     whose scales were read last in turn 2 t - 1.
     auto change = [&]() {  // (this wavefront's writes to LDS are over; the reads of the first value fragments may go on)
-        static_assert(2 * kAhead == 8, "the wait");
-        asm volatile("s_waitcnt lgkmcnt(8)" ::: "memory");
+        static_assert(2 * kAhead == 6, "the wait");
+        asm volatile("s_waitcnt lgkmcnt(6)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
