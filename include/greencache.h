@@ -505,7 +505,9 @@ gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const vo
  * gc_prefix_prefill_run and gc_prefix_prefill_attention (plan and run) over 4-bit pools: the same attention with
  * every key and value element as the number it stands for. Plans, workspaces, tilings and options are
  * those of the other pools (gc_prefix_prefill_plan and gc_prefix_prefill_workspace_size serve all). A value
- * block that is NaN makes those rows NaN that see its token, in its elements. Errors as those calls, and
+ * block that is NaN makes those rows NaN that see its token, in its elements. Scores are sums in fp32, but of
+ * products q k that are added in groups of eight elements on a grid of 2^-13 to 2^-12 of the group's largest: a
+ * score is off by at most scale times the sum over groups of 7 * 2^-12 max |q k|. Errors as those calls, and
  * GC_ERR_BAD_SHAPE for q or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_UNSUPPORTED
  * for a batch of more work than one launch holds. Shared prefixes (gc_shared_prefix_*) are over bf16 and 8-bit
  * pools only.

@@ -517,3 +517,65 @@ def test_tiles_that_are_not_full(D, Hq, Hkv, split):
     w = W.build(P, n, Hq, Hkv, D, seed=2580 + Hq + D, values="peaked", name=f"fp4_partial_{Hq}_{Hkv}_d{D}")
     run, ref = appended(w)
     check(w, *run.attention(split=split, tiling=1), ref)
+
+
+def score_errors(w, images):
+    """For every output row the most that one of its scores may be off by. The matrix products add the terms q k of eight
+    neighbouring elements on a grid of 2^-13 of the largest one's power of two (of twice that where the key's code is 0.5), towards zero: each of
+    the seven others loses less than 2^-12 of the largest. The split of a query adds 2^-22 of the row's largest per element, and its second part, at
+    most 2^-4 of the first, as much of its own terms; fp32 sums, the scale and the offset round at 2^-24 of the sum of magnitudes, a few times."""
+    T, Hq, D = w.q.shape
+    q = np.abs(R.rows_of(w.q))
+    out = np.zeros((T, Hq))
+    k4 = np.abs(R.values(images[0], images[2][..., 0]))
+    for r in range(w.batch):
+        L = int(w.prefix_lens[r] + w.new_lens[r])
+        pos = np.arange(L)
+        k = k4[w.block_tables[r][pos // 16], :, pos % 16]             # [L][Hkv][D]
+        for t in range(int(w.cu_new_lens[r]), int(w.cu_new_lens[r + 1])):
+            seen = int(w.prefix_lens[r]) + t - int(w.cu_new_lens[r]) + 1
+            for h in range(Hq):
+                terms = q[t, h] * k[:seen, h // (Hq // w.num_kv_heads)]
+                lost = 7 * 2.0 ** -12 * (1 + 2.0 ** -4) * terms.reshape(seen, D // 8, 8).max(axis=-1).sum(axis=-1)
+                lost += 2.0 ** -22 * q[t, h].max() * k[:seen, h // (Hq // w.num_kv_heads)].sum(axis=-1) + 2.0 ** -21 * terms.sum(axis=-1)
+                out[t, h] = w.scale * lost.max()
+    return out.reshape(T * Hq)
+
+
+def check_large_scores(w, out, lse, images):
+    """The bounds of check, and what scores off by up to d do: weights change by factors within e^(+-2 d), so that an output moves by
+    at most (e^(2 d) - 1) max |v|, and by no more than 2 max |v|; the log-sum-exp moves by d."""
+    ref, ref_lse = H.oracle_rows(w, *R.as_bf16_pools(*images))
+    T, Hq, D = w.q.shape
+    vmax = 2 * float(np.abs(W.bf16_bits_to_f32(np.concatenate([w.v_new.ravel(), w.v_prefix.ravel()]))).max(initial=0.0))
+    d = score_errors(w, images)
+    got, got_lse = numbers(out).reshape(T * Hq, D), numbers(lse).reshape(T * Hq)
+    more = vmax * np.minimum(np.expm1(np.minimum(2 * d, 1.0)), 2.0)
+    more[2 * d > 1] = 2 * vmax
+    assert np.all(np.abs(got - ref) <= H.derived_bound(ref, vmax) + more[:, None])
+    assert np.all(np.abs(got_lse - ref_lse) <= 2.0 ** -8 + 1e-5 * np.abs(ref_lse) + d), np.abs(got_lse - ref_lse).max()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [35, 45, 61])
+@pytest.mark.parametrize("jump", [9000.0, 900000.0])
+def test_second_pass_of_tiles_that_are_not_full(jump, n, D):
+    """Score jumps that only a few of a tile's 70 to 122 rows see, in their last blocks or in their first ones: the wavefronts of one and
+    of two row blocks take the second pass together."""
+    for last in (True, False):
+        w = W.build([300], [n], 4, 2, D, seed=2750 + n, values="unit", name=f"fp4_jumps_{n}_{last}")
+        w.k_prefix[:] = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.k_prefix) * np.float32(0.01))
+        w.k_new[:] = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.k_new) * np.float32(0.01))
+        if last:
+            w.k_new[n - 3] = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.k_new[n - 3]) * np.float32(jump))
+        else:
+            w.k_prefix[290] = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.k_prefix[290]) * np.float32(jump))
+            w.q[8:] = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.q[8:]) * np.float32(2.0 ** -14))
+        w.finish()
+        run, ref = appended(w)
+        for split in (None, -1, 2):
+            out, lse = run.attention(tiling=1, split=split)
+            if jump < 10000:
+                check(w, out, lse, ref)
+            else:
+                check_large_scores(w, out, lse, run.images())
