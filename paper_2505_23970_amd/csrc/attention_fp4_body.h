@@ -455,8 +455,8 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 // What bounds it: the matrix cores and, beside them, the softmax's vector instructions. 6 prompts of 800 tokens on 9000, 64 heads
 // on 8, d = 128 (wide tiles, 1.09 TFLOP): 805-830 us, 1320-1360 TFLOP/s, matrix cores busy 62 % of the time (830 where bf16 pools take 881).
 // 8 requests of 288 on 2560, 32 heads on 8 (128-row tiles): 102 us, of which the slot that ends last has 60 key tiles on a mean
-// of 46. At d = 64 (24 requests of 20 on 3000) 36 us: vector instructions 52 % of the cycles, matrix cores 35 %, little of
-// it at once with two wavefronts a SIMD; copies three tiles ahead, or three workgroups a compute unit, change nothing.
+// of 46. At d = 64 (24 requests of 20 on 3000) 36 us: matrix cores busy 29 % of the cycles, the vector unit about half,
+// little of it at once with two wavefronts a SIMD; copies three tiles ahead, or three workgroups a compute unit, change nothing.
 template <int D, int WAVES>
 struct Fp4Lds {
     static constexpr int kSlots = 4;  // tiles t to t + 2 are in use, and the scales of t - 1
