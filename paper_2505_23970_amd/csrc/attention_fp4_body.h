@@ -765,6 +765,8 @@ __device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const W
     //   - codes of tile t + 2 are asked for in turn 2 t + 1 (values, scales) and 2 t + 2 (keys), waited for at the end of the
     //     turn after, and needed from turn 2 t + 3 (values, scales) and 2 t + 4 (keys) on; what lay there was tile t - 2's,
     //     whose scales were read last in turn 2 t - 1.
+    // Both halves pass the same number of barriers. The last one of those ahead comes before the last products of those
+    // behind: whoever writes to the value buffers after turns() needs a barrier of its own.
     auto change = [&]() {  // (this wavefront's writes to LDS are over; the reads of the first value fragments may go on)
         static_assert(2 * kAhead == 6, "the wait");
         asm volatile("s_waitcnt lgkmcnt(6)" ::: "memory");
@@ -843,7 +845,13 @@ __device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const W
                 if (++tile >= tiles) break;
             }
         }
-        if (exact || !__syncthreads_or(!(l_run[0][0] <= 0x1p100f) || !(l_run[RB - 1][0] <= 0x1p100f))) break;
+        // (A barrier after either pass: wavefronts behind leave turns() with value reads that no barrier has followed, of the
+        // buffers that the others then stage their output rows in.)
+        if (exact) {
+            __syncthreads();
+            break;
+        }
+        if (!__syncthreads_or(!(l_run[0][0] <= 0x1p100f) || !(l_run[RB - 1][0] <= 0x1p100f))) break;
         exact = true;
     }
 
