@@ -292,8 +292,11 @@ def _geo_from_pools4(k_pool4, v_pool4, q_heads, batch: PagedBatch):
 
 
 def _geo_for_plan(k_pool, v_pool, q_heads, batch: PagedBatch):
-    """The geometry of pools of any kind (value pages of 4-bit pools are not transposed)."""
-    four = k_pool.dtype == _t().uint8 and k_pool.shape == v_pool.shape
+    """The geometry of pools of any kind. 4-bit pools are known by their rows of D / 2 = 32 or 64 bytes and by value pages that are
+    not transposed. (8-bit pools of D = 64 with value pages left untransposed have the very shapes of 4-bit pools of
+    D = 128 and are planned as such; every call that reads or writes them refuses them.)"""
+    four = (k_pool.shape == v_pool.shape and len(k_pool.shape) == 4 and k_pool.shape[3] in (32, 64) and
+            k_pool.dtype == _t().uint8)
     return (_geo_from_pools4 if four else _geo_from_pools)(k_pool, v_pool, q_heads, batch)
 
 
