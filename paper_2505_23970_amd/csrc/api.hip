@@ -465,15 +465,17 @@ int resident_workgroups(const gc_geometry* geo, const Shape& sh, const Plan& pl)
 }
 
 // Pools of bf16 elements (fp8 false, scales 1), of E4M3 codes with one scale each, or of E2M1 codes
-// with scales of their own (scales4 not null).
+// with scales of their own.
 struct PoolKind {
     bool fp8 = false;
     float k_scale = 1.f, v_scale = 1.f;
+    bool fp4 = false;
     const void* scales4 = nullptr;
-    gc::Pool pool() const { return scales4 != nullptr ? gc::Pool::kFp4 : fp8 ? gc::Pool::kFp8 : gc::Pool::kBf16; }
+    gc::Pool pool() const { return fp4 ? gc::Pool::kFp4 : fp8 ? gc::Pool::kFp8 : gc::Pool::kBf16; }
 };
 PoolKind fp4_pools(const void* scales) {
     PoolKind pk;
+    pk.fp4 = true;
     pk.scales4 = scales;
     return pk;
 }
@@ -503,7 +505,7 @@ gc_status enqueue_run(const gc_geometry* geo, const gc_batch* b, const Shape& sh
     a.prefer_span = (uint32_t)device_cus();
     a.prefer_odd = pl.heaviest_decides ? 0 : 1;
     hipError_t e;
-    if (pk.scales4 != nullptr) {
+    if (pk.fp4) {
         gc::Fp4AttnArgs a4{a, static_cast<const uint8_t*>(pk.scales4)};
         e = gc::launch_attention_fp4(a4, geo->head_dim, pl.items, sh.small, sh.wide, resident_workgroups(geo, sh, pl), stream);
     } else if (sh.small) {
@@ -702,6 +704,7 @@ gc_status read_rows(const gc_geometry* geo, const gc_batch* batch, const void* k
     gc_status st = check_common(geo, batch, &sh);
     if (st != GC_OK || sh.total_tokens == 0) return st;
     if (k_pool == nullptr || v_pool == nullptr || k_out == nullptr || v_out == nullptr) return GC_ERR_NULL_ARG;
+    if (pk.fp4 && pk.scales4 == nullptr) return GC_ERR_NULL_ARG;
     if (!aligned16(k_pool) || !aligned16(v_pool) || !aligned16(pk.scales4) || !aligned16(k_out) || !aligned16(v_out))
         return GC_ERR_BAD_SHAPE;
     const gc::Pool kind = pk.pool();
@@ -760,7 +763,7 @@ gc_status run(const gc_geometry* geo, const gc_batch* batch, const gc_plan_optio
         st = check_pool_scales(pk.k_scale, pk.v_scale);
         if (st != GC_OK) return st;
     }
-    if (pk.scales4 != nullptr) {
+    if (pk.fp4) {
         st = check_fp4(k_pool, v_pool, pk.scales4);
         if (st != GC_OK) return st;
         if (!aligned16(q) || !aligned16(out)) return GC_ERR_BAD_SHAPE;
@@ -1337,7 +1340,6 @@ __attribute__((visibility("default")))
 gc_status gc_kv_append_rotary_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
                                   const gc_new_rows* rows, void* q_out, void* k_pool4, void* v_pool4, void* scales4,
                                   hipStream_t stream) {
-    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
     return append_rotary(geo, batch, rotary, rows, q_out, k_pool4, v_pool4, fp4_pools(scales4), stream);
 }
 
@@ -1358,7 +1360,6 @@ gc_status gc_kv_read_fp8(const gc_geometry* geo, const gc_batch* batch, const vo
 __attribute__((visibility("default")))
 gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_pool4, const void* v_pool4,
                          const void* scales4, void* k_out, void* v_out, hipStream_t stream) {
-    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
     return read_rows(geo, batch, k_pool4, v_pool4, fp4_pools(scales4), k_out, v_out, stream);
 }
 
@@ -1367,7 +1368,6 @@ gc_status gc_prefix_prefill_run_fp4(const gc_geometry* geo, const gc_batch* batc
                                     const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
                                     float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
                                     hipStream_t stream) {
-    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
     return run(geo, batch, opts, q, k_pool4, v_pool4, scale, out, lse, workspace, workspace_bytes, stream, false,
                fp4_pools(scales4));
 }
@@ -1377,7 +1377,6 @@ gc_status gc_prefix_prefill_attention_fp4(const gc_geometry* geo, const gc_batch
                                           const void* q, const void* k_pool4, const void* v_pool4, const void* scales4,
                                           float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
                                           hipStream_t stream) {
-    if (scales4 == nullptr) return GC_ERR_NULL_ARG;
     return run(geo, batch, opts, q, k_pool4, v_pool4, scale, out, lse, workspace, workspace_bytes, stream, true,
                fp4_pools(scales4));
 }
