@@ -768,7 +768,10 @@ gc_status run(const gc_geometry* geo, const gc_batch* batch, const gc_plan_optio
         if (st != GC_OK) return st;
         if (!aligned16(q) || !aligned16(out)) return GC_ERR_BAD_SHAPE;
         if (!aligned16(workspace)) return GC_ERR_WORKSPACE;
-        if (pl.items * geo->num_kv_heads > gc::kMaxWorkgroups) return GC_ERR_UNSUPPORTED;
+        if (pl.items * geo->num_kv_heads > gc::kMaxWorkgroups ||
+            gc::combine_workgroups(pl.combines, geo->num_kv_heads, sh.block_m, geo->head_dim, pl.max_splits) >
+                (int64_t)UINT32_MAX / gc::kCombineThreads)
+            return GC_ERR_UNSUPPORTED;
     }
     st = check_workspace(pl, workspace, workspace_bytes);
     if (st != GC_OK) return st;

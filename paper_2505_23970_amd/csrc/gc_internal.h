@@ -418,6 +418,7 @@ hipError_t launch_attention_shared(const SharedAttnArgs& a, int head_dim, bool f
 int64_t shared_merge_workgroups(int64_t rows, int head_dim, int max_chunks);  // at most UINT32_MAX / kCombineThreads
 hipError_t launch_shared_merge(const SharedMergeArgs& a, int head_dim, int max_chunks, hipStream_t s);
 // max_splits: the most key chunks of any split query tile
+int64_t combine_workgroups(int64_t num_combines, int num_kv_heads, int block_m, int head_dim, int max_splits);  // of that launch
 hipError_t launch_combine(const CombineArgs& a, int head_dim, int64_t num_combines, int max_splits, hipStream_t s);
 
 }  // namespace gc
