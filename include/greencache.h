@@ -475,8 +475,9 @@ gc_status gc_kv_append_rotary_fp8(const gc_geometry* geo, const gc_batch* batch,
 gc_status gc_kv_append_fp4(const gc_geometry* geo, const gc_batch* batch, const void* k_new, const void* v_new,
                            void* k_pool4, void* v_pool4, void* scales4, hipStream_t stream);
 
-/* gc_kv_append_rotary into 4-bit pools: a rotated key element is the exact x_a cos -+ x_b sin of the table's
- * numbers rounded to fp32, then stored as above. q_out, errors and everything else as there. */
+/* gc_kv_append_rotary into 4-bit pools: a rotated key element is x_a cos -+ x_b sin of the table's numbers, its
+ * two exact products added in 64-bit floating point (one rounding) and the sum rounded to fp32, then stored as above.
+ * q_out, errors and everything else as there. */
 gc_status gc_kv_append_rotary_fp4(const gc_geometry* geo, const gc_batch* batch, const gc_rotary* rotary,
                                   const gc_new_rows* rows, void* q_out, void* k_pool4, void* v_pool4, void* scales4,
                                   hipStream_t stream);
@@ -506,8 +507,10 @@ gc_status gc_kv_read_fp4(const gc_geometry* geo, const gc_batch* batch, const vo
  * every key and value element as the number it stands for. Plans, workspaces, tilings and options are
  * those of the other pools (gc_prefix_prefill_plan and gc_prefix_prefill_workspace_size serve all). A value
  * block that is NaN makes those rows NaN that see its token, in its elements. Scores are sums in fp32, but of
- * products q k that are added in groups of eight elements on a grid of 2^-13 to 2^-12 of the group's largest: a
- * score is off by at most scale times the sum over groups of 7 * 2^-12 max |q k|. Errors as those calls, and
+ * products q k that are added in groups of eight elements on a grid of 2^-13 to 2^-12 of the group's largest (as
+ * measured on gfx950), for a query in two parts, the second at most 2^-4 of the first: a score is off by at most scale times
+ *   sum over groups of 7 * 2^-12 (1 + 2^-4) max |q k|  +  2^-22 max |q| sum |k|  +  2^-21 sum |q k|
+ * (the groups; the queries' split; fp32 sums, scale and offset). Errors as those calls, and
  * GC_ERR_BAD_SHAPE for q or out off 16 bytes (a workspace off 16 bytes: GC_ERR_WORKSPACE), GC_ERR_UNSUPPORTED
  * for a batch of more work than one launch holds. Shared prefixes (gc_shared_prefix_*) are over bf16 and 8-bit
  * pools only.
