@@ -454,9 +454,9 @@ __device__ __forceinline__ void fp4_small_body(const Fp4AttnArgs& a, const WorkI
 // Query tiles of 32 rows a wavefront, key tiles of 64 (four pages). Pages of codes and of scales are copied straight into
 // LDS, two tiles ahead; keys are multiplied as they are, values are widened from there into rows of bf16, a tile ahead.
 // What bounds it: the matrix cores and, beside them, the softmax's vector instructions. 6 prompts of 800 tokens on 9000, 64 heads
-// on 8, d = 128 (wide tiles, 1.09 TFLOP): 805-830 us, 1320-1360 TFLOP/s, matrix cores busy 62 % of the time (830 where bf16 pools take 881).
-// 8 requests of 288 on 2560, 32 heads on 8 (128-row tiles): 102 us, of which the slot that ends last has 60 key tiles on a mean
-// of 46. At d = 64 (24 requests of 20 on 3000) 36 us: matrix cores busy 29 % of the cycles, the vector unit about half,
+// on 8, d = 128 (wide tiles, 1.09 TFLOP): 805-833 us by card, 1310-1360 TFLOP/s, matrix cores busy 60-62 % of the time (830 where bf16 pools take 881).
+// 8 requests of 288 on 2560, 32 heads on 8 (128-row tiles): 102-105 us by card, of which the slot that ends last has 60 key tiles on a mean
+// of 46. At d = 64 (24 requests of 20 on 3000) 35-36 us: matrix cores busy 29 % of the cycles, the vector unit about half,
 // little of it at once with two wavefronts a SIMD; copies three tiles ahead, or three workgroups a compute unit, change nothing.
 template <int D, int WAVES>
 struct Fp4Lds {
@@ -928,7 +928,7 @@ __device__ __forceinline__ void fp4_attention_rows(const Fp4AttnArgs& a, const W
 
 // Rows of a tile: 8 wavefronts take 32 in a row each. Of 4, wavefront w takes the 16-row blocks w and w + 4, and only the first where
 // the second is empty: a tile of up to 64 rows costs half (24 requests of 10 tokens, 32 heads on 8, d = 64: 33.5 -> 23.8 us; of 20
-// tokens 38 -> 36; 8 requests of 288, d = 128, whose tiles are full, 101 -> 102).
+// tokens 38 -> 36). Full tiles pay for it: with the merge, one card, 8 requests of 288, d = 128, 102.7 -> 105.0.
 template <int D, int WAVES>
 __device__ __forceinline__ void fp4_attention_body(const Fp4AttnArgs& a, const unsigned bid, Fp4Lds<D, WAVES>& lds) {
     constexpr int RB = kRowsPerWave / 16;
